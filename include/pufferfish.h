@@ -445,6 +445,187 @@ int pf_lowrank_lstm_stack_bwd(const pf_lstm_stack_desc *d, const void *x,
                               size_t workspace_bytes, void *stream);
 
 /* ------------------------------------------------------------------ */
+/* What a Transformer layer has between its factorized projections      */
+/* (paper Section 2.4): Y[groups, M, out] of pf_lowrank_linear_shared_*  */
+/* holds queries, keys and values as [B, L, heads, head_dim] with        */
+/* M = B L and out = heads head_dim; the calls below take them there,    */
+/* and their backward calls write where pf_lowrank_linear_shared_bwd     */
+/* reads dY.                                                            */
+/*   Strides: these calls alone take tensors that are not dense.  A      */
+/* stride triple holds the elements from one sequence, one token and one */
+/* head to the next; the values of a head are adjacent.  Three zeros:    */
+/* dense [B, L, heads, head_dim].  Otherwise every stride has to be a    */
+/* multiple of 16 bytes and not negative (PF_ERR_UNSUPPORTED); the       */
+/* strides of a tensor that is written must not make elements meet.      */
+/* ------------------------------------------------------------------ */
+
+/* ------------------------------------------------------------------ */
+/* Norms of queries and keys for each head, with the position rotation  */
+/* in the same pass.  For each head x of head_dim values:               */
+/*   PF_NORM_RMS:  u = gamma x / sqrt(mean(x^2) + eps)                  */
+/*   PF_NORM_NONE: u = x                                                */
+/* then the first rot_dim values of u are turned in pairs: pair i of    */
+/* rot_dim / 2 by the angle position * theta^(-2 i / rot_dim),           */
+/*   y1 = u1 cos - u2 sin,  y2 = u1 sin + u2 cos;                       */
+/* PF_ROT_HALVES pairs value i with i + rot_dim / 2, PF_ROT_PAIRS value  */
+/* 2 i with 2 i + 1.  Angles are formed and reduced in double, so that   */
+/* far positions are as exact as near ones.                             */
+/*   Q[B, L, heads_q, head_dim], K[B, L, heads_k, head_dim] in dtype;    */
+/*   gamma_q, gamma_k: float[head_dim], nullable (1);                    */
+/*   positions: int32[B, L], nullable (token l of a sequence stands at l)*/
+/* heads_k == 0: no keys, K and all that belongs to it are not touched.  */
+/* head_dim: a multiple of 8, 8 .. 256; rot_dim: a multiple of 4,        */
+/* 0 .. head_dim; B L heads < 2^31 (PF_ERR_UNSUPPORTED otherwise).       */
+/* Outputs may be the inputs themselves (same strides).                  */
+/* ------------------------------------------------------------------ */
+typedef enum { PF_NORM_NONE = 0, PF_NORM_RMS = 1 } pf_norm;
+typedef enum { PF_ROT_HALVES = 0, PF_ROT_PAIRS = 1 } pf_rotation;
+
+typedef struct {
+    int64_t B, L;
+    int heads_q, heads_k, head_dim, rot_dim;
+    int norm;     /* pf_norm */
+    int rotation; /* pf_rotation */
+    int dtype;    /* pf_dtype */
+    float eps;
+    double theta;
+    int64_t q_stride[3], k_stride[3];   /* Q, K: sequence, token, head */
+    int64_t qo_stride[3], ko_stride[3]; /* Qo, Ko (backward: dQo, dKo) */
+    int64_t dq_stride[3], dk_stride[3]; /* dQ, dK */
+} pf_qk_norm_desc;
+
+/* Qo, Ko: the queries and keys that the attention reads. */
+int pf_qk_norm_rotate_fwd(const pf_qk_norm_desc *d, const void *Q, const void *K,
+                          const void *gamma_q /* nullable */,
+                          const void *gamma_k /* nullable */,
+                          const void *positions /* nullable */, void *Qo, void *Ko,
+                          void *stream);
+
+/* From dQo = dL/dQo, dKo = dL/dKo and the forward call's inputs: dQ, dK, and
+ * dgamma_q, dgamma_k (float[head_dim], each nullable; overwritten or
+ * accumulated; untouched with PF_NORM_NONE).  The same call gives the same
+ * bits each time.  With PF_NORM_NONE Q and K are not read (nullable). */
+size_t pf_qk_norm_rotate_bwd_workspace_bytes(const pf_qk_norm_desc *d);
+int pf_qk_norm_rotate_bwd(const pf_qk_norm_desc *d, const void *Q, const void *K,
+                          const void *gamma_q, const void *gamma_k,
+                          const void *positions, const void *dQo, const void *dKo,
+                          void *dQ, void *dK, void *dgamma_q, void *dgamma_k,
+                          int accumulate, void *workspace, size_t workspace_bytes,
+                          void *stream);
+
+/* ------------------------------------------------------------------ */
+/* Attention with a learned relative position bias by buckets.          */
+/*   Q[B, Lq, heads_q, head_dim], K, V[B, Lk, heads_kv, head_dim];       */
+/*   heads_q is a multiple of heads_kv, query head h reads key head      */
+/*   h / (heads_q / heads_kv).  Query i of sequence b stands at position */
+/*   p = q_start[b] + i, key j at position j.                            */
+/*   S = scale q . k_j + table[bucket(j - p), h]                         */
+/*   A query sees the keys j < kv_len[b], with `causal` those of them    */
+/*   with j <= p.  O = softmax(S) V over what it sees,                   */
+/*   lse[B, heads_q, Lq] (float, nullable) = log sum exp S.              */
+/*   A query that sees nothing, and a query i >= q_len[b], has O = 0 and */
+/*   lse = -infinity and takes no part in any gradient; what K and V hold */
+/*   from kv_len[b] on, and Q and dO from q_len[b] on, does not matter   */
+/*   (not even NaN).                                                     */
+/*   q_start, q_len, kv_len: int32[B] on the device, each nullable       */
+/*   (0, Lq, Lk); lengths are taken as within 0 .. Lq and 0 .. Lk,       */
+/*   q_start as within -2^30 .. 2^30.                                    */
+/* Buckets: table[buckets, heads_q] float; buckets == 0: no bias, table  */
+/* unused.  With `bidirectional` keys after the query use the upper half */
+/* of the buckets, else all of them bucket 0.  A side of nb buckets has  */
+/* e = nb / 2 for the distances 0 .. e - 1 and the others spaced          */
+/* logarithmically up to max_distance:                                   */
+/*   bucket(n) = min(nb - 1, e + floor((nb - e) log(n/e) / log(max_distance/e))) */
+/* for n >= e, with the borders where exact arithmetic has them.         */
+/* Limits (PF_ERR_UNSUPPORTED): head_dim a multiple of 8, 8 .. 128;       */
+/* buckets 0 or 2 .. 256, with bidirectional a multiple of 2 and >= 4;    */
+/* max_distance > e and <= 1024; Lq, Lk < 2^30; B heads_q < 2^31.         */
+/* Lq == 0 or Lk == 0 is legal.                                           */
+/* Sums are the same bits in every call of the same sizes.                */
+/* ------------------------------------------------------------------ */
+typedef struct {
+    int64_t B, Lq, Lk;
+    int heads_q, heads_kv, head_dim;
+    int causal;
+    int buckets, max_distance, bidirectional;
+    int dtype; /* pf_dtype */
+    float scale;
+    int64_t q_stride[3], k_stride[3], v_stride[3]; /* Q, K, V: sequence, token, head */
+} pf_attention_desc;
+
+size_t pf_attention_fwd_workspace_bytes(const pf_attention_desc *d);
+int pf_attention_fwd(const pf_attention_desc *d, const void *Q, const void *K,
+                     const void *V, const void *table /* nullable */,
+                     const void *q_start /* nullable */,
+                     const void *q_len /* nullable */,
+                     const void *kv_len /* nullable */, void *O,
+                     void *lse /* nullable */, void *workspace,
+                     size_t workspace_bytes, void *stream);
+
+/* O, lse: the forward call's.  dQ, dK, dV in dtype, dense [B, L, heads,
+ * head_dim] (gradients of a key head are summed over the query heads that
+ * read it); dtable[buckets, heads_q] float, nullable, overwritten or
+ * accumulated.  O and dO are dense. */
+size_t pf_attention_bwd_workspace_bytes(const pf_attention_desc *d);
+int pf_attention_bwd(const pf_attention_desc *d, const void *Q, const void *K,
+                     const void *V, const void *table, const void *q_start,
+                     const void *q_len, const void *kv_len, const void *O,
+                     const void *lse, const void *dO, void *dQ, void *dK, void *dV,
+                     void *dtable /* nullable */, int accumulate, void *workspace,
+                     size_t workspace_bytes, void *stream);
+
+/* ------------------------------------------------------------------ */
+/* One AdamW step over many tensors in one launch.  For each value:      */
+/*   g = grad_scale grad                                                 */
+/*   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2          */
+/*   p = p (1 - lr weight_decay)                                         */
+/*       - lr / (1 - beta1^t) m / (sqrt(v) / sqrt(1 - beta2^t) + eps)     */
+/* t = steps + 1; the call stores t in `steps` (device int64).  lr and   */
+/* grad_scale are device floats, so that a captured step follows a       */
+/* schedule.                                                             */
+/*   param, grad: float.  copy (nullable): the parameters rounded to     */
+/*   bfloat16, as the layers above read them.                            */
+/*   state_bits 32: m, v float.                                          */
+/*   state_bits 8: every 256 consecutive values of a tensor (the last     */
+/*   ones: fewer) share a scale; m holds e4m3 codes of m / m_scale, v     */
+/*   those of sqrt(v) / v_scale (the root halves the range that a code    */
+/*   has to span); m_scale, v_scale float[ceil(count / 256)] are powers   */
+/*   of two, the smallest (from 2^-126) that keep the codes within 448.   */
+/*   A root that is not zero is not held as zero.  The step itself uses   */
+/*   m and v before they are rounded.  Values that are not finite are     */
+/*   held as NaN and do not change the scale of the others.               */
+/* Alignment: 4 bytes everywhere (copy: 2 bytes): slices of flat buffers  */
+/* will do.  The tensors of a call must not overlap.                      */
+/*                                                                       */
+/* The addresses live in a plan: ask its size, let pf_adamw_plan_fill     */
+/* write it to HOST memory, copy it to the device once (256-byte aligned),*/
+/* and hand it to every step.  A plan holds a counter of the launch that  */
+/* runs: steps of one plan must not overlap.                              */
+/* ------------------------------------------------------------------ */
+typedef struct {
+    void *param;
+    const void *grad;
+    void *m, *v;
+    void *m_scale, *v_scale; /* state_bits 8 */
+    void *copy;              /* nullable */
+    int64_t count;
+    float weight_decay;
+} pf_adamw_tensor;
+
+typedef struct {
+    int64_t tensors;
+    int state_bits; /* 32 or 8 */
+    double beta1, beta2, eps;
+} pf_adamw_desc;
+
+size_t pf_adamw_plan_bytes(const pf_adamw_desc *d, const pf_adamw_tensor *tensors);
+int pf_adamw_plan_fill(const pf_adamw_desc *d, const pf_adamw_tensor *tensors,
+                       void *plan_host, size_t plan_bytes);
+int pf_adamw_step(const pf_adamw_desc *d, void *plan, size_t plan_bytes,
+                  const void *lr, const void *grad_scale /* nullable: 1 */,
+                  void *steps, void *stream);
+
+/* ------------------------------------------------------------------ */
 /* Truncated-SVD factor initialisation (Algorithm 1, the step before    */
 /* the factorized layers are trained): W[m x n] (fp32, row-major) ->    */
 /*   U[m x r] = Ut_r S_r^(1/2),  V[n x r] = Vt_r S_r^(1/2)  (fp32),     */

@@ -8,6 +8,7 @@ are marshalled natively (csrc/pf_binding.cpp), the rest through ctypes.  There i
 no CPU fallback: importing without the built library, or calling with CPU
 tensors, raises.
 """
+import bisect
 import ctypes
 import os
 
@@ -21,6 +22,10 @@ PF_F32, PF_BF16 = 0, 1
 PF_NCHW, PF_NHWC = 0, 1
 PF_ACT_NONE, PF_ACT_RELU = 0, 1
 _ACT = {None: 0, "none": 0, "relu": 1}
+PF_NORM_NONE, PF_NORM_RMS = 0, 1
+PF_ROT_HALVES, PF_ROT_PAIRS = 0, 1
+_NORM = {None: 0, "none": 0, "rms": 1}
+_ROT = {"halves": 0, "pairs": 1}
 
 
 class PfError(RuntimeError):
@@ -59,6 +64,33 @@ class pf_lstm_stack_desc(ctypes.Structure):
                 ("has_bias", ctypes.c_int)]
 
 
+class pf_qk_norm_desc(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int64), ("L", ctypes.c_int64), ("heads_q", ctypes.c_int), ("heads_k", ctypes.c_int),
+                ("head_dim", ctypes.c_int), ("rot_dim", ctypes.c_int), ("norm", ctypes.c_int), ("rotation", ctypes.c_int),
+                ("dtype", ctypes.c_int), ("eps", ctypes.c_float), ("theta", ctypes.c_double),
+                ("q_stride", ctypes.c_int64 * 3), ("k_stride", ctypes.c_int64 * 3), ("qo_stride", ctypes.c_int64 * 3),
+                ("ko_stride", ctypes.c_int64 * 3), ("dq_stride", ctypes.c_int64 * 3), ("dk_stride", ctypes.c_int64 * 3)]
+
+
+class pf_attention_desc(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int64), ("Lq", ctypes.c_int64), ("Lk", ctypes.c_int64), ("heads_q", ctypes.c_int),
+                ("heads_kv", ctypes.c_int), ("head_dim", ctypes.c_int), ("causal", ctypes.c_int), ("buckets", ctypes.c_int),
+                ("max_distance", ctypes.c_int), ("bidirectional", ctypes.c_int), ("dtype", ctypes.c_int),
+                ("scale", ctypes.c_float), ("q_stride", ctypes.c_int64 * 3), ("k_stride", ctypes.c_int64 * 3),
+                ("v_stride", ctypes.c_int64 * 3)]
+
+
+class pf_adamw_tensor(ctypes.Structure):
+    _fields_ = [("param", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("m", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p), ("copy", ctypes.c_void_p),
+                ("count", ctypes.c_int64), ("weight_decay", ctypes.c_float)]
+
+
+class pf_adamw_desc(ctypes.Structure):
+    _fields_ = [("tensors", ctypes.c_int64), ("state_bits", ctypes.c_int), ("beta1", ctypes.c_double),
+                ("beta2", ctypes.c_double), ("eps", ctypes.c_double)]
+
+
 class pf_svd_desc(ctypes.Structure):
     _fields_ = [("m", ctypes.c_int64), ("n", ctypes.c_int64), ("r", ctypes.c_int64)]
 
@@ -79,6 +111,9 @@ EXPORTS = [
     "pf_lowrank_lstm_seq_fwd", "pf_lowrank_lstm_seq_bwd",
     "pf_lowrank_lstm_stack_fwd_workspace_bytes", "pf_lowrank_lstm_stack_bwd_workspace_bytes",
     "pf_lowrank_lstm_stack_fwd", "pf_lowrank_lstm_stack_bwd",
+    "pf_qk_norm_rotate_fwd", "pf_qk_norm_rotate_bwd_workspace_bytes", "pf_qk_norm_rotate_bwd",
+    "pf_attention_fwd_workspace_bytes", "pf_attention_fwd", "pf_attention_bwd_workspace_bytes", "pf_attention_bwd",
+    "pf_adamw_plan_bytes", "pf_adamw_plan_fill", "pf_adamw_step",
     "pf_svd_split_workspace_bytes", "pf_svd_split",
     "pf_dense_linear_workspace_bytes", "pf_dense_linear_fwd", "pf_dense_linear_bwd",
     "pf_dense_conv_workspace_bytes", "pf_dense_conv_fwd", "pf_dense_conv_bwd",
@@ -361,6 +396,46 @@ def pf_lowrank_lstm_stack_bwd(x, h0, c0, h_all, c_all, gates_all, Tx_all, Th_all
                              need_dx, grads)
 
 
+# ------------------------------------------------- between a Transformer layer's projections
+
+def pf_qk_norm_rotate_fwd(Q, K, gamma_q=None, gamma_k=None, positions=None, norm="rms", eps=1e-6, rot_dim=None,
+                          theta=10000.0, style="halves", out=None):
+    """Norms of queries Q[B, L, heads_q, D] and keys K[B, L, heads_k, D] (or None) for each head ("rms" with weights
+    gamma float32 [D], or "none"), then the first rot_dim values (None: all) turned by their token's position: int32
+    [B, L], None: 0 .. L - 1.  `style` pairs value i with i + rot_dim / 2 ("halves") or 2 i with 2 i + 1 ("pairs").
+    Q, K and out = (Qo, Ko) may have strides (slices of one buffer, of a cache) as long as a head's values are adjacent
+    and every head starts 16-byte aligned.  Returns (Qo, Ko)."""
+    return _native.qk_fwd(Q, K, gamma_q, gamma_k, positions, _NORM[norm], eps, rot_dim, theta, _ROT[style], out)
+
+
+def pf_qk_norm_rotate_bwd(Q, K, dQo, dKo, gamma_q=None, gamma_k=None, positions=None, norm="rms", eps=1e-6, rot_dim=None,
+                          theta=10000.0, style="halves", grads=None, out=None):
+    """From the gradients of pf_qk_norm_rotate_fwd's outputs: (dQ, dK, dgamma_q, dgamma_k), the latter float32 [D] (None
+    without that gamma), accumulated into `grads` = (dgamma_q, dgamma_k) when given.  out = (dQ, dK): where to write them."""
+    return _native.qk_bwd(Q, K, dQo, dKo, gamma_q, gamma_k, positions, _NORM[norm], eps, rot_dim, theta, _ROT[style], grads,
+                          out)
+
+
+def pf_attention_fwd(Q, K, V, table=None, causal=False, scale=None, max_distance=128, bidirectional=True, q_start=None,
+                     q_len=None, kv_len=None, save_lse=True):
+    """softmax(scale Q K^T + bias) V with a learned bias table[buckets, heads_q] (float32, None: no bias) by the bucket of
+    the distance key - query.  Q[B, Lq, heads_q, D], K, V[B, Lk, heads_kv, D], heads_q a multiple of heads_kv; scale None:
+    1 / sqrt(D).  q_start, q_len, kv_len: int32 [B] on the device: the position of each sequence's first query (None: 0)
+    and how many queries and keys it has (None: all).  A padded batch gives its lengths; a decoding step gives the
+    cache as K, V with kv_len = tokens in it and q_start = kv_len - Lq.  Q, K, V may have strides.  Returns
+    (O[B, Lq, heads_q, D], lse[B, heads_q, Lq] float32, kept for backward); O is 0 and lse -inf where nothing is seen."""
+    return _native.attn_fwd(Q, K, V, table, causal, scale, max_distance, bidirectional, q_start, q_len, kv_len, save_lse)
+
+
+def pf_attention_bwd(Q, K, V, O, lse, dO, table=None, causal=False, scale=None, max_distance=128, bidirectional=True,
+                     q_start=None, q_len=None, kv_len=None, need_dtable=True, grads=None, out=None):
+    """(dQ, dK, dV, dtable) from pf_attention_fwd's inputs and outputs and dO = dL/dO.  dtable[buckets, heads_q] is
+    float32 (None without a table or with need_dtable=False), accumulated into `grads` when given; out = (dQ, dK, dV):
+    dense tensors to write them to, e.g. slices of the dY[3, M, out] of pf_lowrank_linear_shared_bwd."""
+    return _native.attn_bwd(Q, K, V, table, causal, scale, max_distance, bidirectional, q_start, q_len, kv_len, O, lse, dO,
+                            need_dtable, grads, out)
+
+
 def pf_svd_split(W, r, return_info=False):
     """Algorithm 1's factor initialisation: W[m, n] float32 -> (U[m, r], V[n, r], sigma[min(m, n)]) with
     U V^T the best rank-r approximation of W and the singular values split evenly between the factors.
@@ -412,6 +487,104 @@ class GradBuffer:
     def zero(self):
         self.flat.zero_()
         return self
+
+
+class AdamW:
+    """AdamW over many tensors, one launch per step.  params, grads: lists of float32 tensors on one device (e.g. a
+    model's factors and their slices in a GradBuffer); copies: None or a list of bfloat16 tensors (entries may be None)
+    that receive the rounded parameters, as the bf16 layers read them.  weight_decay: one number or one per tensor.
+
+    state_bits 32: m, v are float32.  8: m[i] holds float8_e4m3fn codes of the first moment in units of m_scale[i][k]
+    for values 256 k .. 256 k + 255, v[i] codes of the ROOT of the second moment in units of v_scale[i][k].
+    `state` = dict(m, v[, m_scale, v_scale]) hands over lists of existing tensors (a checkpoint's), else they begin as
+    zeros.  `steps` (int64, one element, device) counts the steps done, `lr` (float32 [1], device) is read by each step:
+    `opt.lr.fill_(x)` changes it, also between replays of a captured step.
+
+    The addresses are noted once: the tensors are updated in place and must not be replaced.  Steps of one AdamW follow
+    one another: do not let two streams run them at once."""
+
+    def __init__(self, params, grads, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, copies=None, state_bits=32,
+                 state=None, steps=None):
+        params, grads = list(params), list(grads)
+        n = len(params)
+        if state_bits not in (32, 8):
+            raise PfError("state_bits must be 32 or 8")
+        if not params:
+            raise ValueError("no parameters")
+        if not (0 <= betas[0] < 1 and 0 <= betas[1] < 1 and eps >= 0):
+            raise ValueError("betas must lie in [0, 1) and eps must not be negative")
+        copies = [None] * n if copies is None else list(copies)
+        decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * n
+        if not len(grads) == len(copies) == len(decay) == n:
+            raise ValueError("params, grads, copies and weight_decay must have the same length")
+        self.device = dev = params[0].device
+        blocks = [-(-p.numel() // 256) for p in params]
+        code = torch.float32 if state_bits == 32 else torch.float8_e4m3fn
+        if state is None:
+            # codes of each tensor start 4-byte aligned: whole blocks for each
+            flat = lambda: torch.zeros((256 * sum(blocks),), dtype=torch.uint8, device=dev).view(code) if state_bits == 8 \
+                else torch.zeros((256 * sum(blocks),), dtype=code, device=dev)  # noqa: E731
+            cut = lambda f: [b[:p.numel()].view(p.shape) for b, p in zip(f.split([256 * k for k in blocks]), params)]  # noqa: E731
+            state = dict(m=cut(flat()), v=cut(flat()))
+            if state_bits == 8:
+                for k in ("m_scale", "v_scale"):
+                    state[k] = list(torch.full((sum(blocks),), 2.0 ** -126, device=dev).split(blocks))
+        self.m, self.v = list(state["m"]), list(state["v"])
+        self.m_scale = list(state["m_scale"]) if state_bits == 8 else None
+        self.v_scale = list(state["v_scale"]) if state_bits == 8 else None
+        self.params, self.grads, self.copies, self.state_bits = params, grads, copies, state_bits
+        self.betas, self.eps = (float(betas[0]), float(betas[1])), float(eps)
+        self.steps = torch.zeros((), dtype=torch.int64, device=dev) if steps is None else steps
+        self.lr = torch.full((1,), float(lr), dtype=torch.float32, device=dev)
+        lists = [params, grads, self.m, self.v] + ([self.m_scale, self.v_scale] if state_bits == 8 else [])
+        if any(len(x) != n for x in lists):
+            raise ValueError("every list must have one tensor per parameter")
+        f32 = torch.float32
+        written, read = [], []  # address ranges
+        for i, p in enumerate(params):
+            block = (blocks[i],)
+            mine = [(written, p, f32, p.shape), (read, grads[i], f32, p.shape), (written, self.m[i], code, p.shape),
+                    (written, self.v[i], code, p.shape)]
+            if copies[i] is not None:
+                mine.append((written, copies[i], torch.bfloat16, p.shape))
+            if state_bits == 8:
+                mine += [(written, self.m_scale[i], f32, block), (written, self.v_scale[i], f32, block)]
+            for where, t, dt, shape in mine:
+                _ptr(t, dt, allow_none=False)
+                if t.device != dev:
+                    raise PfError("tensors must be on one device")
+                if tuple(t.shape) != tuple(shape):
+                    raise ValueError(f"tensor {i}: shape {tuple(t.shape)}, expected {tuple(shape)}")
+                if t.numel():
+                    where.append((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size(), i))
+        written.sort()
+        for (_, end, i), (start, _, j) in zip(written, written[1:]):
+            if start < end:
+                raise PfError(f"tensors {i} and {j} overlap: a step updates every tensor once")
+        for start, end, i in read:
+            k = bisect.bisect_left(written, (end,)) - 1  # the last one that begins before this one's end
+            if k >= 0 and written[k][1] > start:
+                raise PfError(f"the gradient of tensor {i} overlaps a tensor that the step updates")
+        if self.steps.dtype != torch.int64 or self.steps.numel() != 1 or self.steps.device != dev:
+            raise PfError("steps must be one int64 on the parameters' device")
+        d = pf_adamw_desc(n, state_bits, self.betas[0], self.betas[1], self.eps)
+        rec = (pf_adamw_tensor * n)()
+        addr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+        for i, p in enumerate(params):
+            rec[i] = pf_adamw_tensor(addr(p), addr(grads[i]), addr(self.m[i]), addr(self.v[i]),
+                                     addr(self.m_scale[i]) if state_bits == 8 else None,
+                                     addr(self.v_scale[i]) if state_bits == 8 else None, addr(copies[i]), p.numel(), float(decay[i]))
+        size = lib.pf_adamw_plan_bytes(ctypes.byref(d), rec)
+        host = torch.zeros((max(size, 1),), dtype=torch.uint8)
+        _check(lib.pf_adamw_plan_fill(ctypes.byref(d), rec, ctypes.c_void_p(host.data_ptr()), ctypes.c_size_t(size)),
+               "pf_adamw_plan_fill")
+        self.plan = host[:size].to(dev)
+        self._args = (n, state_bits, self.betas[0], self.betas[1], self.eps, self.plan, self.lr)
+
+    def step(self, grad_scale=None):
+        """One step with the gradients that `grads` hold now, times grad_scale (None or a float32 device tensor of one
+        element, e.g. what clips their norm).  Runs on torch's current stream of the tensors' device."""
+        _native.adamw_step(*self._args, grad_scale, self.steps)
 
 
 def timing_enable(on=True):

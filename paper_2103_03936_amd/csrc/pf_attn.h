@@ -1,0 +1,217 @@
+// What the attention kernels share: arguments, matrix operands, tiles in LDS, the bias by distance.
+//
+// Orientation.  A product of 32 x 32 leaves lane l with column l % 32 and the rows 8 (i / 4) + 4 (l / 32) + i % 4,
+// i = 0 .. 15, of the result.  Forward and for dQ the scores are formed transposed (rows: keys, columns: queries), so that
+// a lane has one query: its maximum, sum, position and masks are scalars of the lane, and a row statistic needs one exchange
+// between the two halves of the wave.  What a lane holds of P is then, without any exchange, the right operand of the next
+// product, O^T = V^T P^T, if that product takes its contraction index in the same order, 16 keys at a time:
+// {4 h .. 4 h + 3, 8 + 4 h .. 8 + 4 h + 3} in the half h.  The left operand, V^T, is read from LDS in that order (for bf16
+// with the transposing reads).  For dK and dV the scores are formed with rows: queries, columns: keys, and the same holds.
+#pragma once
+
+#include "pf_attn_bias.h"
+#include "pf_common.h"
+
+namespace pf {
+
+struct AttnArgs {
+    const void *Q, *K, *V, *dO, *Oin;
+    void *O, *dQ, *dK, *dV;
+    const float *table, *lse_in;
+    float *lse, *delta, *tab; // delta[B, Hq, Lq]; tab[Hq][B * tiles][buckets]: sums of dS per workgroup
+    const int *q_start, *q_len, *kv_len;
+    int B, Lq, Lk, Hq, Hkv, G, D, causal, buckets, two_sided, tiles;
+    float scale;
+    i64 qs[3], ks[3], vs[3]; // strides: sequence, token, head
+    // few queries: the split of the keys and where its parts go (partial O, then maxima and sums)
+    int splits, rows;
+    float *part_o, *part_ml;
+    AttnBuckets bk;
+};
+
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+
+// ------------------------------------------------------------------ matrix operands
+template <typename T>
+struct Frag;
+template <>
+struct Frag<bf16_t> {
+    bf16x8_t v;
+};
+template <>
+struct Frag<float> {
+    float v[8];
+};
+
+__device__ __forceinline__ void mma(f32x16_t &c, const Frag<bf16_t> &a, const Frag<bf16_t> &b)
+{
+    c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, b.v, c, 0, 0, 0);
+}
+__device__ __forceinline__ void mma(f32x16_t &c, const Frag<float> &a, const Frag<float> &b)
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[j], b.v[j], c, 0, 0, 0);
+}
+
+// Operand with the index along the rows and the contraction along 16 columns from `p` on, p in the lane's row; h = lane / 32.
+// (The halves share the 16 columns in an order of their own, the same for both operands.)
+__device__ __forceinline__ Frag<bf16_t> row_frag(const bf16_t *p, int h)
+{
+    Frag<bf16_t> f;
+    f.v = *(const bf16x8_t *)(p + 8 * h);
+    return f;
+}
+__device__ __forceinline__ Frag<float> row_frag(const float *p, int h)
+{
+    Frag<float> f;
+    const float4 a = *(const float4 *)(p + 4 * h), b = *(const float4 *)(p + 8 + 4 * h);
+    f.v[0] = a.x, f.v[1] = a.y, f.v[2] = a.z, f.v[3] = a.w, f.v[4] = b.x, f.v[5] = b.y, f.v[6] = b.z, f.v[7] = b.w;
+    return f;
+}
+// The same from global memory, zeros where the row does not exist (ok) or has no such column (head_dim is a multiple of 8)
+__device__ __forceinline__ Frag<bf16_t> row_frag_global(const bf16_t *row, int col, int D, int h, bool ok)
+{
+    Frag<bf16_t> f;
+    f.v = bf16x8_t{};
+    if (ok && col + 8 * h < D) f.v = *(const bf16x8_t *)(row + col + 8 * h);
+    return f;
+}
+__device__ __forceinline__ Frag<float> row_frag_global(const float *row, int col, int D, int h, bool ok)
+{
+    Frag<float> f;
+    float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
+    if (ok && col + 4 * h < D) a = *(const float4 *)(row + col + 4 * h);
+    if (ok && col + 8 + 4 * h < D) b = *(const float4 *)(row + col + 8 + 4 * h);
+    f.v[0] = a.x, f.v[1] = a.y, f.v[2] = a.z, f.v[3] = a.w, f.v[4] = b.x, f.v[5] = b.y, f.v[6] = b.z, f.v[7] = b.w;
+    return f;
+}
+
+// Operand with the index along the columns c0 .. c0 + 31 of a row-major LDS tile and the contraction along its rows
+// r0 .. r0 + 15, in the order in which a product's result lies in the lanes (above)
+__device__ __forceinline__ Frag<bf16_t> col_frag(const bf16_t *tile, int pitch, int r0, int c0, int lane)
+{
+    typedef __attribute__((address_space(3))) bf16x4_t *lds_ptr;
+    const int g = lane >> 4, i = lane & 15;
+    const bf16_t *p = tile + (r0 + 4 * (g >> 1) + (i >> 2)) * pitch + c0 + 16 * (g & 1) + 4 * (i & 3);
+    const bf16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_ptr)p);
+    const bf16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_ptr)(p + 8 * pitch));
+    Frag<bf16_t> f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f.v[e] = lo[e], f.v[4 + e] = hi[e];
+    return f;
+}
+__device__ __forceinline__ Frag<float> col_frag(const float *tile, int pitch, int r0, int c0, int lane)
+{
+    const float *p = tile + (r0 + 4 * (lane >> 5)) * pitch + c0 + (lane & 31);
+    Frag<float> f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f.v[e] = p[e * pitch], f.v[4 + e] = p[(8 + e) * pitch];
+    return f;
+}
+
+// Eight values of a result (its registers 8 c .. 8 c + 7) as the operand for rows 16 c .. 16 c + 15; bf16: rounded to
+// nearest even, the one rounding of P and dS, half a step of 2^-8 each
+__device__ __forceinline__ void pack(const float (&x)[16], int c, Frag<bf16_t> &f)
+{
+    union {
+        uint32_t u[4];
+        bf16x8_t v;
+    } w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w.u[i] = pack_bf16x2(x[8 * c + 2 * i], x[8 * c + 2 * i + 1]);
+    f.v = w.v;
+}
+__device__ __forceinline__ void pack(const float (&x)[16], int c, Frag<float> &f)
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f.v[i] = x[8 * c + i];
+}
+
+// Four adjacent values
+__device__ __forceinline__ void put4(float *p, float a, float b, float c, float d) { *(float4 *)p = make_float4(a, b, c, d); }
+__device__ __forceinline__ void put4(bf16_t *p, float a, float b, float c, float d)
+{
+    *(uint2 *)p = make_uint2(pack_bf16x2(a, b), pack_bf16x2(c, d));
+}
+
+// ------------------------------------------------------------------ tiles
+// ROWS rows of DP columns in LDS, 16 bytes of padding to a row; a workgroup of THREADS loads one through registers
+template <typename T, int DP, int ROWS, int THREADS>
+struct Tile {
+    static constexpr int VEC = 16 / sizeof(T), PITCH = DP + VEC, PIECES = ROWS * DP / VEC, N = (PIECES + THREADS - 1) / THREADS;
+    static constexpr int BYTES = ROWS * PITCH * (int)sizeof(T);
+    uint4 r[N];
+    // rows r0 .. r0 + ROWS - 1 of `src` (elements `stride` apart), zeros from row `rows` and column D on
+    __device__ __forceinline__ void load(const T *src, i64 stride, int r0, int rows, int D, int t)
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int p = t + i * THREADS, row = p / (DP / VEC), col = p % (DP / VEC) * VEC;
+            r[i] = make_uint4(0u, 0u, 0u, 0u);
+            if ((PIECES % THREADS == 0 || p < PIECES) && r0 + row < rows && col < D) r[i] = *(const uint4 *)(src + (r0 + row) * stride + col);
+        }
+    }
+    __device__ __forceinline__ void store(T *lds, int t) const
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int p = t + i * THREADS, row = p / (DP / VEC), col = p % (DP / VEC) * VEC;
+            if (PIECES % THREADS == 0 || p < PIECES) *(uint4 *)(lds + row * PITCH + col) = r[i];
+        }
+    }
+};
+
+// ------------------------------------------------------------------ lengths and positions
+__device__ __forceinline__ int clamped(int x, int lo, int hi) { return x < lo ? lo : x > hi ? hi : x; }
+struct AttnLens {
+    int nq, nk, start;
+    __device__ __forceinline__ AttnLens(const AttnArgs &a, int b)
+    {
+        nq = a.q_len ? clamped(a.q_len[b], 0, a.Lq) : a.Lq;
+        nk = a.kv_len ? clamped(a.kv_len[b], 0, a.Lk) : a.Lk;
+        start = a.q_start ? clamped(a.q_start[b], -(1 << 30), 1 << 30) : 0;
+    }
+};
+
+// Bucket of the distance key - query
+__device__ __forceinline__ int bucket_of(const AttnArgs &a, int dist)
+{
+    if (dist > 0 && !a.two_sided) return 0;
+    const int n = dist < 0 ? -dist : dist;
+    int u = n;
+    if (n >= a.bk.exact) {
+        u = a.bk.exact;
+        for (int k = 0; k < a.bk.borders; ++k) u += n >= a.bk.border[k];
+    }
+    return u + (dist > 0 ? a.bk.side : 0);
+}
+// The bias of query head `head` in a bucket, times log2(e); finite values stay finite (a table may hold the type's lowest)
+__device__ __forceinline__ float bias_of(const AttnArgs &a, int bucket, int head)
+{
+    const float x = a.table[(i64)bucket * a.Hq + head], y = x * LOG2E;
+    return __builtin_isinf(y) && !__builtin_isinf(x) ? __builtin_copysignf(3.4028234e38f, x) : y;
+}
+// bias[far + d], d = -far .. far: the head's bias at distance d (further ones have that of +-far), times log2(e)
+__device__ __forceinline__ void fill_bias(const AttnArgs &a, float *bias, int head, int t, int threads)
+{
+    for (int i = t; i <= 2 * a.bk.far; i += threads) bias[i] = bias_of(a, bucket_of(a, i - a.bk.far), head);
+}
+
+// XCDs take workgroups in turn: consecutive pieces of work (the tiles of a head, which share keys and values) go to one XCD
+// and its L2.  A bijection for any number of workgroups.
+__device__ __forceinline__ unsigned xcd_order(unsigned id, unsigned n)
+{
+    const unsigned x = id & 7, per = n >> 3, more = n & 7;
+    return x * per + (x < more ? x : more) + (id >> 3);
+}
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); } // (one instruction, 1 ulp)
+
+// ------------------------------------------------------------------ host
+int attn_split_fwd(const pf_attention_desc *d, AttnArgs &a, void *workspace, hipStream_t s); // few queries (pf_attn_split.hip)
+int attn_split_count(const pf_attention_desc *d); // 0: the ordinary kernel
+size_t attn_split_bytes(const pf_attention_desc *d);
+int attn_check(const pf_attention_desc *d);
+void attn_fill(const pf_attention_desc *d, AttnArgs &a);
+
+} // namespace pf

@@ -1,0 +1,248 @@
+// Attention with a relative position bias by buckets, forward: pf_attention_fwd.
+//
+// A workgroup has 128 queries of one head, a wave 32 of them in its columns (pf_attn.h); keys and values pass through LDS
+// in tiles, the next one loaded into registers while this one is used.  One pass over the keys with the running maximum and
+// sum of each query; the score matrix, the bias and P exist in registers only.
+#include "pf_attn.h"
+
+namespace pf {
+
+template <typename T>
+constexpr int KEYS = sizeof(T) == 2 ? 64 : 32; // keys of a tile
+
+template <typename T, int DP, bool BIAS>
+__global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a)
+{
+    constexpr int KT = KEYS<T>, SUB = KT / 32;
+    using Tl = Tile<T, DP, KT, 256>;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    T *const kt = (T *)lds, *const vt = (T *)(lds + Tl::BYTES);
+    float *const bias = (float *)(lds + 2 * Tl::BYTES);
+
+    const unsigned w = xcd_order(blockIdx.x, gridDim.x);
+    const int tile = a.tiles - 1 - (int)(w % a.tiles), bh = w / a.tiles, b = bh / a.Hq, head = bh - b * a.Hq;
+    const int t = threadIdx.x, wave = t >> 6, lane = t & 63, col = lane & 31, h = lane >> 5;
+    const AttnLens n(a, b);
+    const int i0 = tile * 128 + wave * 32, i = i0 + col; // the lane's query
+    const bool ok = i < n.nq;
+
+    const T *const Kp = (const T *)a.K + b * a.ks[0] + head / a.G * a.ks[2], *const Vp = (const T *)a.V + b * a.vs[0] + head / a.G * a.vs[2];
+    // keys that some query of the workgroup sees
+    int keys = n.nk;
+    if (tile * 128 >= n.nq) keys = 0;
+    const int block_last = (tile * 128 + 128 < n.nq ? tile * 128 + 128 : n.nq) - 1 + n.start; // positions
+    if (a.causal && block_last + 1 < keys) keys = block_last + 1 < 0 ? 0 : block_last + 1;
+    const int last = (i0 + 32 < n.nq ? i0 + 32 : n.nq) - 1, pmin = i0 + n.start, pmax = last + n.start, pos = i + n.start;
+    const bool idle = i0 >= n.nq;
+
+    if (BIAS && keys > 0) fill_bias(a, bias, head, t, 256);
+    Frag<T> q[DP / 16];
+    {
+        const T *const Qp = (const T *)a.Q + b * a.qs[0] + head * a.qs[2] + i * a.qs[1];
+#pragma unroll
+        for (int c = 0; c < DP / 16; ++c) q[c] = row_frag_global(Qp, 16 * c, a.D, h, ok);
+    }
+    const float sl2 = a.scale * LOG2E;
+    const int far = a.bk.far;
+    f32x16_t o[DP / 32];
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d) o[d] = f32x16_t{};
+    float m = -INFINITY, sum = 0.f; // the running maximum (base 2); the sum of the lane's keys
+
+    Tl kr, vr;
+    if (keys > 0) {
+        kr.load(Kp, a.ks[1], 0, n.nk, a.D, t);
+        vr.load(Vp, a.vs[1], 0, n.nk, a.D, t);
+    }
+    for (int k0 = 0; k0 < keys; k0 += KT) {
+        __syncthreads();
+        kr.store(kt, t);
+        vr.store(vt, t);
+        if (k0 + KT < keys) {
+            kr.load(Kp, a.ks[1], k0 + KT, n.nk, a.D, t);
+            vr.load(Vp, a.vs[1], k0 + KT, n.nk, a.D, t);
+        }
+        __syncthreads();
+        if (idle || (a.causal && k0 > pmax)) continue;
+        float s[SUB][16];
+        float top = -INFINITY;
+        const bool edge = k0 + KT > n.nk || (a.causal && k0 + KT - 1 > pmin);
+        const bool near = BIAS && k0 + KT - 1 - pmin > -far && k0 - pmax < far;
+        const float flat = BIAS ? bias[k0 >= pmin ? 2 * far : 0] : 0.f; // where no key is near
+#pragma unroll
+        for (int u = 0; u < SUB; ++u) {
+            f32x16_t acc = {};
+            const T *const row = kt + (32 * u + col) * Tl::PITCH;
+#pragma unroll
+            for (int c = 0; c < DP / 16; ++c) mma(acc, row_frag(row + 16 * c, h), q[c]);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int j = k0 + 32 * u + 8 * (e >> 2) + 4 * h + (e & 3);
+                float x = acc[e] * sl2 + flat;
+                if (near) x = acc[e] * sl2 + bias[clamped(j - pos, -far, far) + far];
+                if (edge && (j >= n.nk || (a.causal && j > pos))) x = -INFINITY;
+                s[u][e] = x;
+                top = fmaxf(top, x);
+            }
+        }
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float m_new = fmaxf(m, top), base = m_new == -INFINITY ? 0.f : m_new;
+        if (__any(m_new > m)) {
+            const float f = exp2_fast(m - base);
+            sum *= f;
+#pragma unroll
+            for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[d][e] *= f;
+            m = m_new;
+        }
+#pragma unroll
+        for (int u = 0; u < SUB; ++u) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                s[u][e] = exp2_fast(s[u][e] - base);
+                sum += s[u][e];
+            }
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                Frag<T> p;
+                pack(s[u], c, p);
+#pragma unroll
+                for (int d = 0; d < DP / 32; ++d) mma(o[d], col_frag(vt, Tl::PITCH, 32 * u + 16 * c, 32 * d, lane), p);
+            }
+        }
+    }
+    sum += __shfl_xor(sum, 32);
+    if (i >= a.Lq) return;
+    const bool some = ok && sum > 0.f;
+    const float inv = some ? 1.f / sum : 0.f;
+    T *const Op = (T *)a.O + (((i64)b * a.Lq + i) * a.Hq + head) * a.D;
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) {
+            const int c = 32 * d + 8 * (e >> 2) + 4 * h;
+            float v[4];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) v[x] = some ? o[d][e + x] * inv : 0.f;
+            if (c < a.D) put4(Op + c, v[0], v[1], v[2], v[3]);
+        }
+    if (a.lse && h == 0) a.lse[((i64)b * a.Hq + head) * a.Lq + i] = some ? (m + __builtin_amdgcn_logf(sum)) * LN2 : -INFINITY;
+}
+
+// ------------------------------------------------------------------ host
+static bool strides_ok(const int64_t *s, int unit)
+{
+    for (int i = 0; i < 3; ++i)
+        if (s[i] < 0 || s[i] % unit) return false;
+    return true;
+}
+static void strides_of(const int64_t *s, i64 L, int heads, int D, i64 (&out)[3])
+{
+    const bool dense = !s[0] && !s[1] && !s[2];
+    out[2] = dense ? D : s[2];
+    out[1] = dense ? (i64)heads * D : s[1];
+    out[0] = dense ? L * heads * D : s[0];
+}
+
+int attn_check(const pf_attention_desc *d)
+{
+    if (!d) return PF_ERR_NULL;
+    if (d->B < 0 || d->Lq < 0 || d->Lk < 0 || d->heads_q <= 0 || d->heads_kv <= 0 || d->head_dim <= 0) return PF_ERR_SHAPE;
+    if (d->heads_q % d->heads_kv) return PF_ERR_SHAPE;
+    if (d->dtype != PF_F32 && d->dtype != PF_BF16) return PF_ERR_UNSUPPORTED;
+    if (d->head_dim % 8 || d->head_dim > 128) return PF_ERR_UNSUPPORTED;
+    if (!isfinite(d->scale)) return PF_ERR_UNSUPPORTED;
+    if (d->Lq >= 1 << 30 || d->Lk >= 1 << 30 || d->B > INT32_MAX / d->heads_q) return PF_ERR_UNSUPPORTED;
+    // workgroups of 32 rows or keys at the least are counted in 32 bits
+    if (d->B * d->heads_q > INT32_MAX / ((d->Lq + 31) / 32 + 1) || d->B * d->heads_kv > INT32_MAX / ((d->Lk + 31) / 32 + 1)) return PF_ERR_UNSUPPORTED;
+    if (d->buckets) {
+        const int side = d->bidirectional ? d->buckets / 2 : d->buckets;
+        if (d->buckets < 0 || d->buckets > ATTN_MAX_BUCKETS || side < 2 || (d->bidirectional && d->buckets % 2)) return PF_ERR_UNSUPPORTED;
+        if (d->max_distance <= side / 2 || d->max_distance > ATTN_MAX_DISTANCE) return PF_ERR_UNSUPPORTED;
+    }
+    const int unit = 16 / (d->dtype == PF_BF16 ? 2 : 4);
+    if (!strides_ok(d->q_stride, unit) || !strides_ok(d->k_stride, unit) || !strides_ok(d->v_stride, unit)) return PF_ERR_UNSUPPORTED;
+    return PF_OK;
+}
+
+void attn_fill(const pf_attention_desc *d, AttnArgs &a)
+{
+    a.B = (int)d->B, a.Lq = (int)d->Lq, a.Lk = (int)d->Lk;
+    a.Hq = d->heads_q, a.Hkv = d->heads_kv, a.G = d->heads_q / d->heads_kv, a.D = d->head_dim;
+    a.causal = d->causal != 0;
+    a.buckets = d->buckets;
+    a.two_sided = d->bidirectional != 0;
+    a.scale = d->scale;
+    strides_of(d->q_stride, d->Lq, d->heads_q, d->head_dim, a.qs);
+    strides_of(d->k_stride, d->Lk, d->heads_kv, d->head_dim, a.ks);
+    strides_of(d->v_stride, d->Lk, d->heads_kv, d->head_dim, a.vs);
+    if (d->buckets) { // (a model has one bias: its borders are worked out once)
+        static thread_local struct {
+            int side, distance;
+            AttnBuckets b;
+        } known = {};
+        const int side = d->bidirectional ? d->buckets / 2 : d->buckets;
+        if (known.side != side || known.distance != d->max_distance) known = {side, d->max_distance, attn_buckets(side, d->max_distance)};
+        a.bk = known.b;
+    }
+}
+
+template <typename T, int DP>
+static int attn_fwd_launch(const AttnArgs &a, hipStream_t s)
+{
+    using Tl = Tile<T, DP, KEYS<T>, 256>;
+    const unsigned blocks = (unsigned)a.B * a.Hq * a.tiles;
+    const size_t lds = 2 * Tl::BYTES + (a.buckets ? (2 * a.bk.far + 1) * sizeof(float) : 0);
+    int st = PF_OK;
+    if (a.buckets)
+        PF_LAUNCH_LDS(st, "attn_fwd", (attn_fwd_kernel<T, DP, true>), dim3(blocks), dim3(256), lds, s, a);
+    else
+        PF_LAUNCH_LDS(st, "attn_fwd", (attn_fwd_kernel<T, DP, false>), dim3(blocks), dim3(256), lds, s, a);
+    return st;
+}
+
+} // namespace pf
+
+extern "C" {
+
+using namespace pf;
+
+size_t pf_attention_fwd_workspace_bytes(const pf_attention_desc *d)
+{
+    if (attn_check(d) != PF_OK || d->B == 0 || d->Lq == 0) return 0;
+    return attn_split_bytes(d);
+}
+
+int pf_attention_fwd(const pf_attention_desc *d, const void *Q, const void *K, const void *V, const void *table, const void *q_start,
+                     const void *q_len, const void *kv_len, void *O, void *lse, void *workspace, size_t workspace_bytes, void *stream)
+{
+    const int status = attn_check(d);
+    if (status != PF_OK) return status;
+    if (d->B == 0 || d->Lq == 0) return PF_OK;
+    if (!Q || !O || (d->Lk && (!K || !V)) || (d->buckets && !table)) return PF_ERR_NULL;
+    if (any_misaligned({Q, O, d->Lk ? K : nullptr, d->Lk ? V : nullptr}, 16) || any_misaligned({table, q_start, q_len, kv_len, lse}, 4) ||
+        any_misaligned({workspace}, 256))
+        return PF_ERR_UNSUPPORTED;
+    const size_t need = attn_split_bytes(d);
+    if (need && (!workspace || workspace_bytes < need)) return PF_ERR_WORKSPACE;
+    AttnArgs a = {};
+    attn_fill(d, a);
+    a.Q = Q, a.K = K, a.V = V, a.O = O;
+    a.table = (const float *)table;
+    a.lse = (float *)lse;
+    a.q_start = (const int *)q_start;
+    a.q_len = (const int *)q_len;
+    a.kv_len = (const int *)kv_len;
+    if (attn_split_count(d)) return attn_split_fwd(d, a, workspace, (hipStream_t)stream);
+    a.tiles = (a.Lq + 127) / 128;
+    const hipStream_t s = (hipStream_t)stream;
+    const int DP = (a.D + 31) / 32 * 32;
+    if (d->dtype == PF_BF16)
+        return DP == 32 ? attn_fwd_launch<bf16_t, 32>(a, s) : DP == 64 ? attn_fwd_launch<bf16_t, 64>(a, s)
+             : DP == 96 ? attn_fwd_launch<bf16_t, 96>(a, s) : attn_fwd_launch<bf16_t, 128>(a, s);
+    return DP == 32 ? attn_fwd_launch<float, 32>(a, s) : DP == 64 ? attn_fwd_launch<float, 64>(a, s)
+         : DP == 96 ? attn_fwd_launch<float, 96>(a, s) : attn_fwd_launch<float, 128>(a, s);
+}
+
+} // extern "C"

@@ -7,9 +7,12 @@
 
 #include <ATen/ATen.h>
 #include <ATen/hip/EmptyTensor.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
+#include <cmath>
 #include <initializer_list>
 #include <map>
 #include <mutex>
@@ -633,6 +636,314 @@ PyObject *stack_bwd(PyObject *const *a)
     return tuple({dx.give(), dh0.give(), dc0.give(), grads});
 }
 
+// ------------------------------------------------------------------ between the projections
+// These calls run on the device of their tensors, on torch's current stream there, whatever device is current, and take
+// their workspace from torch's allocator for the call: of two graphs captured on one stream each has memory of its own.
+hipStream_t stream_of(const at::Device &dev) { return c10::hip::getCurrentHIPStream(dev.index()).stream(); }
+
+template <class F>
+void call_here(const char *what, size_t bytes, const at::Device &dev, F f)
+{
+    const Out ws = bytes ? Out({(int64_t)bytes}, at::kByte, dev) : Out();
+    void *const s = (void *)stream_of(dev);
+    int status;
+    {
+        NoGil released;
+        status = f(ws.p, bytes, s);
+    }
+    check(status, what);
+}
+
+void same_device(const Tensor &t, const at::Device &dev)
+{
+    if (!t.is_cuda()) fail("tensors must live on the GPU; there is no CPU path");
+    if (t.device() != dev) fail("tensors must be on one device");
+}
+void shape_is(const Tensor &t, at::IntArrayRef want, const char *name)
+{
+    if (t.sizes() != want) {
+        std::string w = std::string(name) + " must have the shape (";
+        for (int64_t x : want) w += std::to_string(x) + ", ";
+        throw Fail{PyExc_ValueError, w + ")"};
+    }
+}
+// A dense tensor of a given shape and type, or none
+void *dense(PyObject *o, at::IntArrayRef want, at::ScalarType type, const at::Device &dev, const char *name)
+{
+    if (o == Py_None) return nullptr;
+    const Tensor &t = tensor(o);
+    same_device(t, dev);
+    shape_is(t, want, name);
+    return address(t, type);
+}
+// [B, L, heads, head_dim] with the values of a head adjacent: its address, and its strides (extents of one: 0, which
+// no element depends on)
+void *heads(const Tensor &t, at::IntArrayRef want, at::ScalarType type, const at::Device &dev, int64_t (&stride)[3], const char *name, bool written)
+{
+    same_device(t, dev);
+    shape_is(t, want, name);
+    if (t.scalar_type() != type) fail(std::string("expected ") + c10::toString(type) + ", got " + c10::toString(t.scalar_type()));
+    if (t.is_contiguous()) {
+        stride[0] = stride[1] = stride[2] = 0;
+        return t.data_ptr();
+    }
+    if (t.size(3) > 1 && t.stride(3) != 1) fail(std::string(name) + ": the values of a head must be adjacent");
+    for (int i = 0; i < 3; ++i) stride[i] = t.size(i) > 1 ? t.stride(i) : 0;
+    if (!stride[0] && !stride[1] && !stride[2]) fail(std::string(name) + ": one head cannot stand for all of them");
+    if (written) { // each dimension steps over what the smaller ones span
+        int order[3] = {0, 1, 2};
+        for (int i = 0; i < 2; ++i)
+            for (int j = 0; j < 2; ++j)
+                if (stride[order[j]] > stride[order[j + 1]]) std::swap(order[j], order[j + 1]);
+        int64_t span = t.size(3);
+        for (int i : order) {
+            if (t.size(i) <= 1) continue;
+            if (stride[i] < span) fail(std::string(name) + ": elements of an output meet");
+            span = stride[i] * (t.size(i) - 1) + span;
+        }
+    }
+    return t.data_ptr();
+}
+
+// The tensors of one call: Q (4 dimensions), K or none
+struct QkCall {
+    pf_qk_norm_desc d = {};
+    at::Device dev;
+    at::ScalarType dt;
+    int64_t sq[4], sk[4] = {0, 0, 0, 0};
+    // positions, norm, eps, rot_dim (or None), theta, style from a[0] on
+    void *positions;
+    QkCall(const Tensor &Q, PyObject *K, PyObject *const *a) : dev(Q.device()), dt(Q.scalar_type())
+    {
+        dims(Q, 4, "Q");
+        same_device(Q, dev);
+        for (int i = 0; i < 4; ++i) sq[i] = Q.size(i);
+        d.B = sq[0], d.L = sq[1], d.heads_q = (int)sq[2], d.head_dim = (int)sq[3];
+        if (K != Py_None) {
+            const Tensor &k = tensor(K);
+            dims(k, 4, "K");
+            sk[0] = sq[0], sk[1] = sq[1], sk[2] = k.size(2), sk[3] = sq[3];
+            d.heads_k = (int)sk[2];
+        }
+        d.dtype = dtype_code(Q);
+        d.norm = (int)integer(a[1]);
+        d.eps = (float)number(a[2]);
+        d.rot_dim = a[3] == Py_None ? d.head_dim : (int)integer(a[3]);
+        d.theta = number(a[4]);
+        d.rotation = (int)integer(a[5]);
+        positions = dense(a[0], {sq[0], sq[1]}, at::kInt, dev, "positions");
+    }
+    at::IntArrayRef qshape() const { return at::IntArrayRef(sq, 4); }
+    at::IntArrayRef kshape() const { return at::IntArrayRef(sk, 4); }
+    static double number(PyObject *o)
+    {
+        const double v = PyFloat_AsDouble(o);
+        if (v == -1.0 && PyErr_Occurred()) throw Fail{nullptr, ""};
+        return v;
+    }
+};
+
+// A pair of given tensors, or two new ones
+struct Pair {
+    Ref items;
+    PyObject *given[2] = {nullptr, nullptr};
+    Pair(PyObject *o, const char *what)
+    {
+        if (o == Py_None) return;
+        items.o = PySequence_Fast(o, what);
+        if (!items.o) throw Fail{nullptr, ""};
+        if (PySequence_Fast_GET_SIZE(items.o) != 2) throw Fail{PyExc_ValueError, what};
+        for (int i = 0; i < 2; ++i) given[i] = PySequence_Fast_GET_ITEM(items.o, i);
+    }
+};
+// Output i of a call: the given tensor's address and strides, or a new dense tensor
+void *output(const Pair &p, int i, Out &o, at::IntArrayRef shape, at::ScalarType dt, const at::Device &dev, int64_t (&stride)[3], const char *name)
+{
+    if (p.given[i] && p.given[i] != Py_None) return heads(tensor(p.given[i]), shape, dt, dev, stride, name, true);
+    o = Out(shape, dt, dev);
+    stride[0] = stride[1] = stride[2] = 0;
+    return o.p;
+}
+PyObject *give_output(const Pair &p, int i, Out &o) { return p.given[i] && p.given[i] != Py_None ? borrowed(p.given[i]) : o.give(); }
+
+// Q, K, gamma_q, gamma_k, positions, norm, eps, rot_dim, theta, rotation, out
+PyObject *qk_fwd(PyObject *const *a)
+{
+    const Tensor &Q = tensor(a[0]);
+    QkCall c(Q, a[1], a + 4);
+    const c10::DeviceGuard on(c.dev);
+    const bool keys = a[1] != Py_None;
+    void *const q = heads(Q, c.qshape(), c.dt, c.dev, c.d.q_stride, "Q", false);
+    void *const k = keys ? heads(tensor(a[1]), c.kshape(), c.dt, c.dev, c.d.k_stride, "K", false) : nullptr;
+    void *const gq = dense(a[2], {c.d.head_dim}, F32, c.dev, "gamma_q"), *const gk = dense(a[3], {c.d.head_dim}, F32, c.dev, "gamma_k");
+    Pair out(a[10], "out must hold the outputs for Q and K");
+    Out oq, ok;
+    void *const pq = output(out, 0, oq, c.qshape(), c.dt, c.dev, c.d.qo_stride, "out[0]");
+    void *const pk = keys ? output(out, 1, ok, c.kshape(), c.dt, c.dev, c.d.ko_stride, "out[1]") : nullptr;
+    call_here("pf_qk_norm_rotate_fwd", 0, c.dev, [&](void *, size_t, void *s) { return pf_qk_norm_rotate_fwd(&c.d, q, k, gq, gk, c.positions, pq, pk, s); });
+    return tuple({give_output(out, 0, oq), keys ? give_output(out, 1, ok) : borrowed(Py_None)});
+}
+
+// Q, K, dQo, dKo, gamma_q, gamma_k, positions, norm, eps, rot_dim, theta, rotation, grads, out
+PyObject *qk_bwd(PyObject *const *a)
+{
+    const Tensor &Q = tensor(a[0]);
+    QkCall c(Q, a[1], a + 6);
+    const c10::DeviceGuard on(c.dev);
+    const bool keys = a[1] != Py_None;
+    int64_t in_q[3], in_k[3] = {0, 0, 0};
+    void *const q = heads(Q, c.qshape(), c.dt, c.dev, in_q, "Q", false);
+    void *const k = keys ? heads(tensor(a[1]), c.kshape(), c.dt, c.dev, in_k, "K", false) : nullptr;
+    void *const gq = dense(a[4], {c.d.head_dim}, F32, c.dev, "gamma_q"), *const gk = dense(a[5], {c.d.head_dim}, F32, c.dev, "gamma_k");
+    void *const dqo = heads(tensor(a[2]), c.qshape(), c.dt, c.dev, c.d.qo_stride, "dQo", false);
+    void *const dko = keys ? heads(tensor(a[3]), c.kshape(), c.dt, c.dev, c.d.ko_stride, "dKo", false) : nullptr;
+    Pair grads(a[12], "grads must hold dgamma_q and dgamma_k"), out(a[13], "out must hold dQ and dK");
+    const bool given = a[12] != Py_None;
+    Out oq, ok, og[2];
+    void *dg[2] = {nullptr, nullptr};
+    for (int i = 0; i < 2; ++i) {
+        if (given) {
+            dg[i] = dense(grads.given[i], {c.d.head_dim}, F32, c.dev, "a gamma gradient");
+        } else if (c.d.norm && (i ? keys && gk : gq != nullptr)) {
+            og[i] = Out({c.d.head_dim}, F32, c.dev);
+            dg[i] = og[i].p;
+        }
+    }
+    int64_t sq[3], sk[3] = {0, 0, 0};
+    void *const pq = output(out, 0, oq, c.qshape(), c.dt, c.dev, sq, "out[0]");
+    void *const pk = keys ? output(out, 1, ok, c.kshape(), c.dt, c.dev, sk, "out[1]") : nullptr;
+    for (int i = 0; i < 3; ++i) {
+        c.d.q_stride[i] = in_q[i], c.d.k_stride[i] = in_k[i];
+        c.d.dq_stride[i] = sq[i], c.d.dk_stride[i] = sk[i];
+    }
+    call_here("pf_qk_norm_rotate_bwd", pf_qk_norm_rotate_bwd_workspace_bytes(&c.d), c.dev, [&](void *ws, size_t n, void *s) {
+        return pf_qk_norm_rotate_bwd(&c.d, q, k, gq, gk, c.positions, dqo, dko, pq, pk, dg[0], dg[1], given, ws, n, s);
+    });
+    return tuple({give_output(out, 0, oq), keys ? give_output(out, 1, ok) : borrowed(Py_None), given ? borrowed(grads.given[0]) : og[0].give(),
+                  given ? borrowed(grads.given[1]) : og[1].give()});
+}
+
+// Q, K, V, table, causal, scale (or None), max_distance, bidirectional, q_start, q_len, kv_len from a[0] on
+struct AttnCall {
+    pf_attention_desc d = {};
+    at::Device dev;
+    at::ScalarType dt;
+    void *q, *k, *v, *table, *start, *nq, *nk;
+    int64_t sq[4], sk[4], stat[3], tab[2];
+    explicit AttnCall(PyObject *const *a) : dev(tensor(a[0]).device()), dt(tensor(a[0]).scalar_type())
+    {
+        const Tensor &Q = tensor(a[0]), &K = tensor(a[1]), &V = tensor(a[2]);
+        dims(Q, 4, "Q");
+        dims(K, 4, "K");
+        for (int i = 0; i < 4; ++i) sq[i] = Q.size(i);
+        sk[0] = sq[0], sk[1] = K.size(1), sk[2] = K.size(2), sk[3] = sq[3];
+        d.B = sq[0], d.Lq = sq[1], d.Lk = sk[1], d.heads_q = (int)sq[2], d.heads_kv = (int)sk[2], d.head_dim = (int)sq[3];
+        d.dtype = dtype_code(Q);
+        q = heads(Q, at::IntArrayRef(sq, 4), dt, dev, d.q_stride, "Q", false);
+        k = heads(K, at::IntArrayRef(sk, 4), dt, dev, d.k_stride, "K", false);
+        v = heads(V, at::IntArrayRef(sk, 4), dt, dev, d.v_stride, "V", false);
+        d.causal = truth(a[4]);
+        d.scale = (float)(a[5] == Py_None ? 1.0 / std::sqrt((double)std::max<int64_t>(1, sq[3])) : QkCall::number(a[5]));
+        table = nullptr;
+        tab[0] = 0, tab[1] = sq[2];
+        if (a[3] != Py_None) {
+            const Tensor &T = tensor(a[3]);
+            dims(T, 2, "table");
+            tab[0] = T.size(0);
+            if (tab[0] == 0) throw Fail{PyExc_ValueError, "table has no bucket"};
+            table = dense(a[3], at::IntArrayRef(tab, 2), F32, dev, "table");
+            d.buckets = (int)std::min<int64_t>(tab[0], INT32_MAX);
+            d.max_distance = (int)integer(a[6]);
+            d.bidirectional = truth(a[7]);
+        }
+        start = dense(a[8], {sq[0]}, at::kInt, dev, "q_start");
+        nq = dense(a[9], {sq[0]}, at::kInt, dev, "q_len");
+        nk = dense(a[10], {sq[0]}, at::kInt, dev, "kv_len");
+        stat[0] = sq[0], stat[1] = sq[2], stat[2] = sq[1];
+    }
+};
+
+// Q .. kv_len as above, save_lse
+PyObject *attn_fwd(PyObject *const *a)
+{
+    AttnCall c(a);
+    const c10::DeviceGuard on(c.dev);
+    Out O(at::IntArrayRef(c.sq, 4), c.dt, c.dev), lse;
+    if (truth(a[11])) lse = Out(at::IntArrayRef(c.stat, 3), F32, c.dev);
+    call_here("pf_attention_fwd", pf_attention_fwd_workspace_bytes(&c.d), c.dev, [&](void *ws, size_t n, void *s) {
+        return pf_attention_fwd(&c.d, c.q, c.k, c.v, c.table, c.start, c.nq, c.nk, O.p, lse.p, ws, n, s);
+    });
+    return tuple({O.give(), lse.give()});
+}
+
+// Q .. kv_len as above, O, lse, dO, need_dtable, grads, out
+PyObject *attn_bwd(PyObject *const *a)
+{
+    AttnCall c(a);
+    const c10::DeviceGuard on(c.dev);
+    const at::IntArrayRef qs(c.sq, 4), ks(c.sk, 4), ts(c.tab, 2);
+    void *const o = dense(a[11], qs, c.dt, c.dev, "O"), *const lse = dense(a[12], at::IntArrayRef(c.stat, 3), F32, c.dev, "lse"),
+               *const g = dense(a[13], qs, c.dt, c.dev, "dO");
+    const bool given = a[15] != Py_None;
+    Out dt, d[3];
+    void *pt = given ? dense(a[15], ts, F32, c.dev, "grads") : nullptr, *p[3];
+    if (!given && c.table && truth(a[14])) {
+        dt = Out(ts, F32, c.dev);
+        pt = dt.p;
+    }
+    Ref items;
+    if (a[16] != Py_None) {
+        items.o = PySequence_Fast(a[16], "out must hold dQ, dK and dV");
+        if (!items.o) throw Fail{nullptr, ""};
+        if (PySequence_Fast_GET_SIZE(items.o) != 3) throw Fail{PyExc_ValueError, "out must hold dQ, dK and dV"};
+    }
+    PyObject *into[3];
+    for (int i = 0; i < 3; ++i) {
+        into[i] = items.o ? PySequence_Fast_GET_ITEM(items.o, i) : Py_None;
+        if (into[i] != Py_None) {
+            p[i] = dense(into[i], i ? ks : qs, c.dt, c.dev, "out");
+        } else {
+            d[i] = Out(i ? ks : qs, c.dt, c.dev);
+            p[i] = d[i].p;
+        }
+    }
+    call_here("pf_attention_bwd", pf_attention_bwd_workspace_bytes(&c.d), c.dev, [&](void *ws, size_t n, void *s) {
+        return pf_attention_bwd(&c.d, c.q, c.k, c.v, c.table, c.start, c.nq, c.nk, o, lse, g, p[0], p[1], p[2], pt, given, ws, n, s);
+    });
+    const auto give = [&](int i) { return into[i] != Py_None ? borrowed(into[i]) : d[i].give(); };
+    return tuple({give(0), give(1), give(2), given ? borrowed(a[15]) : dt.give()});
+}
+
+// tensors, state_bits, beta1, beta2, eps, plan, lr, grad_scale, steps
+PyObject *adamw_step(PyObject *const *a)
+{
+    pf_adamw_desc d = {};
+    d.tensors = integer(a[0]);
+    d.state_bits = (int)integer(a[1]);
+    d.beta1 = QkCall::number(a[2]);
+    d.beta2 = QkCall::number(a[3]);
+    d.eps = QkCall::number(a[4]);
+    const Tensor &plan = tensor(a[5]);
+    const auto dev = plan.device();
+    same_device(plan, dev);
+    const c10::DeviceGuard on(dev);
+    void *const p = address(plan, at::kByte), *const lr = dense(a[6], {1}, F32, dev, "lr");
+    void *scale = nullptr;
+    if (a[7] != Py_None) {
+        const Tensor &t = tensor(a[7]);
+        same_device(t, dev);
+        if (t.numel() != 1) throw Fail{PyExc_ValueError, "grad_scale must have one element"};
+        scale = address(t, F32);
+    }
+    const Tensor &steps = tensor(a[8]);
+    same_device(steps, dev);
+    if (steps.numel() != 1) throw Fail{PyExc_ValueError, "steps must have one element"};
+    void *const st = address(steps, at::kLong);
+    const size_t n = (size_t)plan.numel();
+    call_here("pf_adamw_step", 0, dev, [&](void *, size_t, void *s) { return pf_adamw_step(&d, p, n, lr, scale, st, s); });
+    Py_RETURN_NONE;
+}
+
 // bytes, a tensor on the device: the scratch buffer of the current stream, held by this thread until it gives it back
 PyObject *lend(PyObject *const *a)
 {
@@ -680,6 +991,11 @@ PyMethodDef methods[] = {CALL(linear_fwd, 8),
                          CALL(cell_bwd, 16),
                          CALL(stack_fwd, 9),
                          CALL(stack_bwd, 18),
+                         CALL(qk_fwd, 11),
+                         CALL(qk_bwd, 14),
+                         CALL(attn_fwd, 12),
+                         CALL(attn_bwd, 17),
+                         CALL(adamw_step, 9),
                          CALL(lend, 2),
                          CALL(give_back, 1),
                          {"set_errors", set_errors, METH_VARARGS, nullptr},
