@@ -205,6 +205,9 @@ __device__ __forceinline__ unsigned xcd_order(unsigned id, unsigned n)
     return x * per + (x < more ? x : more) + (id >> 3);
 }
 
+// The wave's number, known to be one for all its lanes (what is decided by it is a branch, not a mask)
+__device__ __forceinline__ int wave_of(int t) { return __builtin_amdgcn_readfirstlane(t >> 6); }
+
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); } // (one instruction, 1 ulp)
 
 // ------------------------------------------------------------------ host

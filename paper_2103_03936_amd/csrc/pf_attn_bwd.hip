@@ -43,7 +43,7 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= (TAB ? 128 : sizeof(T) == 2 
 
     const unsigned w = xcd_order(blockIdx.x, gridDim.x);
     const int tile = a.tiles - 1 - (int)(w % a.tiles), bh = w / a.tiles, b = bh / a.Hq, head = bh - b * a.Hq;
-    const int t = threadIdx.x, wave = t >> 6, lane = t & 63, col = lane & 31, h = lane >> 5;
+    const int t = threadIdx.x, wave = wave_of(t), lane = t & 63, col = lane & 31, h = lane >> 5;
     float *const diag = diag_all + wave * 32 * DIAG, *const sums = sums_all + wave * span;
     const AttnLens n(a, b);
     const int i0 = tile * 128 + wave * 32, i = i0 + col;
@@ -122,14 +122,23 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= (TAB ? 128 : sizeof(T) == 2 
                     mma(dp, row_frag(vrow + 16 * c, h), g[c]);
                 }
                 float ds[16];
+                const float base = flat - lse2;
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int j = ks + 8 * (e >> 2) + 4 * h + (e & 3);
-                    float x = s[e] * sl2 + flat;
-                    if (near) x = s[e] * sl2 + bias[clamped(j - pos, -far, far) + far];
-                    float p = exp2_fast(x - lse2);
-                    if (edge && (j >= n.nk || (a.causal && j > pos))) p = 0.f;
-                    ds[e] = p * (dp[e] - delta); // (first pass: delta is 0, and the sum of these is delta)
+                for (int e = 0; e < 16; ++e) ds[e] = s[e];
+                if (edge || near) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int j = ks + 8 * (e >> 2) + 4 * h + (e & 3);
+                        ds[e] = exp2_fast(ds[e] * sl2 + ((BIAS ? bias[clamped(j - pos, -far, far) + far] : 0.f) - lse2));
+                        if (j >= n.nk || (a.causal && j > pos)) ds[e] = 0.f;
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) ds[e] = exp2_fast(ds[e] * sl2 + base);
+                }
+#pragma unroll
+                for (int e = 0; e < 16; ++e) { // (first pass: delta is 0, and the sum of these is delta)
+                    ds[e] *= dp[e] - delta;
                     if (TAB && pass == 0) row += ds[e];
                 }
                 if (TAB && pass == 0) continue;
@@ -244,7 +253,7 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 128 ? 2 : 1) void attn_dkv_k
 
     const unsigned w = xcd_order(blockIdx.x, gridDim.x);
     const int tile = (int)(w % a.tiles), bk = w / a.tiles, b = bk / a.Hkv, kv = bk - b * a.Hkv;
-    const int t = threadIdx.x, wave = t >> 6, lane = t & 63, col = lane & 31, h = lane >> 5;
+    const int t = threadIdx.x, wave = wave_of(t), lane = t & 63, col = lane & 31, h = lane >> 5;
     const AttnLens n(a, b);
     const int far = a.bk.far, j0 = tile * 128 + wave * 32, j = j0 + col;
     const bool ok = j < n.nk;
@@ -313,17 +322,28 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 128 ? 2 : 1) void attn_dkv_k
                 float p[16], ds[16];
 #pragma unroll
                 for (int e4 = 0; e4 < 4; ++e4) {
-                    const float4 l4 = *(const float4 *)(lse_t + 32 * u + 8 * e4 + 4 * h), d4 = *(const float4 *)(delta_t + 32 * u + 8 * e4 + 4 * h);
-                    const float ll[4] = {l4.x, l4.y, l4.z, l4.w}, dd[4] = {d4.x, d4.y, d4.z, d4.w};
+                    const float4 l4 = *(const float4 *)(lse_t + 32 * u + 8 * e4 + 4 * h);
+                    const float ll[4] = {l4.x, l4.y, l4.z, l4.w};
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        const int e = 4 * e4 + x, pos = p0 + 8 * e4 + 4 * h + x;
-                        float y = s[e] * sl2 + flat;
-                        if (near) y = s[e] * sl2 + bias[clamped(j - pos, -far, far) + far];
-                        p[e] = exp2_fast(y - ll[x]);
-                        if (edge && (j >= n.nk || (a.causal && j > pos))) p[e] = 0.f;
-                        ds[e] = p[e] * (dp[e] - dd[x]);
+                    for (int x = 0; x < 4; ++x) p[4 * e4 + x] = ll[x];
+                }
+                if (edge || near) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int pos = p0 + 8 * (e >> 2) + 4 * h + (e & 3);
+                        p[e] = exp2_fast(s[e] * sl2 + ((BIAS ? bias[clamped(j - pos, -far, far) + far] : 0.f) - p[e]));
+                        if (j >= n.nk || (a.causal && j > pos)) p[e] = 0.f;
                     }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) p[e] = exp2_fast(s[e] * sl2 + (flat - p[e]));
+                }
+#pragma unroll
+                for (int e4 = 0; e4 < 4; ++e4) {
+                    const float4 d4 = *(const float4 *)(delta_t + 32 * u + 8 * e4 + 4 * h);
+                    const float dd[4] = {d4.x, d4.y, d4.z, d4.w};
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) ds[4 * e4 + x] = p[4 * e4 + x] * (dp[4 * e4 + x] - dd[x]);
                 }
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {

@@ -21,7 +21,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a)
 
     const unsigned w = xcd_order(blockIdx.x, gridDim.x);
     const int tile = a.tiles - 1 - (int)(w % a.tiles), bh = w / a.tiles, b = bh / a.Hq, head = bh - b * a.Hq;
-    const int t = threadIdx.x, wave = t >> 6, lane = t & 63, col = lane & 31, h = lane >> 5;
+    const int t = threadIdx.x, wave = wave_of(t), lane = t & 63, col = lane & 31, h = lane >> 5;
     const AttnLens n(a, b);
     const int i0 = tile * 128 + wave * 32, i = i0 + col; // the lane's query
     const bool ok = i < n.nq;
@@ -69,6 +69,9 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a)
         const bool edge = k0 + KT > n.nk || (a.causal && k0 + KT - 1 > pmin);
         const bool near = BIAS && k0 + KT - 1 - pmin > -far && k0 - pmax < far;
         const float flat = BIAS ? bias[k0 >= pmin ? 2 * far : 0] : 0.f; // where no key is near
+        // Away from the edges and the near keys, nothing is done to a product but one fused multiply-add on its way into the
+        // exponential; the maximum is that of the products themselves.
+        const bool plain = !edge && !near && sl2 > 0.f;
 #pragma unroll
         for (int u = 0; u < SUB; ++u) {
             f32x16_t acc = {};
@@ -76,17 +79,26 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a)
 #pragma unroll
             for (int c = 0; c < DP / 16; ++c) mma(acc, row_frag(row + 16 * c, h), q[c]);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int j = k0 + 32 * u + 8 * (e >> 2) + 4 * h + (e & 3);
-                float x = acc[e] * sl2 + flat;
-                if (near) x = acc[e] * sl2 + bias[clamped(j - pos, -far, far) + far];
-                if (edge && (j >= n.nk || (a.causal && j > pos))) x = -INFINITY;
-                s[u][e] = x;
-                top = fmaxf(top, x);
-            }
+            for (int e = 0; e < 16; ++e) s[u][e] = acc[e];
         }
+        if (!plain) {
+#pragma unroll
+            for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int j = k0 + 32 * u + 8 * (e >> 2) + 4 * h + (e & 3);
+                    s[u][e] = s[u][e] * sl2 + (BIAS ? bias[clamped(j - pos, -far, far) + far] : 0.f);
+                    if (j >= n.nk || (a.causal && j > pos)) s[u][e] = -INFINITY;
+                }
+        }
+#pragma unroll
+        for (int u = 0; u < SUB; ++u)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) top = fmaxf(top, s[u][e]);
+        if (plain) top = top * sl2 + flat;
         top = fmaxf(top, __shfl_xor(top, 32));
         const float m_new = fmaxf(m, top), base = m_new == -INFINITY ? 0.f : m_new;
+        const float mul = plain ? sl2 : 1.f, add = plain ? flat - base : -base;
         if (__any(m_new > m)) {
             const float f = exp2_fast(m - base);
             sum *= f;
@@ -100,7 +112,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a)
         for (int u = 0; u < SUB; ++u) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                s[u][e] = exp2_fast(s[u][e] - base);
+                s[u][e] = exp2_fast(s[u][e] * mul + add);
                 sum += s[u][e];
             }
 #pragma unroll

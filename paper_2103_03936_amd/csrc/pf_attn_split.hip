@@ -28,7 +28,7 @@ __global__ __launch_bounds__(64 * SPLIT_WAVES<T>) void attn_split_kernel(AttnArg
     extern __shared__ __attribute__((aligned(16))) char lds[];
     float *const ml = (float *)(lds + SplitLds<T, DP>::AREA); // [2][NW][32]: the waves' maxima and sums
     uint8_t *const lut = (uint8_t *)(ml + 2 * NW * 32);       // bucket of each distance from -far to far
-    const int t = threadIdx.x, wave = t >> 6, lane = t & 63, col = lane & 31, h = lane >> 5;
+    const int t = threadIdx.x, wave = wave_of(t), lane = t & 63, col = lane & 31, h = lane >> 5;
     T *const vt = (T *)(lds + wave * Tl::BYTES);
 
     const unsigned w = xcd_order(blockIdx.x, gridDim.x);
