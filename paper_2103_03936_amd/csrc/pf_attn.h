@@ -53,22 +53,8 @@ __device__ __forceinline__ void mma(f32x16_t &c, const Frag<float> &a, const Fra
     for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[j], b.v[j], c, 0, 0, 0);
 }
 
-// Operand with the index along the rows and the contraction along 16 columns from `p` on, p in the lane's row; h = lane / 32.
-// (The halves share the 16 columns in an order of their own, the same for both operands.)
-__device__ __forceinline__ Frag<bf16_t> row_frag(const bf16_t *p, int h)
-{
-    Frag<bf16_t> f;
-    f.v = *(const bf16x8_t *)(p + 8 * h);
-    return f;
-}
-__device__ __forceinline__ Frag<float> row_frag(const float *p, int h)
-{
-    Frag<float> f;
-    const float4 a = *(const float4 *)(p + 4 * h), b = *(const float4 *)(p + 8 + 4 * h);
-    f.v[0] = a.x, f.v[1] = a.y, f.v[2] = a.z, f.v[3] = a.w, f.v[4] = b.x, f.v[5] = b.y, f.v[6] = b.z, f.v[7] = b.w;
-    return f;
-}
-// The same from global memory, zeros where the row does not exist (ok) or has no such column (head_dim is a multiple of 8)
+// Operand with the index along the rows and the contraction along 16 columns from `col` on, `row` the lane's row in global
+// memory; h = lane / 32.  (The halves share the 16 columns in an order of their own, the same for both operands.)  Zeros where the row does not exist (ok) or has no such column (head_dim is a multiple of 8)
 __device__ __forceinline__ Frag<bf16_t> row_frag_global(const bf16_t *row, int col, int D, int h, bool ok)
 {
     Frag<bf16_t> f;
@@ -83,29 +69,6 @@ __device__ __forceinline__ Frag<float> row_frag_global(const float *row, int col
     if (ok && col + 4 * h < D) a = *(const float4 *)(row + col + 4 * h);
     if (ok && col + 8 + 4 * h < D) b = *(const float4 *)(row + col + 8 + 4 * h);
     f.v[0] = a.x, f.v[1] = a.y, f.v[2] = a.z, f.v[3] = a.w, f.v[4] = b.x, f.v[5] = b.y, f.v[6] = b.z, f.v[7] = b.w;
-    return f;
-}
-
-// Operand with the index along the columns c0 .. c0 + 31 of a row-major LDS tile and the contraction along its rows
-// r0 .. r0 + 15, in the order in which a product's result lies in the lanes (above)
-__device__ __forceinline__ Frag<bf16_t> col_frag(const bf16_t *tile, int pitch, int r0, int c0, int lane)
-{
-    typedef __attribute__((address_space(3))) bf16x4_t *lds_ptr;
-    const int g = lane >> 4, i = lane & 15;
-    const bf16_t *p = tile + (r0 + 4 * (g >> 1) + (i >> 2)) * pitch + c0 + 16 * (g & 1) + 4 * (i & 3);
-    const bf16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_ptr)p);
-    const bf16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_ptr)(p + 8 * pitch));
-    Frag<bf16_t> f;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) f.v[e] = lo[e], f.v[4 + e] = hi[e];
-    return f;
-}
-__device__ __forceinline__ Frag<float> col_frag(const float *tile, int pitch, int r0, int c0, int lane)
-{
-    const float *p = tile + (r0 + 4 * (lane >> 5)) * pitch + c0 + (lane & 31);
-    Frag<float> f;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) f.v[e] = p[e * pitch], f.v[4 + e] = p[(8 + e) * pitch];
     return f;
 }
 
@@ -135,12 +98,24 @@ __device__ __forceinline__ void put4(bf16_t *p, float a, float b, float c, float
 }
 
 // ------------------------------------------------------------------ tiles
-// ROWS rows of DP columns in LDS, 16 bytes of padding to a row; a workgroup of THREADS loads one through registers
+// ROWS rows of DP columns in LDS, loaded by THREADS threads through registers.  The tile is read in two ways: as an operand
+// by rows (16 lanes that a cycle serves have one 16-byte piece of 16 rows) and by columns (the transposing reads: 32 lanes that a
+// cycle serves have four adjacent pieces of four rows).  bf16: without padding, piece c of row r lies at c ^ turn(r); both
+// ways meet each of the 64 banks once.  float: rows padded by 16 bytes.
 template <typename T, int DP, int ROWS, int THREADS>
 struct Tile {
-    static constexpr int VEC = 16 / sizeof(T), PITCH = DP + VEC, PIECES = ROWS * DP / VEC, N = (PIECES + THREADS - 1) / THREADS;
+    static constexpr int VEC = 16 / sizeof(T), PIECES = ROWS * DP / VEC, N = (PIECES + THREADS - 1) / THREADS;
+    static constexpr bool TURNED = sizeof(T) == 2;
+    static constexpr int PITCH = TURNED ? (DP == 96 ? 128 : DP) : DP + VEC, CHUNKS = PITCH / VEC;
     static constexpr int BYTES = ROWS * PITCH * (int)sizeof(T);
     uint4 r[N];
+    static __device__ __forceinline__ int turn(int row)
+    {
+        if constexpr (!TURNED) return 0;
+        if constexpr (CHUNKS == 16) return (row & 3) << 2 | (row >> 2 & 3);
+        if constexpr (CHUNKS == 8) return (row >> 1 & 1) << 2 | (row >> 2 & 3);
+        return row >> 2 & 3;
+    }
     // rows r0 .. r0 + ROWS - 1 of `src` (elements `stride` apart), zeros from row `rows` and column D on
     __device__ __forceinline__ void load(const T *src, i64 stride, int r0, int rows, int D, int t)
     {
@@ -155,9 +130,43 @@ struct Tile {
     {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int p = t + i * THREADS, row = p / (DP / VEC), col = p % (DP / VEC) * VEC;
-            if (PIECES % THREADS == 0 || p < PIECES) *(uint4 *)(lds + row * PITCH + col) = r[i];
+            const int p = t + i * THREADS, row = p / (DP / VEC), c = p % (DP / VEC);
+            if (PIECES % THREADS == 0 || p < PIECES) *(uint4 *)(lds + row * PITCH + (c ^ turn(row)) * VEC) = r[i];
         }
+    }
+    // Operand with the index along the rows (the lane's: r0 + lane % 32) and the contraction along columns 16 c ..
+    static __device__ __forceinline__ Frag<T> by_rows(const T *lds, int r0, int c, int lane)
+    {
+        const int row = lane & 31, h = lane >> 5;
+        const T *const p = lds + (r0 + row) * PITCH;
+        Frag<T> f;
+        if constexpr (TURNED) {
+            f.v = *(const bf16x8_t *)(p + ((2 * c + h) ^ turn(row)) * VEC);
+        } else {
+            const float4 x = *(const float4 *)(p + 16 * c + 4 * h), y = *(const float4 *)(p + 16 * c + 8 + 4 * h);
+            f.v[0] = x.x, f.v[1] = x.y, f.v[2] = x.z, f.v[3] = x.w, f.v[4] = y.x, f.v[5] = y.y, f.v[6] = y.z, f.v[7] = y.w;
+        }
+        return f;
+    }
+    // Operand with the index along the columns 32 d .. 32 d + 31 and the contraction along rows r0 .. r0 + 15 (r0 a multiple
+    // of 16), in the order in which a product's result lies in the lanes
+    static __device__ __forceinline__ Frag<T> by_cols(const T *lds, int r0, int d, int lane)
+    {
+        Frag<T> f;
+        if constexpr (TURNED) {
+            typedef __attribute__((address_space(3))) bf16x4_t *lds_ptr;
+            const int g = lane >> 4, i = lane & 15, row = 4 * (g >> 1) + (i >> 2), c = 4 * d + 2 * (g & 1) + (i >> 1 & 1);
+            const T *const lo = lds + (r0 + row) * PITCH + (c ^ turn(row)) * VEC + 4 * (i & 1);
+            const T *const hi = lds + (r0 + row + 8) * PITCH + (c ^ turn(row + 8)) * VEC + 4 * (i & 1);
+            const bf16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_ptr)lo), y = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_ptr)hi);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) f.v[e] = x[e], f.v[4 + e] = y[e];
+        } else {
+            const T *const p = lds + (r0 + 4 * (lane >> 5)) * PITCH + 32 * d + (lane & 31);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) f.v[e] = p[e * PITCH], f.v[4 + e] = p[(8 + e) * PITCH];
+        }
+        return f;
     }
 };
 

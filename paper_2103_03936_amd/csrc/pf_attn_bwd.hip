@@ -115,11 +115,10 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= (TAB ? 128 : sizeof(T) == 2 
                 const bool near = BIAS && ks + 31 - pmin > -far && ks - pmax < far;
                 const float flat = BIAS ? bias[ks >= pmin ? 2 * far : 0] : 0.f;
                 f32x16_t s = {}, dp = {};
-                const T *const krow = kt + (32 * u + col) * Tl::PITCH, *const vrow = vt + (32 * u + col) * Tl::PITCH;
-#pragma unroll
+                #pragma unroll
                 for (int c = 0; c < DP / 16; ++c) {
-                    mma(s, row_frag(krow + 16 * c, h), q[c]);
-                    mma(dp, row_frag(vrow + 16 * c, h), g[c]);
+                    mma(s, Tl::by_rows(kt, 32 * u, c, lane), q[c]);
+                    mma(dp, Tl::by_rows(vt, 32 * u, c, lane), g[c]);
                 }
                 float ds[16];
                 const float base = flat - lse2;
@@ -186,7 +185,7 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= (TAB ? 128 : sizeof(T) == 2 
                     Frag<T> p;
                     pack(ds, c, p);
 #pragma unroll
-                    for (int d = 0; d < DP / 32; ++d) mma(dq[d], col_frag(kt, Tl::PITCH, 32 * u + 16 * c, 32 * d, lane), p);
+                    for (int d = 0; d < DP / 32; ++d) mma(dq[d], Tl::by_cols(kt, 32 * u + 16 * c, d, lane), p);
                 }
             }
         }
@@ -313,11 +312,10 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 128 ? 2 : 1) void attn_dkv_k
                 const bool near = BIAS && j0 + 31 - p0 > -far && j0 - (p0 + 31) < far;
                 const float flat = BIAS ? bias[j0 >= p0 ? 2 * far : 0] : 0.f;
                 f32x16_t s = {}, dp = {};
-                const T *const qrow_t = qt + (32 * u + col) * Tl::PITCH, *const grow_t = gt + (32 * u + col) * Tl::PITCH;
-#pragma unroll
+                #pragma unroll
                 for (int c = 0; c < DP / 16; ++c) {
-                    mma(s, row_frag(qrow_t + 16 * c, h), k[c]);
-                    mma(dp, row_frag(grow_t + 16 * c, h), v[c]);
+                    mma(s, Tl::by_rows(qt, 32 * u, c, lane), k[c]);
+                    mma(dp, Tl::by_rows(gt, 32 * u, c, lane), v[c]);
                 }
                 float p[16], ds[16];
 #pragma unroll
@@ -350,10 +348,10 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 128 ? 2 : 1) void attn_dkv_k
                     Frag<T> f;
                     pack(p, c, f);
 #pragma unroll
-                    for (int d = 0; d < DP / 32; ++d) mma(dv[d], col_frag(gt, Tl::PITCH, 32 * u + 16 * c, 32 * d, lane), f);
+                    for (int d = 0; d < DP / 32; ++d) mma(dv[d], Tl::by_cols(gt, 32 * u + 16 * c, d, lane), f);
                     pack(ds, c, f);
 #pragma unroll
-                    for (int d = 0; d < DP / 32; ++d) mma(dk[d], col_frag(qt, Tl::PITCH, 32 * u + 16 * c, 32 * d, lane), f);
+                    for (int d = 0; d < DP / 32; ++d) mma(dk[d], Tl::by_cols(qt, 32 * u + 16 * c, d, lane), f);
                 }
             }
         }

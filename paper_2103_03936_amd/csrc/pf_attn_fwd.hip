@@ -16,8 +16,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a)
     constexpr int KT = KEYS<T>, SUB = KT / 32;
     using Tl = Tile<T, DP, KT, 256>;
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    T *const kt = (T *)lds, *const vt = (T *)(lds + Tl::BYTES);
-    float *const bias = (float *)(lds + 2 * Tl::BYTES);
+    float *const bias = (float *)(lds + 4 * Tl::BYTES);
 
     const unsigned w = xcd_order(blockIdx.x, gridDim.x);
     const int tile = a.tiles - 1 - (int)(w % a.tiles), bh = w / a.tiles, b = bh / a.Hq, head = bh - b * a.Hq;
@@ -50,79 +49,102 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a)
     float m = -INFINITY, sum = 0.f; // the running maximum (base 2); the sum of the lane's keys
 
     Tl kr, vr;
+    const auto tiles = [&](int k) { return (T *)(lds + (k & 1) * 2 * Tl::BYTES); };
     if (keys > 0) {
         kr.load(Kp, a.ks[1], 0, n.nk, a.D, t);
         vr.load(Vp, a.vs[1], 0, n.nk, a.D, t);
+        kr.store(tiles(0), t);
+        vr.store(tiles(0) + KT * Tl::PITCH, t);
     }
-    for (int k0 = 0; k0 < keys; k0 += KT) {
-        __syncthreads();
-        kr.store(kt, t);
-        vr.store(vt, t);
-        if (k0 + KT < keys) {
+    __syncthreads();
+    for (int k0 = 0, turn = 0; k0 < keys; k0 += KT, ++turn) {
+        const T *const kt = tiles(turn), *const vt = kt + KT * Tl::PITCH;
+        const bool more = k0 + KT < keys;
+        if (more) {
             kr.load(Kp, a.ks[1], k0 + KT, n.nk, a.D, t);
             vr.load(Vp, a.vs[1], k0 + KT, n.nk, a.D, t);
         }
-        __syncthreads();
-        if (idle || (a.causal && k0 > pmax)) continue;
-        float s[SUB][16];
-        float top = -INFINITY;
-        const bool edge = k0 + KT > n.nk || (a.causal && k0 + KT - 1 > pmin);
-        const bool near = BIAS && k0 + KT - 1 - pmin > -far && k0 - pmax < far;
-        const float flat = BIAS ? bias[k0 >= pmin ? 2 * far : 0] : 0.f; // where no key is near
-        // Away from the edges and the near keys, nothing is done to a product but one fused multiply-add on its way into the
-        // exponential; the maximum is that of the products themselves.
-        const bool plain = !edge && !near && sl2 > 0.f;
+        if (!idle && !(a.causal && k0 > pmax)) {
+            float s[SUB][16];
+            float top = -INFINITY;
+            const bool edge = k0 + KT > n.nk || (a.causal && k0 + KT - 1 > pmin);
+            const bool near = BIAS && k0 + KT - 1 - pmin > -far && k0 - pmax < far;
+            const float flat = BIAS ? bias[k0 >= pmin ? 2 * far : 0] : 0.f; // where no key is near
+            // Away from the edges and the near keys, nothing is done to a product but one fused multiply-add on its way into
+            // the exponential; the maximum is that of the products themselves.
+            const bool plain = !edge && !near && sl2 > 0.f;
+            // (the operands of a block of keys are read while the block before it is multiplied)
+            Frag<T> kf[2][DP / 16];
 #pragma unroll
-        for (int u = 0; u < SUB; ++u) {
-            f32x16_t acc = {};
-            const T *const row = kt + (32 * u + col) * Tl::PITCH;
+            for (int c = 0; c < DP / 16; ++c) kf[0][c] = Tl::by_rows(kt, 0, c, lane);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int c = 0; c < DP / 16; ++c) mma(acc, row_frag(row + 16 * c, h), q[c]);
+            for (int u = 0; u < SUB; ++u) {
+                f32x16_t acc = {};
 #pragma unroll
-            for (int e = 0; e < 16; ++e) s[u][e] = acc[e];
-        }
-        if (!plain) {
+                for (int c = 0; c < DP / 16; ++c) {
+                    if (u + 1 < SUB) kf[(u + 1) & 1][c] = Tl::by_rows(kt, 32 * (u + 1), c, lane);
+                    mma(acc, kf[u & 1][c], q[c]);
+                }
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[u][e] = acc[e];
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (!plain) {
+#pragma unroll
+                for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int j = k0 + 32 * u + 8 * (e >> 2) + 4 * h + (e & 3);
+                        s[u][e] = s[u][e] * sl2 + (BIAS ? bias[clamped(j - pos, -far, far) + far] : 0.f);
+                        if (j >= n.nk || (a.causal && j > pos)) s[u][e] = -INFINITY;
+                    }
+            }
 #pragma unroll
             for (int u = 0; u < SUB; ++u)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int j = k0 + 32 * u + 8 * (e >> 2) + 4 * h + (e & 3);
-                    s[u][e] = s[u][e] * sl2 + (BIAS ? bias[clamped(j - pos, -far, far) + far] : 0.f);
-                    if (j >= n.nk || (a.causal && j > pos)) s[u][e] = -INFINITY;
+                for (int e = 0; e < 16; ++e) top = fmaxf(top, s[u][e]);
+            if (plain) top = top * sl2 + flat;
+            top = fmaxf(top, __shfl_xor(top, 32));
+            // The maximum that values are taken relative to follows only when it is left by 2^8: sums and rounded P lose
+            // nothing to a common factor, and most tiles spare the products their rescaling.
+            if (__any(top > m + 8.f)) {
+                const float m_new = fmaxf(m, top), f = exp2_fast(m - (m_new == -INFINITY ? 0.f : m_new));
+                sum *= f;
+#pragma unroll
+                for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) o[d][e] *= f;
+                m = m_new;
+            }
+            const float base = m == -INFINITY ? 0.f : m, mul = plain ? sl2 : 1.f, add = plain ? flat - base : -base;
+            Frag<T> vf[2][DP / 32];
+#pragma unroll
+            for (int d = 0; d < DP / 32; ++d) vf[0][d] = Tl::by_cols(vt, 0, d, lane);
+#pragma unroll
+            for (int c = 0; c < 2 * SUB; ++c) { // 16 keys at a time
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    float &x = s[c / 2][8 * (c & 1) + e];
+                    x = exp2_fast(x * mul + add);
+                    sum += x;
                 }
-        }
-#pragma unroll
-        for (int u = 0; u < SUB; ++u)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) top = fmaxf(top, s[u][e]);
-        if (plain) top = top * sl2 + flat;
-        top = fmaxf(top, __shfl_xor(top, 32));
-        const float m_new = fmaxf(m, top), base = m_new == -INFINITY ? 0.f : m_new;
-        const float mul = plain ? sl2 : 1.f, add = plain ? flat - base : -base;
-        if (__any(m_new > m)) {
-            const float f = exp2_fast(m - base);
-            sum *= f;
-#pragma unroll
-            for (int d = 0; d < DP / 32; ++d)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) o[d][e] *= f;
-            m = m_new;
-        }
-#pragma unroll
-        for (int u = 0; u < SUB; ++u) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                s[u][e] = exp2_fast(s[u][e] * mul + add);
-                sum += s[u][e];
-            }
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
                 Frag<T> p;
-                pack(s[u], c, p);
+                pack(s[c / 2], c & 1, p);
+                if (c + 1 < 2 * SUB) {
 #pragma unroll
-                for (int d = 0; d < DP / 32; ++d) mma(o[d], col_frag(vt, Tl::PITCH, 32 * u + 16 * c, 32 * d, lane), p);
+                    for (int d = 0; d < DP / 32; ++d) vf[(c + 1) & 1][d] = Tl::by_cols(vt, 16 * (c + 1), d, lane);
+                }
+#pragma unroll
+                for (int d = 0; d < DP / 32; ++d) mma(o[d], vf[c & 1][d], p);
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
+        if (more) {
+            kr.store(tiles(turn + 1), t);
+            vr.store(tiles(turn + 1) + KT * Tl::PITCH, t);
+        }
+        __syncthreads();
     }
     sum += __shfl_xor(sum, 32);
     if (i >= a.Lq) return;
@@ -205,7 +227,7 @@ static int attn_fwd_launch(const AttnArgs &a, hipStream_t s)
 {
     using Tl = Tile<T, DP, KEYS<T>, 256>;
     const unsigned blocks = (unsigned)a.B * a.Hq * a.tiles;
-    const size_t lds = 2 * Tl::BYTES + (a.buckets ? (2 * a.bk.far + 1) * sizeof(float) : 0);
+    const size_t lds = 4 * Tl::BYTES + (a.buckets ? (2 * a.bk.far + 1) * sizeof(float) : 0);
     int st = PF_OK;
     if (a.buckets)
         PF_LAUNCH_LDS(st, "attn_fwd", (attn_fwd_kernel<T, DP, true>), dim3(blocks), dim3(256), lds, s, a);

@@ -124,7 +124,7 @@ __global__ __launch_bounds__(64 * SPLIT_WAVES<T>) void attn_split_kernel(AttnArg
             Frag<T> p;
             pack(s, c, p);
 #pragma unroll
-            for (int d = 0; d < DP / 32; ++d) mma(o[d], col_frag(vt, Tl::PITCH, 16 * c, 32 * d, lane), p);
+            for (int d = 0; d < DP / 32; ++d) mma(o[d], Tl::by_cols(vt, 16 * c, d, lane), p);
         }
     }
     sum += __shfl_xor(sum, 32);
