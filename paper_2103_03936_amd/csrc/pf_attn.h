@@ -10,7 +10,7 @@
 #pragma once
 
 #include "pf_attn_bias.h"
-#include "pf_common.h"
+#include "pf_tile.h"
 
 namespace pf {
 
@@ -72,6 +72,28 @@ __device__ __forceinline__ Frag<float> row_frag_global(const float *row, int col
     return f;
 }
 
+// The same through a descriptor that ends with the last row; `at`: bytes to the lane's row
+__device__ __forceinline__ Frag<bf16_t> row_frag_buffer(const BufSrc &src, uint32_t at, int col, int D, int h, bf16_t *)
+{
+    union {
+        uint4 u;
+        bf16x8_t v;
+    } w;
+    w.u = src.load(col + 8 * h < D ? at + 2 * (col + 8 * h) : BUF_OUT);
+    Frag<bf16_t> f;
+    f.v = w.v;
+    return f;
+}
+__device__ __forceinline__ Frag<float> row_frag_buffer(const BufSrc &src, uint32_t at, int col, int D, int h, float *)
+{
+    const uint4 a = src.load(col + 4 * h < D ? at + 4 * (col + 4 * h) : BUF_OUT), b = src.load(col + 8 + 4 * h < D ? at + 4 * (col + 8 + 4 * h) : BUF_OUT);
+    Frag<float> f;
+    const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f.v[e] = __uint_as_float(w[e]);
+    return f;
+}
+
 // Eight values of a result (its registers 8 c .. 8 c + 7) as the operand for rows 16 c .. 16 c + 15; bf16: rounded to
 // nearest even, the one rounding of P and dS, half a step of 2^-8 each
 __device__ __forceinline__ void pack(const float (&x)[16], int c, Frag<bf16_t> &f)
@@ -109,6 +131,7 @@ struct Tile {
     static constexpr int PITCH = TURNED ? (DP == 96 ? 128 : DP) : DP + VEC, CHUNKS = PITCH / VEC;
     static constexpr int BYTES = ROWS * PITCH * (int)sizeof(T);
     uint4 r[N];
+    uint32_t at[N]; // bytes from the tile's first row to the thread's pieces
     static __device__ __forceinline__ int turn(int row)
     {
         if constexpr (!TURNED) return 0;
@@ -116,15 +139,24 @@ struct Tile {
         if constexpr (CHUNKS == 8) return (row >> 1 & 1) << 2 | (row >> 2 & 3);
         return row >> 2 & 3;
     }
-    // rows r0 .. r0 + ROWS - 1 of `src` (elements `stride` apart), zeros from row `rows` and column D on
-    __device__ __forceinline__ void load(const T *src, i64 stride, int r0, int rows, int D, int t)
+    // elements `stride` from one row to the next, D columns (the others are zeros)
+    __device__ __forceinline__ Tile(i64 stride, int D, int t)
     {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int p = t + i * THREADS, row = p / (DP / VEC), col = p % (DP / VEC) * VEC;
-            r[i] = make_uint4(0u, 0u, 0u, 0u);
-            if ((PIECES % THREADS == 0 || p < PIECES) && r0 + row < rows && col < D) r[i] = *(const uint4 *)(src + (r0 + row) * stride + col);
+            const bool in = (PIECES % THREADS == 0 || p < PIECES) && col < D;
+            at[i] = in ? (uint32_t)(row * (int)stride + col) * (uint32_t)sizeof(T) : BUF_OUT;
         }
+    }
+    // ROWS rows from `first` on (the same for all threads), zeros from row `rows` on.  The descriptor ends with the last
+    // row, so that no load needs a branch.
+    __device__ __forceinline__ void load(const T *first, i64 stride, int rows, int D)
+    {
+        const int n = rows < ROWS ? rows : ROWS;
+        const BufSrc src(first, n > 0 ? ((n - 1) * (int)stride + D) * (int)sizeof(T) : 0);
+#pragma unroll
+        for (int i = 0; i < N; ++i) r[i] = src.load(at[i]);
     }
     __device__ __forceinline__ void store(T *lds, int t) const
     {

@@ -91,11 +91,11 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= (TAB ? 128 : sizeof(T) == 2 
     for (int d = 0; d < DP / 32; ++d) dq[d] = f32x16_t{};
     float before = 0.f, after = 0.f; // sums of dS in blocks that are further than `far` off
 
-    Tl kr, vr;
+    Tl kr(a.ks[1], a.D, t), vr(a.vs[1], a.D, t);
     for (int pass = TAB ? 0 : 1; pass < 2; ++pass) {
         if (keys > 0) {
-            kr.load(Kp, a.ks[1], 0, n.nk, a.D, t);
-            vr.load(Vp, a.vs[1], 0, n.nk, a.D, t);
+            kr.load(Kp, a.ks[1], n.nk, a.D);
+            vr.load(Vp, a.vs[1], n.nk, a.D);
         }
         float row = 0.f;
         for (int k0 = 0; k0 < keys; k0 += KT) {
@@ -103,8 +103,8 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= (TAB ? 128 : sizeof(T) == 2 
             kr.store(kt, t);
             vr.store(vt, t);
             if (k0 + KT < keys) {
-                kr.load(Kp, a.ks[1], k0 + KT, n.nk, a.D, t);
-                vr.load(Vp, a.vs[1], k0 + KT, n.nk, a.D, t);
+                kr.load(Kp + (i64)(k0 + KT) * a.ks[1], a.ks[1], n.nk - (k0 + KT), a.D);
+                vr.load(Vp + (i64)(k0 + KT) * a.vs[1], a.vs[1], n.nk - (k0 + KT), a.D);
             }
             __syncthreads();
             if (idle || (a.causal && k0 > pmax)) continue;
@@ -275,14 +275,14 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 128 ? 2 : 1) void attn_dkv_k
     if (a.causal) begin = clamped(tile * 128 - n.start, 0, a.Lq) / QT * QT;
     if (tile * 128 >= n.nk) begin = n.nq;
     const i64 qrow = (i64)a.Hq * a.D;
+    Tl qr(a.qs[1], a.D, t), gr(qrow, a.D, t);
     for (int g0 = 0; g0 < a.G; ++g0) {
         const int head = kv * a.G + g0;
         const T *const Qp = (const T *)a.Q + b * a.qs[0] + head * a.qs[2], *const Gp = (const T *)a.dO + ((i64)b * a.Lq * a.Hq + head) * a.D;
         const i64 stat = ((i64)b * a.Hq + head) * a.Lq;
-        Tl qr, gr;
         if (begin < n.nq) {
-            qr.load(Qp, a.qs[1], begin, n.nq, a.D, t);
-            gr.load(Gp, qrow, begin, n.nq, a.D, t);
+            qr.load(Qp + (i64)(begin) * a.qs[1], a.qs[1], n.nq - (begin), a.D);
+            gr.load(Gp + (i64)(begin) * qrow, qrow, n.nq - (begin), a.D);
         }
         if (BIAS && begin < n.nq) {
             __syncthreads(); // (the last head's bias is not used any more)
@@ -299,8 +299,8 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 128 ? 2 : 1) void attn_dkv_k
                 delta_t[t] = i < n.nq ? a.delta[stat + i] : 0.f;
             }
             if (i0 + QT < n.nq) {
-                qr.load(Qp, a.qs[1], i0 + QT, n.nq, a.D, t);
-                gr.load(Gp, qrow, i0 + QT, n.nq, a.D, t);
+                qr.load(Qp + (i64)(i0 + QT) * a.qs[1], a.qs[1], n.nq - (i0 + QT), a.D);
+                gr.load(Gp + (i64)(i0 + QT) * qrow, qrow, n.nq - (i0 + QT), a.D);
             }
             __syncthreads();
             if (j0 >= n.nk) continue;

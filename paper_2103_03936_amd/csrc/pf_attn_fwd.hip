@@ -48,11 +48,11 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a)
     for (int d = 0; d < DP / 32; ++d) o[d] = f32x16_t{};
     float m = -INFINITY, sum = 0.f; // the running maximum (base 2); the sum of the lane's keys
 
-    Tl kr, vr;
+    Tl kr(a.ks[1], a.D, t), vr(a.vs[1], a.D, t);
     const auto tiles = [&](int k) { return (T *)(lds + (k & 1) * 2 * Tl::BYTES); };
     if (keys > 0) {
-        kr.load(Kp, a.ks[1], 0, n.nk, a.D, t);
-        vr.load(Vp, a.vs[1], 0, n.nk, a.D, t);
+        kr.load(Kp, a.ks[1], n.nk, a.D);
+        vr.load(Vp, a.vs[1], n.nk, a.D);
         kr.store(tiles(0), t);
         vr.store(tiles(0) + KT * Tl::PITCH, t);
     }
@@ -61,8 +61,8 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a)
         const T *const kt = tiles(turn), *const vt = kt + KT * Tl::PITCH;
         const bool more = k0 + KT < keys;
         if (more) {
-            kr.load(Kp, a.ks[1], k0 + KT, n.nk, a.D, t);
-            vr.load(Vp, a.vs[1], k0 + KT, n.nk, a.D, t);
+            kr.load(Kp + (i64)(k0 + KT) * a.ks[1], a.ks[1], n.nk - (k0 + KT), a.D);
+            vr.load(Vp + (i64)(k0 + KT) * a.vs[1], a.vs[1], n.nk - (k0 + KT), a.D);
         }
         if (!idle && !(a.causal && k0 > pmax)) {
             float s[SUB][16];
@@ -197,6 +197,9 @@ int attn_check(const pf_attention_desc *d)
     }
     const int unit = 16 / (d->dtype == PF_BF16 ? 2 : 4);
     if (!strides_ok(d->q_stride, unit) || !strides_ok(d->k_stride, unit) || !strides_ok(d->v_stride, unit)) return PF_ERR_UNSUPPORTED;
+    // a tile of 64 tokens is read through one descriptor, with offsets of 31 bits
+    const i64 q = (i64)d->heads_q * d->head_dim, k = (i64)d->heads_kv * d->head_dim, most = (1 << 22) - d->head_dim;
+    if (q > most || k > most || d->q_stride[1] > most || d->k_stride[1] > most || d->v_stride[1] > most) return PF_ERR_UNSUPPORTED;
     return PF_OK;
 }
 

@@ -65,13 +65,15 @@ __global__ __launch_bounds__(64 * SPLIT_WAVES<T>) void attn_split_kernel(AttnArg
     for (int d = 0; d < DP / 32; ++d) o[d] = f32x16_t{};
     float m = -INFINITY, sum = 0.f;
 
-    Tl vr;
+    Tl vr(a.vs[1], a.D, lane);
     Frag<T> kr[DP / 16];
+    const uint32_t kat = (uint32_t)(col * (int)a.ks[1]) * (uint32_t)sizeof(T);
     const auto fetch = [&](int k) {
-        const int j = 32 * k + col;
+        const int rows = n.nk - 32 * k < 32 ? n.nk - 32 * k : 32;
+        const BufSrc src(Kp + (i64)(32 * k) * a.ks[1], ((rows - 1) * (int)a.ks[1] + a.D) * (int)sizeof(T));
 #pragma unroll
-        for (int c = 0; c < DP / 16; ++c) kr[c] = row_frag_global(Kp + j * a.ks[1], 16 * c, a.D, h, j < n.nk);
-        vr.load(Vp, a.vs[1], 32 * k, n.nk, a.D, lane);
+        for (int c = 0; c < DP / 16; ++c) kr[c] = row_frag_buffer(src, kat, 16 * c, a.D, h, (T *)nullptr);
+        vr.load(Vp + (i64)(32 * k) * a.vs[1], a.vs[1], n.nk - (32 * k), a.D);
     };
     if (first + wave < end) fetch(first + wave);
     for (int k = first + wave; k < end; k += NW) {
