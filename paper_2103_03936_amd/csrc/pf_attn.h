@@ -120,51 +120,47 @@ __device__ __forceinline__ void put4(bf16_t *p, float a, float b, float c, float
 }
 
 // ------------------------------------------------------------------ tiles
-// ROWS rows of DP columns in LDS, loaded by THREADS threads through registers.  The tile is read in two ways: as an operand
-// by rows (16 lanes that a cycle serves have one 16-byte piece of 16 rows) and by columns (the transposing reads: 32 lanes that a
-// cycle serves have four adjacent pieces of four rows).  bf16: without padding, piece c of row r lies at c ^ turn(r); both
-// ways meet each of the 64 banks once.  float: rows padded by 16 bytes.
+// ROWS rows of DP columns in LDS, fetched by THREADS threads straight into it (no registers; a wave's fetches end with
+// fetched()).  A fetch puts the lanes' 16-byte pieces one after the other, so there is no padding: piece c of row r lies at
+// c ^ turn(r).  The tile is read in two ways, as an operand by rows (bf16: 16 lanes that a cycle serves have one piece of 16
+// rows) and by columns (the transposing reads: 32 lanes that a cycle serves have four adjacent pieces of four rows; float:
+// 32 adjacent values of two rows, four apart), and turn() lets each way meet each of the 64 banks once (float of 32
+// columns: twice).
 template <typename T, int DP, int ROWS, int THREADS>
 struct Tile {
-    static constexpr int VEC = 16 / sizeof(T), PIECES = ROWS * DP / VEC, N = (PIECES + THREADS - 1) / THREADS;
-    static constexpr bool TURNED = sizeof(T) == 2;
-    static constexpr int PITCH = TURNED ? (DP == 96 ? 128 : DP) : DP + VEC, CHUNKS = PITCH / VEC;
-    static constexpr int BYTES = ROWS * PITCH * (int)sizeof(T);
-    uint4 r[N];
+    static constexpr int VEC = 16 / sizeof(T), PITCH = DP == 96 ? 128 : DP, CHUNKS = PITCH / VEC, PIECES = ROWS * CHUNKS, N = PIECES / THREADS;
+    static constexpr int BYTES = PIECES * 16, SIZE = ROWS * PITCH;
+    static_assert(PIECES % THREADS == 0, "whole waves of pieces");
     uint32_t at[N]; // bytes from the tile's first row to the thread's pieces
     static __device__ __forceinline__ int turn(int row)
     {
-        if constexpr (!TURNED) return 0;
-        if constexpr (CHUNKS == 16) return (row & 3) << 2 | (row >> 2 & 3);
-        if constexpr (CHUNKS == 8) return (row >> 1 & 1) << 2 | (row >> 2 & 3);
-        return row >> 2 & 3;
+        if constexpr (sizeof(T) == 2) {
+            if constexpr (CHUNKS == 16) return (row & 3) << 2 | (row >> 2 & 3);
+            if constexpr (CHUNKS == 8) return (row >> 1 & 1) << 2 | (row >> 2 & 3);
+            return row >> 2 & 3;
+        }
+        if constexpr (CHUNKS == 8) return row >> 1 & 7;
+        return (row >> 2 & 1) << 3 | (row >> 3 & 1) << 2 | (row & 3);
     }
     // elements `stride` from one row to the next, D columns (the others are zeros)
     __device__ __forceinline__ Tile(i64 stride, int D, int t)
     {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int p = t + i * THREADS, row = p / (DP / VEC), col = p % (DP / VEC) * VEC;
-            const bool in = (PIECES % THREADS == 0 || p < PIECES) && col < D;
-            at[i] = in ? (uint32_t)(row * (int)stride + col) * (uint32_t)sizeof(T) : BUF_OUT;
+            const int p = t + i * THREADS, row = p / CHUNKS, col = ((p % CHUNKS) ^ turn(row)) * VEC;
+            at[i] = col < D ? (uint32_t)(row * (int)stride + col) * (uint32_t)sizeof(T) : BUF_OUT;
         }
     }
-    // ROWS rows from `first` on (the same for all threads), zeros from row `rows` on.  The descriptor ends with the last
-    // row, so that no load needs a branch.
-    __device__ __forceinline__ void load(const T *first, i64 stride, int rows, int D)
+    // ROWS rows from `first` on (the same for all threads), zeros from row `rows` on: the descriptor ends with the last row.
+    // wave: the thread's wave among those of THREADS.
+    __device__ __forceinline__ void fetch(T *lds, const T *first, i64 stride, int rows, int D, int wave) const
     {
+        typedef __attribute__((address_space(3))) void *lds_ptr;
         const int n = rows < ROWS ? rows : ROWS;
         const BufSrc src(first, n > 0 ? ((n - 1) * (int)stride + D) * (int)sizeof(T) : 0);
 #pragma unroll
-        for (int i = 0; i < N; ++i) r[i] = src.load(at[i]);
-    }
-    __device__ __forceinline__ void store(T *lds, int t) const
-    {
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int p = t + i * THREADS, row = p / (DP / VEC), c = p % (DP / VEC);
-            if (PIECES % THREADS == 0 || p < PIECES) *(uint4 *)(lds + row * PITCH + (c ^ turn(row)) * VEC) = r[i];
-        }
+        for (int i = 0; i < N; ++i)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(src.r, (lds_ptr)((char *)lds + (i * THREADS + wave * 64) * 16), 16, (int)at[i], 0, 0, 0);
     }
     // Operand with the index along the rows (the lane's: r0 + lane % 32) and the contraction along columns 16 c ..
     static __device__ __forceinline__ Frag<T> by_rows(const T *lds, int r0, int c, int lane)
@@ -172,10 +168,10 @@ struct Tile {
         const int row = lane & 31, h = lane >> 5;
         const T *const p = lds + (r0 + row) * PITCH;
         Frag<T> f;
-        if constexpr (TURNED) {
+        if constexpr (sizeof(T) == 2) {
             f.v = *(const bf16x8_t *)(p + ((2 * c + h) ^ turn(row)) * VEC);
         } else {
-            const float4 x = *(const float4 *)(p + 16 * c + 4 * h), y = *(const float4 *)(p + 16 * c + 8 + 4 * h);
+            const float4 x = *(const float4 *)(p + ((4 * c + h) ^ turn(row)) * VEC), y = *(const float4 *)(p + ((4 * c + 2 + h) ^ turn(row)) * VEC);
             f.v[0] = x.x, f.v[1] = x.y, f.v[2] = x.z, f.v[3] = x.w, f.v[4] = y.x, f.v[5] = y.y, f.v[6] = y.z, f.v[7] = y.w;
         }
         return f;
@@ -185,7 +181,7 @@ struct Tile {
     static __device__ __forceinline__ Frag<T> by_cols(const T *lds, int r0, int d, int lane)
     {
         Frag<T> f;
-        if constexpr (TURNED) {
+        if constexpr (sizeof(T) == 2) {
             typedef __attribute__((address_space(3))) bf16x4_t *lds_ptr;
             const int g = lane >> 4, i = lane & 15, row = 4 * (g >> 1) + (i >> 2), c = 4 * d + 2 * (g & 1) + (i >> 1 & 1);
             const T *const lo = lds + (r0 + row) * PITCH + (c ^ turn(row)) * VEC + 4 * (i & 1);
@@ -194,13 +190,18 @@ struct Tile {
 #pragma unroll
             for (int e = 0; e < 4; ++e) f.v[e] = x[e], f.v[4 + e] = y[e];
         } else {
-            const T *const p = lds + (r0 + 4 * (lane >> 5)) * PITCH + 32 * d + (lane & 31);
+            const int c = 8 * d + (lane >> 2 & 7);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) f.v[e] = p[e * PITCH], f.v[4 + e] = p[(8 + e) * PITCH];
+            for (int e = 0; e < 8; ++e) {
+                const int row = 4 * (lane >> 5) + (e & 3) + 8 * (e >> 2);
+                f.v[e] = lds[(r0 + row) * PITCH + (c ^ turn(row)) * VEC + (lane & 3)];
+            }
         }
         return f;
     }
 };
+// This wave's fetches have arrived (a barrier after it tells the others)
+__device__ __forceinline__ void fetched() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 // ------------------------------------------------------------------ lengths and positions
 __device__ __forceinline__ int clamped(int x, int lo, int hi) { return x < lo ? lo : x > hi ? hi : x; }

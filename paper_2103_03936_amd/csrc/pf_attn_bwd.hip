@@ -91,21 +91,14 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= (TAB ? 128 : sizeof(T) == 2 
     for (int d = 0; d < DP / 32; ++d) dq[d] = f32x16_t{};
     float before = 0.f, after = 0.f; // sums of dS in blocks that are further than `far` off
 
-    Tl kr(a.ks[1], a.D, t), vr(a.vs[1], a.D, t);
+    const Tl kr(a.ks[1], a.D, t), vr(a.vs[1], a.D, t);
     for (int pass = TAB ? 0 : 1; pass < 2; ++pass) {
-        if (keys > 0) {
-            kr.load(Kp, a.ks[1], n.nk, a.D);
-            vr.load(Vp, a.vs[1], n.nk, a.D);
-        }
         float row = 0.f;
         for (int k0 = 0; k0 < keys; k0 += KT) {
             __syncthreads();
-            kr.store(kt, t);
-            vr.store(vt, t);
-            if (k0 + KT < keys) {
-                kr.load(Kp + (i64)(k0 + KT) * a.ks[1], a.ks[1], n.nk - (k0 + KT), a.D);
-                vr.load(Vp + (i64)(k0 + KT) * a.vs[1], a.vs[1], n.nk - (k0 + KT), a.D);
-            }
+            kr.fetch(kt, Kp + (i64)k0 * a.ks[1], a.ks[1], n.nk - k0, a.D, wave);
+            vr.fetch(vt, Vp + (i64)k0 * a.vs[1], a.vs[1], n.nk - k0, a.D, wave);
+            fetched();
             __syncthreads();
             if (idle || (a.causal && k0 > pmax)) continue;
 #pragma unroll
@@ -275,33 +268,26 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 128 ? 2 : 1) void attn_dkv_k
     if (a.causal) begin = clamped(tile * 128 - n.start, 0, a.Lq) / QT * QT;
     if (tile * 128 >= n.nk) begin = n.nq;
     const i64 qrow = (i64)a.Hq * a.D;
-    Tl qr(a.qs[1], a.D, t), gr(qrow, a.D, t);
+    const Tl qr(a.qs[1], a.D, t), gr(qrow, a.D, t);
     for (int g0 = 0; g0 < a.G; ++g0) {
         const int head = kv * a.G + g0;
         const T *const Qp = (const T *)a.Q + b * a.qs[0] + head * a.qs[2], *const Gp = (const T *)a.dO + ((i64)b * a.Lq * a.Hq + head) * a.D;
         const i64 stat = ((i64)b * a.Hq + head) * a.Lq;
-        if (begin < n.nq) {
-            qr.load(Qp + (i64)(begin) * a.qs[1], a.qs[1], n.nq - (begin), a.D);
-            gr.load(Gp + (i64)(begin) * qrow, qrow, n.nq - (begin), a.D);
-        }
         if (BIAS && begin < n.nq) {
             __syncthreads(); // (the last head's bias is not used any more)
             fill_bias(a, bias, head, t, 256);
         }
         for (int i0 = begin; i0 < n.nq; i0 += QT) {
             __syncthreads();
-            qr.store(qt, t);
-            gr.store(gt, t);
+            qr.fetch(qt, Qp + (i64)i0 * a.qs[1], a.qs[1], n.nq - i0, a.D, wave);
+            gr.fetch(gt, Gp + (i64)i0 * qrow, qrow, n.nq - i0, a.D, wave);
             if (t < QT) {
                 const int i = i0 + t;
                 const float x = i < n.nq ? a.lse_in[stat + i] : -INFINITY;
                 lse_t[t] = x > -INFINITY ? x * LOG2E : INFINITY;
                 delta_t[t] = i < n.nq ? a.delta[stat + i] : 0.f;
             }
-            if (i0 + QT < n.nq) {
-                qr.load(Qp + (i64)(i0 + QT) * a.qs[1], a.qs[1], n.nq - (i0 + QT), a.D);
-                gr.load(Gp + (i64)(i0 + QT) * qrow, qrow, n.nq - (i0 + QT), a.D);
-            }
+            fetched();
             __syncthreads();
             if (j0 >= n.nk) continue;
 #pragma unroll

@@ -10,31 +10,67 @@ namespace pf {
 template <typename T>
 constexpr int KEYS = sizeof(T) == 2 ? 64 : 32; // keys of a tile
 
+// What is scheduled together: per product, reads of LDS and instructions of both vector units (0x100, 0x008, 0x400, 0x002)
+template <int N, int READS, int EXPS, int OPS>
+__device__ __forceinline__ void interleave()
+{
+    if constexpr (N > 0) {
+        __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        if constexpr (EXPS > 0) __builtin_amdgcn_sched_group_barrier(0x400, EXPS, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, OPS, 0);
+        interleave<N - 1, READS, EXPS, OPS>();
+    }
+}
+
+// The scores of a tile of keys, as products: s[u] = keys 32 u .. of `kt` with the wave's queries
+template <typename T, int DP, int SUB, class Tl>
+__device__ __forceinline__ void scores(float (&s)[SUB][16], const T *kt, const Frag<T> (&q)[DP / 16], int lane)
+{
+#pragma unroll
+    for (int u = 0; u < SUB; ++u) {
+        f32x16_t acc = {};
+#pragma unroll
+        for (int c = 0; c < DP / 16; ++c) mma(acc, Tl::by_rows(kt, 32 * u, c, lane), q[c]);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[u][e] = acc[e];
+    }
+}
+
+// One tile of queries.  A turn of the loop has the scores of its keys in registers; their exponentials are worked out while
+// the matrix unit makes the next turn's scores, and the largest of those is found while it multiplies P and V.
 template <typename T, int DP, bool BIAS>
-__global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a)
+__device__ __forceinline__ void attn_fwd_tile(const AttnArgs &a, char *lds, int b, int head, int tile)
 {
     constexpr int KT = KEYS<T>, SUB = KT / 32;
     using Tl = Tile<T, DP, KT, 256>;
-    extern __shared__ __attribute__((aligned(16))) char lds[];
+    T *const kb = (T *)lds, *const vb = kb + 2 * Tl::SIZE; // two tiles of keys, two of values
     float *const bias = (float *)(lds + 4 * Tl::BYTES);
 
-    const unsigned w = xcd_order(blockIdx.x, gridDim.x);
-    const int tile = a.tiles - 1 - (int)(w % a.tiles), bh = w / a.tiles, b = bh / a.Hq, head = bh - b * a.Hq;
     const int t = threadIdx.x, wave = wave_of(t), lane = t & 63, col = lane & 31, h = lane >> 5;
     const AttnLens n(a, b);
     const int i0 = tile * 128 + wave * 32, i = i0 + col; // the lane's query
     const bool ok = i < n.nq;
 
     const T *const Kp = (const T *)a.K + b * a.ks[0] + head / a.G * a.ks[2], *const Vp = (const T *)a.V + b * a.vs[0] + head / a.G * a.vs[2];
-    // keys that some query of the workgroup sees
+    // keys that some query of the workgroup sees, and that some query of the wave sees
     int keys = n.nk;
     if (tile * 128 >= n.nq) keys = 0;
     const int block_last = (tile * 128 + 128 < n.nq ? tile * 128 + 128 : n.nq) - 1 + n.start; // positions
     if (a.causal && block_last + 1 < keys) keys = block_last + 1 < 0 ? 0 : block_last + 1;
     const int last = (i0 + 32 < n.nq ? i0 + 32 : n.nq) - 1, pmin = i0 + n.start, pmax = last + n.start, pos = i + n.start;
-    const bool idle = i0 >= n.nq;
+    int mine = i0 >= n.nq ? 0 : keys;
+    if (a.causal && mine > 0 && pmax + 1 < mine) mine = pmax + 1 < 0 ? 0 : pmax + 1;
 
-    if (BIAS && keys > 0) fill_bias(a, bias, head, t, 256);
+    const Tl kl(a.ks[1], a.D, t), vl(a.vs[1], a.D, t);
+    const auto fetch_keys = [&](int k0) { kl.fetch(kb + (k0 / KT & 1) * Tl::SIZE, Kp + (i64)k0 * a.ks[1], a.ks[1], n.nk - k0, a.D, wave); };
+    const auto fetch_values = [&](int k0) { vl.fetch(vb + (k0 / KT & 1) * Tl::SIZE, Vp + (i64)k0 * a.vs[1], a.vs[1], n.nk - k0, a.D, wave); };
+    if (keys > 0) {
+        fetch_keys(0);
+        fetch_values(0);
+        if (keys > KT) fetch_keys(KT);
+        if constexpr (BIAS) fill_bias(a, bias, head, t, 256);
+    }
     Frag<T> q[DP / 16];
     {
         const T *const Qp = (const T *)a.Q + b * a.qs[0] + head * a.qs[2] + i * a.qs[1];
@@ -46,51 +82,33 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a)
     f32x16_t o[DP / 32];
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d) o[d] = f32x16_t{};
-    float m = -INFINITY, sum = 0.f; // the running maximum (base 2); the sum of the lane's keys
-
-    Tl kr(a.ks[1], a.D, t), vr(a.vs[1], a.D, t);
-    const auto tiles = [&](int k) { return (T *)(lds + (k & 1) * 2 * Tl::BYTES); };
-    if (keys > 0) {
-        kr.load(Kp, a.ks[1], n.nk, a.D);
-        vr.load(Vp, a.vs[1], n.nk, a.D);
-        kr.store(tiles(0), t);
-        vr.store(tiles(0) + KT * Tl::PITCH, t);
+    float m = -INFINITY, sum = 0.f; // the maximum that values are taken relative to (base 2); the sum of the lane's keys
+    float s[SUB][16], top = -INFINITY;
+    fetched();
+    __syncthreads();
+    if (mine > 0) {
+        scores<T, DP, SUB, Tl>(s, kb, q, lane);
+#pragma unroll
+        for (int u = 0; u < SUB; ++u)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) top = fmaxf(top, s[u][e]);
     }
     __syncthreads();
-    for (int k0 = 0, turn = 0; k0 < keys; k0 += KT, ++turn) {
-        const T *const kt = tiles(turn), *const vt = kt + KT * Tl::PITCH;
-        const bool more = k0 + KT < keys;
-        if (more) {
-            kr.load(Kp + (i64)(k0 + KT) * a.ks[1], a.ks[1], n.nk - (k0 + KT), a.D);
-            vr.load(Vp + (i64)(k0 + KT) * a.vs[1], a.vs[1], n.nk - (k0 + KT), a.D);
-        }
-        if (!idle && !(a.causal && k0 > pmax)) {
-            float s[SUB][16];
-            float top = -INFINITY;
+    for (int k0 = 0; k0 < keys; k0 += KT) {
+        if (k0 + 2 * KT < keys) fetch_keys(k0 + 2 * KT);
+        if (k0 + KT < keys) fetch_values(k0 + KT);
+        if (k0 < mine) {
+            const T *const knext = kb + (k0 / KT + 1 & 1) * Tl::SIZE, *const vt = vb + (k0 / KT & 1) * Tl::SIZE;
             const bool edge = k0 + KT > n.nk || (a.causal && k0 + KT - 1 > pmin);
             const bool near = BIAS && k0 + KT - 1 - pmin > -far && k0 - pmax < far;
             const float flat = BIAS ? bias[k0 >= pmin ? 2 * far : 0] : 0.f; // where no key is near
             // Away from the edges and the near keys, nothing is done to a product but one fused multiply-add on its way into
             // the exponential; the maximum is that of the products themselves.
             const bool plain = !edge && !near && sl2 > 0.f;
-            // (the operands of a block of keys are read while the block before it is multiplied)
-            Frag<T> kf[2][DP / 16];
-#pragma unroll
-            for (int c = 0; c < DP / 16; ++c) kf[0][c] = Tl::by_rows(kt, 0, c, lane);
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int u = 0; u < SUB; ++u) {
-                f32x16_t acc = {};
-#pragma unroll
-                for (int c = 0; c < DP / 16; ++c) {
-                    if (u + 1 < SUB) kf[(u + 1) & 1][c] = Tl::by_rows(kt, 32 * (u + 1), c, lane);
-                    mma(acc, kf[u & 1][c], q[c]);
-                }
-#pragma unroll
-                for (int e = 0; e < 16; ++e) s[u][e] = acc[e];
-                __builtin_amdgcn_sched_barrier(0);
-            }
-            if (!plain) {
+            if (plain) {
+                top = top * sl2 + flat;
+            } else {
+                top = -INFINITY;
 #pragma unroll
                 for (int u = 0; u < SUB; ++u)
 #pragma unroll
@@ -98,13 +116,9 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a)
                         const int j = k0 + 32 * u + 8 * (e >> 2) + 4 * h + (e & 3);
                         s[u][e] = s[u][e] * sl2 + (BIAS ? bias[clamped(j - pos, -far, far) + far] : 0.f);
                         if (j >= n.nk || (a.causal && j > pos)) s[u][e] = -INFINITY;
+                        top = fmaxf(top, s[u][e]);
                     }
             }
-#pragma unroll
-            for (int u = 0; u < SUB; ++u)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) top = fmaxf(top, s[u][e]);
-            if (plain) top = top * sl2 + flat;
             top = fmaxf(top, __shfl_xor(top, 32));
             // The maximum that values are taken relative to follows only when it is left by 2^8: sums and rounded P lose
             // nothing to a common factor, and most tiles spare the products their rescaling.
@@ -118,32 +132,57 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a)
                 m = m_new;
             }
             const float base = m == -INFINITY ? 0.f : m, mul = plain ? sl2 : 1.f, add = plain ? flat - base : -base;
-            Frag<T> vf[2][DP / 32];
+            Frag<T> p[2 * SUB];
+            float part[4] = {0.f, 0.f, 0.f, 0.f};
+            const auto exponentials = [&] {
 #pragma unroll
-            for (int d = 0; d < DP / 32; ++d) vf[0][d] = Tl::by_cols(vt, 0, d, lane);
+                for (int c = 0; c < 2 * SUB; ++c) {
 #pragma unroll
-            for (int c = 0; c < 2 * SUB; ++c) { // 16 keys at a time
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    float &x = s[c / 2][8 * (c & 1) + e];
-                    x = exp2_fast(x * mul + add);
-                    sum += x;
+                    for (int e = 0; e < 8; ++e) {
+                        float &x = s[c / 2][8 * (c & 1) + e];
+                        x = exp2_fast(x * mul + add);
+                        part[e & 3] += x;
+                    }
+                    pack(s[c / 2], c & 1, p[c]);
                 }
-                Frag<T> p;
-                pack(s[c / 2], c & 1, p);
-                if (c + 1 < 2 * SUB) {
+            };
+            const auto values = [&] {
 #pragma unroll
-                    for (int d = 0; d < DP / 32; ++d) vf[(c + 1) & 1][d] = Tl::by_cols(vt, 16 * (c + 1), d, lane);
+                for (int c = 0; c < 2 * SUB; ++c)
+#pragma unroll
+                    for (int d = 0; d < DP / 32; ++d) mma(o[d], Tl::by_cols(vt, 16 * c, d, lane), p[c]);
+            };
+            float next[SUB][16];
+            __builtin_amdgcn_sched_barrier(0);
+            if (k0 + KT < mine) {
+                exponentials();
+                scores<T, DP, SUB, Tl>(next, knext, q, lane);
+                if constexpr (sizeof(T) == 2) {
+                    __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);
+                    interleave<SUB * DP / 16, 1, 64 / (DP / 8), 160 / (DP / 8) + 1>();
                 }
-#pragma unroll
-                for (int d = 0; d < DP / 32; ++d) mma(o[d], vf[c & 1][d], p);
                 __builtin_amdgcn_sched_barrier(0);
+                values();
+                top = -INFINITY;
+#pragma unroll
+                for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        top = fmaxf(top, next[u][e]);
+                        s[u][e] = next[u][e];
+                    }
+                if constexpr (sizeof(T) == 2) {
+                    __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+                    interleave<2 * SUB * DP / 32, 2, 0, 2>();
+                }
+            } else {
+                exponentials();
+                values();
             }
+            __builtin_amdgcn_sched_barrier(0);
+            sum += (part[0] + part[1]) + (part[2] + part[3]);
         }
-        if (more) {
-            kr.store(tiles(turn + 1), t);
-            vr.store(tiles(turn + 1) + KT * Tl::PITCH, t);
-        }
+        fetched();
         __syncthreads();
     }
     sum += __shfl_xor(sum, 32);
@@ -162,6 +201,22 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a)
             if (c < a.D) put4(Op + c, v[0], v[1], v[2], v[3]);
         }
     if (a.lse && h == 0) a.lse[((i64)b * a.Hq + head) * a.Lq + i] = some ? (m + __builtin_amdgcn_logf(sum)) * LN2 : -INFINITY;
+}
+
+// paired: a workgroup has a long tile of queries and a short one (causal; a.tiles of them to a head), so that all take the
+// same time
+template <typename T, int DP, bool BIAS>
+__global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void attn_fwd_kernel(AttnArgs a, int paired)
+{
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const unsigned w = xcd_order(blockIdx.x, gridDim.x);
+    const int each = paired ? (a.tiles + 1) / 2 : a.tiles, k = (int)(w % each), bh = w / each, b = bh / a.Hq, head = bh - b * a.Hq;
+    const int other = paired && a.tiles - 1 - k != k ? 2 : 1;
+#pragma unroll 1
+    for (int pass = 0; pass < other; ++pass) {
+        attn_fwd_tile<T, DP, BIAS>(a, lds, b, head, pass ? k : a.tiles - 1 - k);
+        __syncthreads();
+    }
 }
 
 // ------------------------------------------------------------------ host
@@ -229,13 +284,15 @@ template <typename T, int DP>
 static int attn_fwd_launch(const AttnArgs &a, hipStream_t s)
 {
     using Tl = Tile<T, DP, KEYS<T>, 256>;
-    const unsigned blocks = (unsigned)a.B * a.Hq * a.tiles;
+    // two workgroups to a compute unit are resident: causal tiles are paired where there are more
+    const bool paired = a.causal && (i64)a.B * a.Hq * a.tiles > 512;
+    const unsigned blocks = (unsigned)a.B * a.Hq * (paired ? (a.tiles + 1) / 2 : a.tiles);
     const size_t lds = 4 * Tl::BYTES + (a.buckets ? (2 * a.bk.far + 1) * sizeof(float) : 0);
     int st = PF_OK;
     if (a.buckets)
-        PF_LAUNCH_LDS(st, "attn_fwd", (attn_fwd_kernel<T, DP, true>), dim3(blocks), dim3(256), lds, s, a);
+        PF_LAUNCH_LDS(st, "attn_fwd", (attn_fwd_kernel<T, DP, true>), dim3(blocks), dim3(256), lds, s, a, (int)paired);
     else
-        PF_LAUNCH_LDS(st, "attn_fwd", (attn_fwd_kernel<T, DP, false>), dim3(blocks), dim3(256), lds, s, a);
+        PF_LAUNCH_LDS(st, "attn_fwd", (attn_fwd_kernel<T, DP, false>), dim3(blocks), dim3(256), lds, s, a, (int)paired);
     return st;
 }
 

@@ -16,7 +16,7 @@ constexpr int SPLIT_WAVES = sizeof(T) == 2 ? 4 : 2;
 
 template <typename T, int DP>
 struct SplitLds {
-    static constexpr int NW = SPLIT_WAVES<T>, JOIN = DP * 33 * 4, TILES = NW * Tile<T, DP, 32, 64>::BYTES;
+    static constexpr int NW = SPLIT_WAVES<T>, JOIN = DP * 33 * 4, TILES = 2 * NW * Tile<T, DP, 32, 64>::BYTES;
     static constexpr int AREA = JOIN > TILES ? JOIN : TILES;
 };
 
@@ -29,7 +29,7 @@ __global__ __launch_bounds__(64 * SPLIT_WAVES<T>) void attn_split_kernel(AttnArg
     float *const ml = (float *)(lds + SplitLds<T, DP>::AREA); // [2][NW][32]: the waves' maxima and sums
     uint8_t *const lut = (uint8_t *)(ml + 2 * NW * 32);       // bucket of each distance from -far to far
     const int t = threadIdx.x, wave = wave_of(t), lane = t & 63, col = lane & 31, h = lane >> 5;
-    T *const vt = (T *)(lds + wave * Tl::BYTES);
+    T *const vb = (T *)(lds + 2 * wave * Tl::BYTES); // two tiles of this wave's own
 
     const unsigned w = xcd_order(blockIdx.x, gridDim.x);
     const int split = w % a.splits, tile = w / a.splits % a.tiles, bk = w / a.splits / a.tiles, b = bk / a.Hkv, kv = bk - b * a.Hkv;
@@ -65,28 +65,25 @@ __global__ __launch_bounds__(64 * SPLIT_WAVES<T>) void attn_split_kernel(AttnArg
     for (int d = 0; d < DP / 32; ++d) o[d] = f32x16_t{};
     float m = -INFINITY, sum = 0.f;
 
-    Tl vr(a.vs[1], a.D, lane);
+    const Tl vl(a.vs[1], a.D, lane);
     Frag<T> kr[DP / 16];
     const uint32_t kat = (uint32_t)(col * (int)a.ks[1]) * (uint32_t)sizeof(T);
-    const auto fetch = [&](int k) {
+    const auto fetch = [&](int k, int turn) {
         const int rows = n.nk - 32 * k < 32 ? n.nk - 32 * k : 32;
         const BufSrc src(Kp + (i64)(32 * k) * a.ks[1], ((rows - 1) * (int)a.ks[1] + a.D) * (int)sizeof(T));
 #pragma unroll
         for (int c = 0; c < DP / 16; ++c) kr[c] = row_frag_buffer(src, kat, 16 * c, a.D, h, (T *)nullptr);
-        vr.load(Vp + (i64)(32 * k) * a.vs[1], a.vs[1], n.nk - (32 * k), a.D);
+        vl.fetch(vb + turn * Tl::SIZE, Vp + (i64)(32 * k) * a.vs[1], a.vs[1], n.nk - 32 * k, a.D, 0);
     };
-    if (first + wave < end) fetch(first + wave);
-    for (int k = first + wave; k < end; k += NW) {
+    if (first + wave < end) fetch(first + wave, 0);
+    for (int k = first + wave, turn = 0; k < end; k += NW, turn ^= 1) {
         const int k0 = 32 * k;
-        __builtin_amdgcn_wave_barrier();
-        vr.store(vt, lane);
+        const T *const vt = vb + turn * Tl::SIZE;
         f32x16_t acc = {};
+        fetched(); // (K's registers, too)
 #pragma unroll
         for (int c = 0; c < DP / 16; ++c) mma(acc, kr[c], q[c]);
-        if (k + NW < end) fetch(k + NW);
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        if (k + NW < end) fetch(k + NW, turn ^ 1);
         const bool edge = k0 + 32 > n.nk || (a.causal && k0 + 31 > pmin);
         const bool near = BIAS && k0 + 31 - pmin > -far && k0 - pmax < far;
         const float flat = k0 >= pmin ? flat_after : flat_before;
