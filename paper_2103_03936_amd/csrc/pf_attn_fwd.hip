@@ -10,33 +10,6 @@ namespace pf {
 template <typename T>
 constexpr int KEYS = sizeof(T) == 2 ? 64 : 32; // keys of a tile
 
-// What is scheduled together: per product, reads of LDS and instructions of both vector units (0x100, 0x008, 0x400, 0x002)
-template <int N, int READS, int EXPS, int OPS>
-__device__ __forceinline__ void interleave()
-{
-    if constexpr (N > 0) {
-        __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        if constexpr (EXPS > 0) __builtin_amdgcn_sched_group_barrier(0x400, EXPS, 0);
-        __builtin_amdgcn_sched_group_barrier(0x002, OPS, 0);
-        interleave<N - 1, READS, EXPS, OPS>();
-    }
-}
-
-// The scores of a tile of keys, as products: s[u] = keys 32 u .. of `kt` with the wave's queries
-template <typename T, int DP, int SUB, class Tl>
-__device__ __forceinline__ void scores(float (&s)[SUB][16], const T *kt, const Frag<T> (&q)[DP / 16], int lane)
-{
-#pragma unroll
-    for (int u = 0; u < SUB; ++u) {
-        f32x16_t acc = {};
-#pragma unroll
-        for (int c = 0; c < DP / 16; ++c) mma(acc, Tl::by_rows(kt, 32 * u, c, lane), q[c]);
-#pragma unroll
-        for (int e = 0; e < 16; ++e) s[u][e] = acc[e];
-    }
-}
-
 // One tile of queries.  A turn of the loop has the scores of its keys in registers; their exponentials are worked out while
 // the matrix unit makes the next turn's scores, and the largest of those is found while it multiplies P and V.
 template <typename T, int DP, bool BIAS>
@@ -87,7 +60,14 @@ __device__ __forceinline__ void attn_fwd_tile(const AttnArgs &a, char *lds, int 
     fetched();
     __syncthreads();
     if (mine > 0) {
-        scores<T, DP, SUB, Tl>(s, kb, q, lane);
+#pragma unroll
+        for (int u = 0; u < SUB; ++u) {
+            f32x16_t acc = {};
+#pragma unroll
+            for (int c = 0; c < DP / 16; ++c) mma(acc, Tl::by_rows(kb, 32 * u, c, lane), q[c]);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[u][e] = acc[e];
+        }
 #pragma unroll
         for (int u = 0; u < SUB; ++u)
 #pragma unroll
@@ -132,54 +112,47 @@ __device__ __forceinline__ void attn_fwd_tile(const AttnArgs &a, char *lds, int 
                 m = m_new;
             }
             const float base = m == -INFINITY ? 0.f : m, mul = plain ? sl2 : 1.f, add = plain ? flat - base : -base;
-            Frag<T> p[2 * SUB];
+            // The order of what follows is fixed step by step: a step is one product of each kind, the read of the operand of the
+            // product AHEAD steps on, and a share of the vector instructions.
+            constexpr int CH = DP / 16, SC = SUB * CH, DB = DP / 32, PV = 2 * SUB * DB;
+            constexpr int AHEAD = 3;
+            Frag<T> p[2 * SUB], ring[AHEAD + 1];
             float part[4] = {0.f, 0.f, 0.f, 0.f};
-            const auto exponentials = [&] {
+            f32x16_t next[SUB];
 #pragma unroll
-                for (int c = 0; c < 2 * SUB; ++c) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        float &x = s[c / 2][8 * (c & 1) + e];
-                        x = exp2_fast(x * mul + add);
-                        part[e & 3] += x;
-                    }
-                    pack(s[c / 2], c & 1, p[c]);
-                }
-            };
-            const auto values = [&] {
-#pragma unroll
-                for (int c = 0; c < 2 * SUB; ++c)
-#pragma unroll
-                    for (int d = 0; d < DP / 32; ++d) mma(o[d], Tl::by_cols(vt, 16 * c, d, lane), p[c]);
-            };
-            float next[SUB][16];
+            for (int u = 0; u < SUB; ++u) next[u] = f32x16_t{};
             __builtin_amdgcn_sched_barrier(0);
-            if (k0 + KT < mine) {
-                exponentials();
-                scores<T, DP, SUB, Tl>(next, knext, q, lane);
-                if constexpr (sizeof(T) == 2) {
-                    __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);
-                    interleave<SUB * DP / 16, 1, 64 / (DP / 8), 160 / (DP / 8) + 1>();
+            // the next keys' scores (of whatever lies there, after the last) beside this tile's exponentials
+#pragma unroll
+            for (int x = 0; x < AHEAD; ++x) ring[x] = Tl::by_rows(knext, 32 * (x / CH), x % CH, lane);
+#pragma unroll
+            for (int x = 0; x < SC; ++x) {
+                if (x + AHEAD < SC) ring[(x + AHEAD) % (AHEAD + 1)] = Tl::by_rows(knext, 32 * ((x + AHEAD) / CH), (x + AHEAD) % CH, lane);
+                mma(next[x / CH], ring[x % (AHEAD + 1)], q[x % CH]);
+#pragma unroll
+                for (int y = x * (16 * SUB) / SC; y < (x + 1) * (16 * SUB) / SC; ++y) {
+                    float &z = s[y / 16][y % 16];
+                    z = exp2_fast(z * mul + add);
+                    part[y & 3] += z;
+                    if (y % 8 == 7) pack(s[y / 16], y % 16 / 8, p[y / 8]);
                 }
                 __builtin_amdgcn_sched_barrier(0);
-                values();
-                top = -INFINITY;
-#pragma unroll
-                for (int u = 0; u < SUB; ++u)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        top = fmaxf(top, next[u][e]);
-                        s[u][e] = next[u][e];
-                    }
-                if constexpr (sizeof(T) == 2) {
-                    __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
-                    interleave<2 * SUB * DP / 32, 2, 0, 2>();
-                }
-            } else {
-                exponentials();
-                values();
             }
-            __builtin_amdgcn_sched_barrier(0);
+            // P and V beside the largest of the next scores
+            top = -INFINITY;
+#pragma unroll
+            for (int x = 0; x < AHEAD; ++x) ring[x] = Tl::by_cols(vt, 16 * (x / DB), x % DB, lane);
+#pragma unroll
+            for (int x = 0; x < PV; ++x) {
+                if (x + AHEAD < PV) ring[(x + AHEAD) % (AHEAD + 1)] = Tl::by_cols(vt, 16 * ((x + AHEAD) / DB), (x + AHEAD) % DB, lane);
+                mma(o[x % DB], ring[x % (AHEAD + 1)], p[x / DB]);
+#pragma unroll
+                for (int y = x * (16 * SUB) / PV; y < (x + 1) * (16 * SUB) / PV; ++y) {
+                    s[y / 16][y % 16] = next[y / 16][y % 16];
+                    top = fmaxf(top, s[y / 16][y % 16]);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
             sum += (part[0] + part[1]) + (part[2] + part[3]);
         }
         fetched();
