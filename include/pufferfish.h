@@ -539,7 +539,8 @@ int pf_qk_norm_rotate_bwd(const pf_qk_norm_desc *d, const void *Q, const void *K
 /* for n >= e, with the borders where exact arithmetic has them.         */
 /* Limits (PF_ERR_UNSUPPORTED): head_dim a multiple of 8, 8 .. 128;       */
 /* buckets 0 or 2 .. 256, with bidirectional a multiple of 2 and >= 4;    */
-/* max_distance > e and <= 1024; Lq, Lk < 2^30; B heads_q < 2^31.         */
+/* max_distance > e and <= 1024; Lq, Lk < 2^29; fewer than 2^31 blocks of  */
+/* 32 rows; less than 2^22 elements from one token to the next.           */
 /* Lq == 0 or Lk == 0 is legal.                                           */
 /* Sums are the same bits in every call of the same sizes.                */
 /* ------------------------------------------------------------------ */

@@ -128,9 +128,9 @@ __device__ __forceinline__ void put4(bf16_t *p, float a, float b, float c, float
 // columns: twice).
 template <typename T, int DP, int ROWS, int THREADS>
 struct Tile {
-    static constexpr int VEC = 16 / sizeof(T), PITCH = DP == 96 ? 128 : DP, CHUNKS = PITCH / VEC, PIECES = ROWS * CHUNKS, N = PIECES / THREADS;
+    static constexpr int VEC = 16 / sizeof(T), PITCH = DP == 96 ? 128 : DP, CHUNKS = PITCH / VEC, PIECES = ROWS * CHUNKS, N = (PIECES + THREADS - 1) / THREADS;
     static constexpr int BYTES = PIECES * 16, SIZE = ROWS * PITCH;
-    static_assert(PIECES % THREADS == 0, "whole waves of pieces");
+    static_assert(PIECES % 64 == 0, "whole waves of pieces");
     uint32_t at[N]; // bytes from the tile's first row to the thread's pieces
     static __device__ __forceinline__ int turn(int row)
     {
@@ -160,7 +160,8 @@ struct Tile {
         const BufSrc src(first, n > 0 ? ((n - 1) * (int)stride + D) * (int)sizeof(T) : 0);
 #pragma unroll
         for (int i = 0; i < N; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(src.r, (lds_ptr)((char *)lds + (i * THREADS + wave * 64) * 16), 16, (int)at[i], 0, 0, 0);
+            if (PIECES % THREADS == 0 || i * THREADS + wave * 64 < PIECES)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(src.r, (lds_ptr)((char *)lds + (i * THREADS + wave * 64) * 16), 16, (int)at[i], 0, 0, 0);
     }
     // Operand with the index along the rows (the lane's: r0 + lane % 32) and the contraction along columns 16 c ..
     static __device__ __forceinline__ Frag<T> by_rows(const T *lds, int r0, int c, int lane)

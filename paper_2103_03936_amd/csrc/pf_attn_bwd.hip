@@ -5,46 +5,50 @@
 // distance; the second has keys in its columns and makes dK and dV, going through the query heads of a key head.  They form S
 // and dP each (seven products where one kernel with atomic sums of dQ would have five).
 //
-// delta = sum P dP of a row is sum O dO, too, but O is rounded to bf16 there and P was before O was formed: dS is off by
+// delta = sum P dP of a row is sum O dO, too, but O is rounded to bf16 there and P was before O was formed: dS is off by about
 // 2^-9 of delta then, which is below what rounding dS itself costs dQ and dK, but not good enough for dtable, a float32 sum over
-// all pairs in which the rows' errors would stay.  With a table gradient the first kernel therefore goes over its keys twice, for
-// delta in float32 first.
+// all pairs in which the rows' errors would stay.  What delta is off by is the sum of the row's dS, so that it is known once the
+// row is through.
 #include "pf_attn.h"
 #include "pf_gemm.h"
 
 namespace pf {
 
-template <typename T>
-constexpr int BWD_KEYS = sizeof(T) == 2 ? 64 : 32; // keys (queries) of a tile
-
-constexpr int DIAG = 33; // floats from one row of a 32 x 32 block of dS to the next in LDS
+// A 32 x 32 block of dS in LDS, value (r, c) in row r at c - r + 31, so that a column holds a diagonal.  What no value is written
+// to is zero from the start and stays so.
+constexpr int DIAG = 32 * 64;
 
 template <typename T, int DP>
 struct BwdLds {
-    using Tl = Tile<T, DP, BWD_KEYS<T>, 256>;
+    using Tq = Tile<T, DP, 32, 256>;
     static size_t dq(int far, bool bias, bool tab)
     {
-        return 2 * Tl::BYTES + (bias ? (2 * far + 1) * 4 : 0) + (tab ? 4 * 32 * DIAG * 4 + 4 * (2 * far + 1) * 4 : 0);
+        return 5 * Tq::BYTES + (bias ? (2 * far + 1) * 4 : 0) + (tab ? 4 * DIAG * 4 + 4 * (2 * far + 1) * 4 : 0);
     }
-    static size_t dkv(int far, bool bias) { return 2 * Tl::BYTES + 2 * BWD_KEYS<T> * 4 + (bias ? (2 * far + 1) * 4 : 0); }
+    static size_t dkv(int far, bool bias) { return 6 * Tq::BYTES + 3 * 2 * 32 * 4 + (bias ? (2 * far + 1) * 4 : 0); }
 };
 
-// dQ, delta and the sums of dS by distance; a workgroup has 128 queries of one head.  TAB: with the gradient of the table
+// dQ, delta and the sums of dS by distance, for one tile of 128 queries of one head.  TAB: with the gradient of the table.
+//
+// A turn of the loop has S and dP of 32 keys in registers.  It works out dS while the matrix unit makes S and dP of the next 32,
+// then adds dS K to dQ.  Three groups of keys and two of values are in LDS: those whose columns dQ needs, those whose rows S and dP
+// need, and the keys on their way; a turn needs one barrier.
+//
+// With the table's gradient there are two passes.  The first takes delta from O; in the far blocks, where one bucket holds all
+// distances, it keeps the sums of dS and of P of each row, and it sums all dS of a row: that sum is what delta is off by. The
+// second pass goes over the near blocks alone, with the delta that is now exact; the far sums are put right by their sums of P.
 template <typename T, int DP, bool BIAS, bool TAB>
-__global__ __launch_bounds__(256, DP * sizeof(T) <= (TAB ? 128 : sizeof(T) == 2 ? 256 : 320) ? 2 : 1) void attn_dq_kernel(AttnArgs a)
+__device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b, int head, int tile)
 {
-    constexpr int KT = BWD_KEYS<T>, SUB = KT / 32;
-    using Tl = Tile<T, DP, KT, 256>;
-    extern __shared__ __attribute__((aligned(16))) char lds[];
+    using Tl = Tile<T, DP, 32, 256>;
+    constexpr int CH = DP / 16, DB = DP / 32, AHEAD = 3;
     const int far = a.bk.far, span = 2 * far + 1;
-    T *const kt = (T *)lds, *const vt = (T *)(lds + Tl::BYTES);
-    float *const bias = (float *)(lds + 2 * Tl::BYTES);
-    float *const diag_all = bias + span, *const sums_all = diag_all + 4 * 32 * DIAG; // [4][32][DIAG], [4][span]
+    T *const kb = (T *)lds, *const vb = kb + 3 * Tl::SIZE;
+    float *const bias = (float *)(lds + 5 * Tl::BYTES);
+    float *const diag_all = bias + span, *const sums_all = diag_all + 4 * DIAG; // a wave's block, a wave's [span]
 
-    const unsigned w = xcd_order(blockIdx.x, gridDim.x);
-    const int tile = a.tiles - 1 - (int)(w % a.tiles), bh = w / a.tiles, b = bh / a.Hq, head = bh - b * a.Hq;
     const int t = threadIdx.x, wave = wave_of(t), lane = t & 63, col = lane & 31, h = lane >> 5;
-    float *const diag = diag_all + wave * 32 * DIAG, *const sums = sums_all + wave * span;
+    float *const diag = diag_all + wave * DIAG, *const sums = sums_all + wave * span;
     const AttnLens n(a, b);
     const int i0 = tile * 128 + wave * 32, i = i0 + col;
     const bool ok = i < n.nq;
@@ -54,20 +58,26 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= (TAB ? 128 : sizeof(T) == 2 
     const int block_last = (tile * 128 + 128 < n.nq ? tile * 128 + 128 : n.nq) - 1 + n.start;
     if (a.causal && block_last + 1 < keys) keys = block_last + 1 < 0 ? 0 : block_last + 1;
     const int last = (i0 + 32 < n.nq ? i0 + 32 : n.nq) - 1, pmin = i0 + n.start, pmax = last + n.start, pos = i + n.start;
-    const bool idle = i0 >= n.nq;
+    int mine = i0 >= n.nq ? 0 : keys; // of the keys, those that the wave's queries see
+    if (a.causal && mine > 0 && pmax + 1 < mine) mine = pmax + 1 < 0 ? 0 : pmax + 1;
 
     if (BIAS && keys > 0) fill_bias(a, bias, head, t, 256);
     if constexpr (TAB)
-        for (int x = t; x < 4 * span; x += 256) sums_all[x] = 0.f;
+        for (int x = t; x < 4 * (DIAG + span); x += 256) diag_all[x] = 0.f;
     const i64 at = (((i64)b * a.Lq + i) * a.Hq + head) * a.D, stat = ((i64)b * a.Hq + head) * a.Lq + i;
-    Frag<T> q[DP / 16], g[DP / 16];
+    Frag<T> q[CH], g[CH];
+    float delta = 0.f;
     {
-        const T *const Qp = (const T *)a.Q + b * a.qs[0] + head * a.qs[2] + i * a.qs[1], *const Gp = (const T *)a.dO + at;
+        const T *const Qp = (const T *)a.Q + b * a.qs[0] + head * a.qs[2] + i * a.qs[1];
 #pragma unroll
-        for (int c = 0; c < DP / 16; ++c) {
+        for (int c = 0; c < CH; ++c) {
             q[c] = row_frag_global(Qp, 16 * c, a.D, h, ok);
-            g[c] = row_frag_global(Gp, 16 * c, a.D, h, ok);
+            g[c] = row_frag_global((const T *)a.dO + at, 16 * c, a.D, h, ok);
+            const Frag<T> x = row_frag_global((const T *)a.Oin + at, 16 * c, a.D, h, ok);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) delta += (float)x.v[e] * (float)g[c].v[e];
         }
+        delta += __shfl_xor(delta, 32);
     }
     // exp2(S - lse) is 0 for a query that takes no part
     float lse2 = INFINITY;
@@ -75,120 +85,155 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= (TAB ? 128 : sizeof(T) == 2 
         const float x = a.lse_in[stat];
         if (x > -INFINITY) lse2 = x * LOG2E;
     }
-    float delta = 0.f;
-    if constexpr (!TAB) {
-#pragma unroll
-        for (int c = 0; c < DP / 16; ++c) {
-            const Frag<T> x = row_frag_global((const T *)a.Oin + at, 16 * c, a.D, h, ok);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) delta += (float)x.v[e] * (float)g[c].v[e];
-        }
-        delta += __shfl_xor(delta, 32);
-    }
     const float sl2 = a.scale * LOG2E;
-    f32x16_t dq[DP / 32];
+    f32x16_t dq[DB];
 #pragma unroll
-    for (int d = 0; d < DP / 32; ++d) dq[d] = f32x16_t{};
-    float before = 0.f, after = 0.f; // sums of dS in blocks that are further than `far` off
+    for (int d = 0; d < DB; ++d) dq[d] = f32x16_t{};
+    float before = 0.f, after = 0.f, before_p = 0.f, after_p = 0.f, off = 0.f; // far sums of dS and P; the sum of all dS
 
-    const Tl kr(a.ks[1], a.D, t), vr(a.vs[1], a.D, t);
-    for (int pass = TAB ? 0 : 1; pass < 2; ++pass) {
-        float row = 0.f;
-        for (int k0 = 0; k0 < keys; k0 += KT) {
-            __syncthreads();
-            kr.fetch(kt, Kp + (i64)k0 * a.ks[1], a.ks[1], n.nk - k0, a.D, wave);
-            vr.fetch(vt, Vp + (i64)k0 * a.vs[1], a.vs[1], n.nk - k0, a.D, wave);
+    const Tl kl(a.ks[1], a.D, t), vl(a.vs[1], a.D, t);
+    const auto near_at = [&](int k0, int lo, int hi) { return BIAS && k0 + 31 - lo > -far && k0 - hi < far; };
+    for (int pass = 0; pass < (TAB ? 2 : 1); ++pass) {
+        // the groups of 32 keys that the workgroup goes through
+        int begin = 0, end = (keys + 31) / 32;
+        if (TAB && pass == 1 && keys > 0) { // (32 begin + 31 > first position - far; 32 (end - 1) < last position + far)
+            const int lo = tile * 128 + n.start - far - 31, hi = block_last + far;
+            if (lo >= 0) begin = lo / 32 + 1;
+            if (hi <= 0) end = 0;
+            else if ((hi + 31) / 32 < end) end = (hi + 31) / 32;
+        }
+        if (begin < end) {
+            kl.fetch(kb + begin % 3 * Tl::SIZE, Kp + (i64)(32 * begin) * a.ks[1], a.ks[1], n.nk - 32 * begin, a.D, wave);
+            vl.fetch(vb + (begin & 1) * Tl::SIZE, Vp + (i64)(32 * begin) * a.vs[1], a.vs[1], n.nk - 32 * begin, a.D, wave);
             fetched();
             __syncthreads();
-            if (idle || (a.causal && k0 > pmax)) continue;
+        }
+        float s[16];
+        f32x16_t dp = {};
 #pragma unroll
-            for (int u = 0; u < SUB; ++u) {
-                const int ks = k0 + 32 * u;
-                const bool edge = ks + 32 > n.nk || (a.causal && ks + 31 > pmin);
-                const bool near = BIAS && ks + 31 - pmin > -far && ks - pmax < far;
-                const float flat = BIAS ? bias[ks >= pmin ? 2 * far : 0] : 0.f;
-                f32x16_t s = {}, dp = {};
-                #pragma unroll
-                for (int c = 0; c < DP / 16; ++c) {
-                    mma(s, Tl::by_rows(kt, 32 * u, c, lane), q[c]);
-                    mma(dp, Tl::by_rows(vt, 32 * u, c, lane), g[c]);
-                }
-                float ds[16];
-                const float base = flat - lse2;
-#pragma unroll
-                for (int e = 0; e < 16; ++e) ds[e] = s[e];
-                if (edge || near) {
+        for (int e = 0; e < 16; ++e) s[e] = 0.f;
+        int slot = (begin + 2) % 3; // of group j
+        for (int j = begin - 1; j < end; ++j) {
+            const int s1 = slot == 2 ? 0 : slot + 1, s2 = slot == 0 ? 2 : slot - 1; // of groups j + 1, j + 2
+            const int k0 = 32 * j;
+            if (j + 2 < end) {
+                kl.fetch(kb + s2 * Tl::SIZE, Kp + (i64)(k0 + 64) * a.ks[1], a.ks[1], n.nk - k0 - 64, a.D, wave);
+                vl.fetch(vb + (j & 1) * Tl::SIZE, Vp + (i64)(k0 + 64) * a.vs[1], a.vs[1], n.nk - k0 - 64, a.D, wave);
+            }
+            const bool near = near_at(k0, pmin, pmax), there = !TAB || pass == 0;
+            const bool now = j >= begin && k0 < mine && (there || near), then = k0 + 32 < mine && (there || near_at(k0 + 32, pmin, pmax));
+            if (now || then) {
+                const T *const krow = kb + s1 * Tl::SIZE, *const vrow = vb + ((j + 1) & 1) * Tl::SIZE, *const kcol = kb + slot * Tl::SIZE;
+                const bool edge = k0 + 32 > n.nk || (a.causal && k0 + 31 > pmin), plain = !edge && !near;
+                const float flat = BIAS ? bias[k0 >= pmin ? 2 * far : 0] : 0.f;
+                if (now && !plain) {
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
-                        const int j = ks + 8 * (e >> 2) + 4 * h + (e & 3);
-                        ds[e] = exp2_fast(ds[e] * sl2 + ((BIAS ? bias[clamped(j - pos, -far, far) + far] : 0.f) - lse2));
-                        if (j >= n.nk || (a.causal && j > pos)) ds[e] = 0.f;
-                    }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) ds[e] = exp2_fast(ds[e] * sl2 + base);
-                }
-#pragma unroll
-                for (int e = 0; e < 16; ++e) { // (first pass: delta is 0, and the sum of these is delta)
-                    ds[e] *= dp[e] - delta;
-                    if (TAB && pass == 0) row += ds[e];
-                }
-                if (TAB && pass == 0) continue;
-                if constexpr (TAB) {
-                    if (near) {
-                        // along the diagonals of the block: lane x has the distance x - 31 from that of its corner
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) diag[(8 * (e >> 2) + 4 * h + (e & 3)) * DIAG + col] = ds[e];
-                        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-                        __builtin_amdgcn_wave_barrier();
-                        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-                        float y = 0.f;
-#pragma unroll
-                        for (int c = 0; c < 32; ++c) {
-                            const int r = c + lane - 31;
-                            const float v = diag[clamped(r, 0, 31) * DIAG + c];
-                            y += r >= 0 && r < 32 ? v : 0.f;
-                        }
-                        const int dist = ks - pmin + lane - 31;
-                        // distances beyond far share their sum's place: one lane after the other would be needed, so those go to
-                        // the lanes' own sums
-                        if (lane < 63) {
-                            if (dist <= -far)
-                                before += y;
-                            else if (dist >= far)
-                                after += y;
-                            else
-                                sums[dist + far] += y;
-                        }
-                        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-                        __builtin_amdgcn_wave_barrier();
-                        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-                    } else {
-                        float y = 0.f;
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) y += ds[e];
-                        if (ks >= pmin)
-                            after += y;
-                        else
-                            before += y;
+                        const int x = k0 + 8 * (e >> 2) + 4 * h + (e & 3);
+                        s[e] = s[e] * sl2 + ((BIAS ? bias[clamped(x - pos, -far, far) + far] : 0.f) - lse2);
+                        if (x >= n.nk || (a.causal && x > pos)) s[e] = -INFINITY;
                     }
                 }
+                const float mul = plain ? sl2 : 1.f, add = plain ? flat - lse2 : 0.f;
+                f32x16_t next = {}, dnext = {};
+                Frag<T> ring[AHEAD + 1], f[2];
+                float sum = 0.f, sum_p = 0.f;
+                __builtin_amdgcn_sched_barrier(0);
+                // S and dP of the next keys (step 2 c: S, columns 16 c ..; 2 c + 1: dP) beside dS of these
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    Frag<T> p;
-                    pack(ds, c, p);
+                for (int x = 0; x < AHEAD; ++x) ring[x] = Tl::by_rows(x & 1 ? vrow : krow, 0, x / 2, lane);
 #pragma unroll
-                    for (int d = 0; d < DP / 32; ++d) mma(dq[d], Tl::by_cols(kt, 32 * u + 16 * c, d, lane), p);
+                for (int x = 0; x < 2 * CH; ++x) {
+                    if (x + AHEAD < 2 * CH) ring[(x + AHEAD) % (AHEAD + 1)] = Tl::by_rows((x + AHEAD) & 1 ? vrow : krow, 0, (x + AHEAD) / 2, lane);
+                    if (x & 1)
+                        mma(dnext, ring[x % (AHEAD + 1)], g[x / 2]);
+                    else
+                        mma(next, ring[x % (AHEAD + 1)], q[x / 2]);
+#pragma unroll
+                    for (int e = x * 16 / (2 * CH); e < (x + 1) * 16 / (2 * CH); ++e) {
+                        const float p = exp2_fast(s[e] * mul + add);
+                        s[e] = p * (dp[e] - delta);
+                        if constexpr (TAB) {
+                            sum += s[e];
+                            sum_p += p;
+                        }
+                        if (e % 8 == 7) pack(s, e / 8, f[e / 8]);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
                 }
+                if (now) {
+                    bool add_dq = true;
+                    if constexpr (TAB) {
+                        if (pass == 0) {
+                            off += sum;
+                            add_dq = !near;
+                            if (!near) {
+                                if (k0 >= pmin) {
+                                    after += sum;
+                                    after_p += sum_p;
+                                } else {
+                                    before += sum;
+                                    before_p += sum_p;
+                                }
+                            }
+                        } else {
+                            // along the diagonals of the block: lane x has the distance x - 31 from that of its corner
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) diag[(8 * (e >> 2) + 4 * h + (e & 3)) * 63 + col + 31] = s[e];
+                            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+                            __builtin_amdgcn_wave_barrier();
+                            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+                            float y = 0.f;
+#pragma unroll
+                            for (int r = 0; r < 32; ++r) y += diag[r * 64 + lane];
+                            // (distances from far on have one place, several lanes' sums go there: by way of the lanes' own)
+                            const int dist = k0 - pmin + 31 - lane;
+                            if (lane < 63) {
+                                if (dist <= -far)
+                                    before += y;
+                                else if (dist >= far)
+                                    after += y;
+                                else
+                                    sums[dist + far] += y;
+                            }
+                            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+                            __builtin_amdgcn_wave_barrier();
+                            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+                        }
+                    }
+                    if (add_dq) {
+                        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                        for (int x = 0; x < AHEAD; ++x) ring[x] = Tl::by_cols(kcol, 16 * (x / DB), x % DB, lane);
+#pragma unroll
+                        for (int x = 0; x < 2 * DB; ++x) {
+                            if (x + AHEAD < 2 * DB) ring[(x + AHEAD) % (AHEAD + 1)] = Tl::by_cols(kcol, 16 * ((x + AHEAD) / DB), (x + AHEAD) % DB, lane);
+                            mma(dq[x % DB], ring[x % (AHEAD + 1)], f[x / DB]);
+                            __builtin_amdgcn_sched_barrier(0);
+                        }
+                    }
+                }
+                dp = dnext;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[e] = next[e];
+            }
+            slot = s1;
+            fetched();
+            __syncthreads();
+        }
+        if constexpr (TAB) {
+            if (pass == 0) {
+                off += __shfl_xor(off, 32);
+                delta += off;
+                before -= off * before_p;
+                after -= off * after_p;
             }
         }
-        if (TAB && pass == 0) delta = row + __shfl_xor(row, 32);
-        __syncthreads(); // (the tiles are free for the next pass)
     }
     if (i < a.Lq) {
         T *const out = (T *)a.dQ + at;
 #pragma unroll
-        for (int d = 0; d < DP / 32; ++d)
+        for (int d = 0; d < DB; ++d)
 #pragma unroll
             for (int e = 0; e < 16; e += 4) {
                 const int c = 32 * d + 8 * (e >> 2) + 4 * h;
@@ -204,6 +249,7 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= (TAB ? 128 : sizeof(T) == 2 
             before += __shfl_xor(before, o);
             after += __shfl_xor(after, o);
         }
+        __syncthreads();
         if (lane == 0) {
             sums[0] += before;
             sums[2 * far] += after;
@@ -233,120 +279,176 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= (TAB ? 128 : sizeof(T) == 2 
     }
 }
 
-// dK and dV: a workgroup has 128 keys of one key head, a wave 32 of them
-template <typename T, int DP, bool BIAS>
-__global__ __launch_bounds__(256, DP * sizeof(T) <= 128 ? 2 : 1) void attn_dkv_kernel(AttnArgs a)
+// paired: a long tile of queries and a short one to a workgroup, as forward
+template <typename T, int DP, bool BIAS, bool TAB>
+__global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void attn_dq_kernel(AttnArgs a, int paired)
 {
-    constexpr int QT = BWD_KEYS<T>, SUB = QT / 32;
-    using Tl = Tile<T, DP, QT, 256>;
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    T *const qt = (T *)lds, *const gt = (T *)(lds + Tl::BYTES);
-    float *const lse_t = (float *)(lds + 2 * Tl::BYTES), *const delta_t = lse_t + QT, *const bias = delta_t + QT;
+    const unsigned w = xcd_order(blockIdx.x, gridDim.x);
+    const int each = paired ? (a.tiles + 1) / 2 : a.tiles, k = (int)(w % each), bh = w / each, b = bh / a.Hq, head = bh - b * a.Hq;
+    const int count = paired && a.tiles - 1 - k != k ? 2 : 1;
+#pragma unroll 1
+    for (int x = 0; x < count; ++x) {
+        attn_dq_tile<T, DP, BIAS, TAB>(a, lds, b, head, x ? k : a.tiles - 1 - k);
+        __syncthreads();
+    }
+}
+
+// dK and dV: a workgroup has 64 keys of one key head, a wave 32 of them in its columns; the query heads of the key head one
+// after the other, each 32 queries at a time.  As above, dS and P of 32 queries are worked out while S and dP of the next 32
+// are made; two waves to a workgroup, so that there are workgroups enough to even out what causal masks leave them.
+template <typename T, int DP, bool BIAS>
+__global__ __launch_bounds__(128, DP * sizeof(T) <= 128 ? 2 : 1) void attn_dkv_kernel(AttnArgs a)
+{
+    using Tl = Tile<T, DP, 32, 128>;
+    constexpr int CH = DP / 16, DB = DP / 32, AHEAD = 3;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    T *const qb = (T *)lds, *const gb = qb + 3 * Tl::SIZE;
+    float *const stats = (float *)(lds + 6 * Tl::BYTES); // [3][2][32]: lse (base 2) and delta
+    float *const bias = stats + 3 * 64;
 
     const unsigned w = xcd_order(blockIdx.x, gridDim.x);
     const int tile = (int)(w % a.tiles), bk = w / a.tiles, b = bk / a.Hkv, kv = bk - b * a.Hkv;
     const int t = threadIdx.x, wave = wave_of(t), lane = t & 63, col = lane & 31, h = lane >> 5;
     const AttnLens n(a, b);
-    const int far = a.bk.far, j0 = tile * 128 + wave * 32, j = j0 + col;
+    const int far = a.bk.far, j0 = tile * 64 + wave * 32, j = j0 + col;
     const bool ok = j < n.nk;
-    Frag<T> k[DP / 16], v[DP / 16];
+    Frag<T> k[CH], v[CH];
     {
         const T *const Kp = (const T *)a.K + b * a.ks[0] + kv * a.ks[2] + j * a.ks[1], *const Vp = (const T *)a.V + b * a.vs[0] + kv * a.vs[2] + j * a.vs[1];
 #pragma unroll
-        for (int c = 0; c < DP / 16; ++c) {
+        for (int c = 0; c < CH; ++c) {
             k[c] = row_frag_global(Kp, 16 * c, a.D, h, ok);
             v[c] = row_frag_global(Vp, 16 * c, a.D, h, ok);
         }
     }
     const float sl2 = a.scale * LOG2E;
-    f32x16_t dk[DP / 32], dv[DP / 32];
+    f32x16_t dk[DB], dv[DB];
 #pragma unroll
-    for (int d = 0; d < DP / 32; ++d) dk[d] = dv[d] = f32x16_t{};
+    for (int d = 0; d < DB; ++d) dk[d] = dv[d] = f32x16_t{};
 
-    // the first query that sees a key of the workgroup
-    int begin = 0;
-    if (a.causal) begin = clamped(tile * 128 - n.start, 0, a.Lq) / QT * QT;
-    if (tile * 128 >= n.nk) begin = n.nq;
-    const i64 qrow = (i64)a.Hq * a.D;
-    const Tl qr(a.qs[1], a.D, t), gr(qrow, a.D, t);
-    for (int g0 = 0; g0 < a.G; ++g0) {
+    const i64 grow = (i64)a.Hq * a.D;
+    const Tl ql(a.qs[1], a.D, t), gl(grow, a.D, t);
+    // the groups of 32 queries that see a key of the workgroup, and of the wave
+    int begin = 0, end = (n.nq + 31) / 32, mine = 0;
+    if (a.causal) {
+        begin = clamped(tile * 64 - n.start, 0, a.Lq) / 32;
+        mine = clamped(j0 - n.start, 0, a.Lq) / 32;
+    }
+    if (tile * 64 >= n.nk) begin = end;
+    if (j0 >= n.nk) mine = end;
+    for (int g0 = 0; g0 < a.G && begin < end; ++g0) {
         const int head = kv * a.G + g0;
         const T *const Qp = (const T *)a.Q + b * a.qs[0] + head * a.qs[2], *const Gp = (const T *)a.dO + ((i64)b * a.Lq * a.Hq + head) * a.D;
         const i64 stat = ((i64)b * a.Hq + head) * a.Lq;
-        if (BIAS && begin < n.nq) {
-            __syncthreads(); // (the last head's bias is not used any more)
-            fill_bias(a, bias, head, t, 256);
-        }
-        for (int i0 = begin; i0 < n.nq; i0 += QT) {
-            __syncthreads();
-            qr.fetch(qt, Qp + (i64)i0 * a.qs[1], a.qs[1], n.nq - i0, a.D, wave);
-            gr.fetch(gt, Gp + (i64)i0 * qrow, qrow, n.nq - i0, a.D, wave);
-            if (t < QT) {
-                const int i = i0 + t;
-                const float x = i < n.nq ? a.lse_in[stat + i] : -INFINITY;
-                lse_t[t] = x > -INFINITY ? x * LOG2E : INFINITY;
-                delta_t[t] = i < n.nq ? a.delta[stat + i] : 0.f;
-            }
-            fetched();
-            __syncthreads();
-            if (j0 >= n.nk) continue;
+        const auto fetch = [&](int x, int slot) {
+            ql.fetch(qb + slot * Tl::SIZE, Qp + (i64)(32 * x) * a.qs[1], a.qs[1], n.nq - 32 * x, a.D, wave);
+            gl.fetch(gb + slot * Tl::SIZE, Gp + (i64)(32 * x) * grow, grow, n.nq - 32 * x, a.D, wave);
+        };
+        // thread t: lse (t < 32) or delta (t < 64) of query t % 32 of group x
+        const auto stat_of = [&](int x) {
+            const int i = 32 * x + (t & 31);
+            if (t >= 64) return 0.f;
+            if (t >= 32) return i < n.nq ? a.delta[stat + i] : 0.f;
+            const float y = i < n.nq ? a.lse_in[stat + i] : -INFINITY;
+            return y > -INFINITY ? y * LOG2E : INFINITY;
+        };
+        if constexpr (BIAS) fill_bias(a, bias, head, t, 128);
+        int slot = (begin + 2) % 3;
+        fetch(begin, begin % 3);
+        if (t < 64) stats[begin % 3 * 64 + t] = stat_of(begin);
+        fetched();
+        __syncthreads();
+        float s[16];
+        f32x16_t dp = {};
 #pragma unroll
-            for (int u = 0; u < SUB; ++u) {
-                const int p0 = i0 + 32 * u + n.start; // the position of the first row
-                if (a.causal && p0 + 31 < j0) continue;
+        for (int e = 0; e < 16; ++e) s[e] = 0.f;
+        for (int x0 = begin - 1; x0 < end; ++x0) {
+            const int s1 = slot == 2 ? 0 : slot + 1, s2 = slot == 0 ? 2 : slot - 1;
+            float coming = 0.f;
+            if (x0 + 2 < end) {
+                fetch(x0 + 2, s2);
+                coming = stat_of(x0 + 2);
+            }
+            const bool now = x0 >= begin && x0 >= mine, then = x0 + 1 < end && x0 + 1 >= mine;
+            if (now || then) {
+                const T *const qrow = qb + s1 * Tl::SIZE, *const grow_t = gb + s1 * Tl::SIZE, *const qcol = qb + slot * Tl::SIZE, *const gcol = gb + slot * Tl::SIZE;
+                const float *const st = stats + slot * 64;
+                const int p0 = 32 * x0 + n.start; // the position of the first row
                 const bool edge = j0 + 32 > n.nk || (a.causal && j0 + 31 > p0);
                 const bool near = BIAS && j0 + 31 - p0 > -far && j0 - (p0 + 31) < far;
                 const float flat = BIAS ? bias[j0 >= p0 ? 2 * far : 0] : 0.f;
-                f32x16_t s = {}, dp = {};
-                #pragma unroll
-                for (int c = 0; c < DP / 16; ++c) {
-                    mma(s, Tl::by_rows(qt, 32 * u, c, lane), k[c]);
-                    mma(dp, Tl::by_rows(gt, 32 * u, c, lane), v[c]);
-                }
-                float p[16], ds[16];
-#pragma unroll
-                for (int e4 = 0; e4 < 4; ++e4) {
-                    const float4 l4 = *(const float4 *)(lse_t + 32 * u + 8 * e4 + 4 * h);
-                    const float ll[4] = {l4.x, l4.y, l4.z, l4.w};
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) p[4 * e4 + x] = ll[x];
-                }
-                if (edge || near) {
+                const bool plain = !edge && !near;
+                if (now && !plain) {
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
                         const int pos = p0 + 8 * (e >> 2) + 4 * h + (e & 3);
-                        p[e] = exp2_fast(s[e] * sl2 + ((BIAS ? bias[clamped(j - pos, -far, far) + far] : 0.f) - p[e]));
-                        if (j >= n.nk || (a.causal && j > pos)) p[e] = 0.f;
+                        s[e] = s[e] * sl2 + (BIAS ? bias[clamped(j - pos, -far, far) + far] : 0.f);
+                        if (j >= n.nk || (a.causal && j > pos)) s[e] = -INFINITY;
                     }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) p[e] = exp2_fast(s[e] * sl2 + (flat - p[e]));
                 }
+                const float mul = plain ? sl2 : 1.f, add = plain ? flat : 0.f;
+                f32x16_t next = {}, dnext = {};
+                Frag<T> ring[AHEAD + 1], fp[2], fs[2];
+                float p[16];
+                float4 l4 = *(const float4 *)(st + 4 * h), d4 = *(const float4 *)(st + 32 + 4 * h);
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int e4 = 0; e4 < 4; ++e4) {
-                    const float4 d4 = *(const float4 *)(delta_t + 32 * u + 8 * e4 + 4 * h);
-                    const float dd[4] = {d4.x, d4.y, d4.z, d4.w};
+                for (int x = 0; x < AHEAD; ++x) ring[x] = Tl::by_rows(x & 1 ? grow_t : qrow, 0, x / 2, lane);
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) ds[4 * e4 + x] = p[4 * e4 + x] * (dp[4 * e4 + x] - dd[x]);
+                for (int x = 0; x < 2 * CH; ++x) {
+                    if (x + AHEAD < 2 * CH) ring[(x + AHEAD) % (AHEAD + 1)] = Tl::by_rows((x + AHEAD) & 1 ? grow_t : qrow, 0, (x + AHEAD) / 2, lane);
+                    if (x & 1)
+                        mma(dnext, ring[x % (AHEAD + 1)], v[x / 2]);
+                    else
+                        mma(next, ring[x % (AHEAD + 1)], k[x / 2]);
+#pragma unroll
+                    for (int e = x * 16 / (2 * CH); e < (x + 1) * 16 / (2 * CH); ++e) {
+                        const float ll = e % 4 == 0 ? l4.x : e % 4 == 1 ? l4.y : e % 4 == 2 ? l4.z : l4.w;
+                        const float dd = e % 4 == 0 ? d4.x : e % 4 == 1 ? d4.y : e % 4 == 2 ? d4.z : d4.w;
+                        p[e] = exp2_fast(s[e] * mul + (add - ll));
+                        s[e] = p[e] * (dp[e] - dd);
+                        if (e % 8 == 7) {
+                            pack(p, e / 8, fp[e / 8]);
+                            pack(s, e / 8, fs[e / 8]);
+                        }
+                        if (e % 4 == 3 && e < 15) {
+                            l4 = *(const float4 *)(st + 8 * (e / 4 + 1) + 4 * h);
+                            d4 = *(const float4 *)(st + 32 + 8 * (e / 4 + 1) + 4 * h);
+                        }
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
                 }
+                if (now) {
+                    // step x: rows 16 (x / 2 DB) .., dV and dK in turn
+                    const auto operand = [&](int x) { return Tl::by_cols(x & 1 ? qcol : gcol, 16 * (x / (2 * DB)), x / 2 % DB, lane); };
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    Frag<T> f;
-                    pack(p, c, f);
+                    for (int x = 0; x < AHEAD; ++x) ring[x] = operand(x);
 #pragma unroll
-                    for (int d = 0; d < DP / 32; ++d) mma(dv[d], Tl::by_cols(gt, 32 * u + 16 * c, d, lane), f);
-                    pack(ds, c, f);
-#pragma unroll
-                    for (int d = 0; d < DP / 32; ++d) mma(dk[d], Tl::by_cols(qt, 32 * u + 16 * c, d, lane), f);
+                    for (int x = 0; x < 4 * DB; ++x) {
+                        if (x + AHEAD < 4 * DB) ring[(x + AHEAD) % (AHEAD + 1)] = operand(x + AHEAD);
+                        if (x & 1)
+                            mma(dk[x / 2 % DB], ring[x % (AHEAD + 1)], fs[x / (2 * DB)]);
+                        else
+                            mma(dv[x / 2 % DB], ring[x % (AHEAD + 1)], fp[x / (2 * DB)]);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
                 }
+                dp = dnext;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[e] = next[e];
             }
+            if (x0 + 2 < end && t < 64) stats[s2 * 64 + t] = coming;
+            slot = s1;
+            fetched();
+            __syncthreads();
         }
     }
     if (j >= a.Lk) return;
     const i64 at = (((i64)b * a.Lk + j) * a.Hkv + kv) * a.D;
     T *const ok_ = (T *)a.dK + at, *const ov = (T *)a.dV + at;
 #pragma unroll
-    for (int d = 0; d < DP / 32; ++d)
+    for (int d = 0; d < DB; ++d)
 #pragma unroll
         for (int e = 0; e < 16; e += 4) {
             const int c = 32 * d + 8 * (e >> 2) + 4 * h;
@@ -375,24 +477,25 @@ static int attn_bwd_launch(AttnArgs &a, float *dtable, int accumulate, hipStream
     int st = PF_OK;
     a.tiles = (a.Lq + 127) / 128;
     const int parts = a.B * a.tiles;
-    const dim3 grid((unsigned)a.B * a.Hq * a.tiles);
+    const int paired = a.causal && (i64)a.B * a.Hq * a.tiles > 512; // (two workgroups to a compute unit are resident)
+    const dim3 grid((unsigned)a.B * a.Hq * (paired ? (a.tiles + 1) / 2 : a.tiles));
     const size_t lds = BwdLds<T, DP>::dq(a.bk.far, bias, tab);
     if (a.Lq > 0) {
         if (tab)
-            PF_LAUNCH_LDS(st, "attn_dq_tab", (attn_dq_kernel<T, DP, true, true>), grid, dim3(256), lds, s, a);
+            PF_LAUNCH_LDS(st, "attn_dq_tab", (attn_dq_kernel<T, DP, true, true>), grid, dim3(256), lds, s, a, paired);
         else if (bias)
-            PF_LAUNCH_LDS(st, "attn_dq", (attn_dq_kernel<T, DP, true, false>), grid, dim3(256), lds, s, a);
+            PF_LAUNCH_LDS(st, "attn_dq", (attn_dq_kernel<T, DP, true, false>), grid, dim3(256), lds, s, a, paired);
         else
-            PF_LAUNCH_LDS(st, "attn_dq", (attn_dq_kernel<T, DP, false, false>), grid, dim3(256), lds, s, a);
+            PF_LAUNCH_LDS(st, "attn_dq", (attn_dq_kernel<T, DP, false, false>), grid, dim3(256), lds, s, a, paired);
     }
     if (a.Lk > 0) {
-        a.tiles = (a.Lk + 127) / 128;
+        a.tiles = (a.Lk + 63) / 64;
         const dim3 kgrid((unsigned)a.B * a.Hkv * a.tiles);
         const size_t klds = BwdLds<T, DP>::dkv(a.bk.far, bias);
         if (bias)
-            PF_LAUNCH_LDS(st, "attn_dkv", (attn_dkv_kernel<T, DP, true>), kgrid, dim3(256), klds, s, a);
+            PF_LAUNCH_LDS(st, "attn_dkv", (attn_dkv_kernel<T, DP, true>), kgrid, dim3(128), klds, s, a);
         else
-            PF_LAUNCH_LDS(st, "attn_dkv", (attn_dkv_kernel<T, DP, false>), kgrid, dim3(256), klds, s, a);
+            PF_LAUNCH_LDS(st, "attn_dkv", (attn_dkv_kernel<T, DP, false>), kgrid, dim3(128), klds, s, a);
     }
     if (tab)
         PF_LAUNCH(st, "attn_table", attn_table_kernel, dim3((unsigned)a.buckets * a.Hq), dim3(64), s, a.tab, parts, a.buckets, a.Hq, dtable, accumulate);

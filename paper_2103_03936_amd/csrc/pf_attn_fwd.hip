@@ -215,7 +215,7 @@ int attn_check(const pf_attention_desc *d)
     if (d->dtype != PF_F32 && d->dtype != PF_BF16) return PF_ERR_UNSUPPORTED;
     if (d->head_dim % 8 || d->head_dim > 128) return PF_ERR_UNSUPPORTED;
     if (!isfinite(d->scale)) return PF_ERR_UNSUPPORTED;
-    if (d->Lq >= 1 << 30 || d->Lk >= 1 << 30 || d->B > INT32_MAX / d->heads_q) return PF_ERR_UNSUPPORTED;
+    if (d->Lq >= 1 << 29 || d->Lk >= 1 << 29 || d->B > INT32_MAX / d->heads_q) return PF_ERR_UNSUPPORTED;
     // workgroups of 32 rows or keys at the least are counted in 32 bits
     if (d->B * d->heads_q > INT32_MAX / ((d->Lq + 31) / 32 + 1) || d->B * d->heads_kv > INT32_MAX / ((d->Lk + 31) / 32 + 1)) return PF_ERR_UNSUPPORTED;
     if (d->buckets) {
