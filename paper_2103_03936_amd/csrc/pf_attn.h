@@ -112,6 +112,31 @@ __device__ __forceinline__ void pack(const float (&x)[16], int c, Frag<float> &f
     for (int i = 0; i < 8; ++i) f.v[i] = x[8 * c + i];
 }
 
+// A value that is taken to change here (what follows from it is not kept in registers over a loop)
+__device__ __forceinline__ int anew(int x)
+{
+    asm volatile("" : "+v"(x));
+    return x;
+}
+__device__ __forceinline__ float anew(float x)
+{
+    asm volatile("" : "+v"(x));
+    return x;
+}
+// Values that are worked out here, whatever branch uses them later (the compiler would put them off to behind the branch)
+__device__ __forceinline__ void here(Frag<bf16_t> &f)
+{
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    u32x4 w = __builtin_bit_cast(u32x4, f.v);
+    asm volatile("" : "+v"(w));
+    f.v = __builtin_bit_cast(bf16x8_t, w);
+}
+__device__ __forceinline__ void here(Frag<float> &f)
+{
+#pragma unroll
+    for (int e = 0; e < 8; ++e) asm volatile("" : "+v"(f.v[e]));
+}
+
 // Four adjacent values
 __device__ __forceinline__ void put4(float *p, float a, float b, float c, float d) { *(float4 *)p = make_float4(a, b, c, d); }
 __device__ __forceinline__ void put4(bf16_t *p, float a, float b, float c, float d)

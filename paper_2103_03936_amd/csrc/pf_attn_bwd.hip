@@ -25,7 +25,9 @@ struct BwdLds {
     {
         return 5 * Tq::BYTES + (bias ? (2 * far + 1) * 4 : 0) + (tab ? 4 * DIAG * 4 + 4 * (2 * far + 1) * 4 : 0);
     }
-    static size_t dkv(int far, bool bias) { return 6 * Tq::BYTES + 3 * 2 * 32 * 4 + (bias ? (2 * far + 1) * 4 : 0); }
+    // dK and dV: how many waves share the queries (what six tiles of float rows take leaves room for one)
+    static constexpr int QW = sizeof(T) == 4 && DP > 64 ? 1 : 2;
+    static size_t dkv(int far, bool bias) { return 6 * QW * Tq::BYTES + 3 * 2 * 32 * QW * 4 + (bias ? (2 * far + 1) * 4 : 0); }
 };
 
 // dQ, delta and the sums of dS by distance, for one tile of 128 queries of one head.  TAB: with the gradient of the table.
@@ -41,7 +43,7 @@ template <typename T, int DP, bool BIAS, bool TAB>
 __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b, int head, int tile)
 {
     using Tl = Tile<T, DP, 32, 256>;
-    constexpr int CH = DP / 16, DB = DP / 32, AHEAD = 3;
+    constexpr int CH = DP / 16, DB = DP / 32, AHEAD = 2;
     const int far = a.bk.far, span = 2 * far + 1;
     T *const kb = (T *)lds, *const vb = kb + 3 * Tl::SIZE;
     float *const bias = (float *)(lds + 5 * Tl::BYTES);
@@ -60,6 +62,8 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b
     const int last = (i0 + 32 < n.nq ? i0 + 32 : n.nq) - 1, pmin = i0 + n.start, pmax = last + n.start, pos = i + n.start;
     int mine = i0 >= n.nq ? 0 : keys; // of the keys, those that the wave's queries see
     if (a.causal && mine > 0 && pmax + 1 < mine) mine = pmax + 1 < 0 ? 0 : pmax + 1;
+
+    const int most = a.causal && n.nk > pos ? 0 : n.nk - 1 - pos; // the furthest distance seen
 
     if (BIAS && keys > 0) fill_bias(a, bias, head, t, 256);
     if constexpr (TAB)
@@ -127,15 +131,19 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b
                 const bool edge = k0 + 32 > n.nk || (a.causal && k0 + 31 > pmin), plain = !edge && !near;
                 const float flat = BIAS ? bias[k0 >= pmin ? 2 * far : 0] : 0.f;
                 if (now && !plain) {
+                    const int rel = anew(k0 + 4 * h - pos); // distance of the first key that the lane holds
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
-                        const int x = k0 + 8 * (e >> 2) + 4 * h + (e & 3);
-                        s[e] = s[e] * sl2 + ((BIAS ? bias[clamped(x - pos, -far, far) + far] : 0.f) - lse2);
-                        if (x >= n.nk || (a.causal && x > pos)) s[e] = -INFINITY;
+                        const int x = rel + 8 * (e >> 2) + (e & 3);
+                        s[e] = s[e] * sl2 + ((BIAS ? bias[clamped(x, -far, far) + far] : 0.f) - lse2);
+                        if (x > most) s[e] = -INFINITY;
                     }
                 }
                 const float mul = plain ? sl2 : 1.f, add = plain ? flat - lse2 : 0.f;
-                f32x16_t next = {}, dnext = {};
+                f32x16_t next = {}, dnext; // (dP is formed on -delta: dS = P (dP - delta))
+                const float start = anew(-delta);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) dnext[e] = start;
                 Frag<T> ring[AHEAD + 1], f[2];
                 float sum = 0.f, sum_p = 0.f;
                 __builtin_amdgcn_sched_barrier(0);
@@ -152,12 +160,15 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b
 #pragma unroll
                     for (int e = x * 16 / (2 * CH); e < (x + 1) * 16 / (2 * CH); ++e) {
                         const float p = exp2_fast(s[e] * mul + add);
-                        s[e] = p * (dp[e] - delta);
+                        s[e] = p * dp[e];
                         if constexpr (TAB) {
                             sum += s[e];
                             sum_p += p;
                         }
-                        if (e % 8 == 7) pack(s, e / 8, f[e / 8]);
+                        if (e % 8 == 7) {
+                            pack(s, e / 8, f[e / 8]);
+                            here(f[e / 8]);
+                        }
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 }
@@ -185,7 +196,14 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b
                             __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
                             float y = 0.f;
 #pragma unroll
-                            for (int r = 0; r < 32; ++r) y += diag[r * 64 + lane];
+                            for (int r0 = 0; r0 < 32; r0 += 8) {
+                                float v[8];
+#pragma unroll
+                                for (int r = 0; r < 8; ++r) v[r] = diag[(r0 + r) * 64 + lane];
+                                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                                for (int r = 0; r < 8; ++r) y += v[r];
+                            }
                             // (distances from far on have one place, several lanes' sums go there: by way of the lanes' own)
                             const int dist = k0 - pmin + 31 - lane;
                             if (lane < 63) {
@@ -295,24 +313,29 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void attn_dq_ke
 }
 
 // dK and dV: a workgroup has 64 keys of one key head, a wave 32 of them in its columns; the query heads of the key head one
-// after the other, each 32 queries at a time.  As above, dS and P of 32 queries are worked out while S and dP of the next 32
-// are made; two waves to a workgroup, so that there are workgroups enough to even out what causal masks leave them.
+// after the other, each in groups of 32 QW queries, of which a wave has 32.  As above, dS and P of 32 queries are worked out
+// while S and dP of the next are made.  The waves that share keys add up what they have at the end.  (With all queries in
+// one wave, a causal mask's longest column alone, 512 blocks of 2 x 4096 tokens with four query heads to a key head, took 765 us:
+// the time of the whole kernel.)
 template <typename T, int DP, bool BIAS>
-__global__ __launch_bounds__(128, DP * sizeof(T) <= 128 ? 2 : 1) void attn_dkv_kernel(AttnArgs a)
+__global__ __launch_bounds__((128 * BwdLds<T, DP>::QW), (DP * sizeof(T) <= 128 ? 2 : 1)) void attn_dkv_kernel(AttnArgs a)
 {
-    using Tl = Tile<T, DP, 32, 128>;
+    constexpr int QW = BwdLds<T, DP>::QW, ROWS = 32 * QW, THREADS = 128 * QW;
+    using Tl = Tile<T, DP, ROWS, THREADS>;
     constexpr int CH = DP / 16, DB = DP / 32, AHEAD = 3;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     T *const qb = (T *)lds, *const gb = qb + 3 * Tl::SIZE;
-    float *const stats = (float *)(lds + 6 * Tl::BYTES); // [3][2][32]: lse (base 2) and delta
-    float *const bias = stats + 3 * 64;
+    float *const stats = (float *)(lds + 6 * Tl::BYTES); // [3][2][ROWS]: lse (base 2) and delta
+    float *const bias = stats + 3 * 2 * ROWS;
 
     const unsigned w = xcd_order(blockIdx.x, gridDim.x);
     const int tile = (int)(w % a.tiles), bk = w / a.tiles, b = bk / a.Hkv, kv = bk - b * a.Hkv;
     const int t = threadIdx.x, wave = wave_of(t), lane = t & 63, col = lane & 31, h = lane >> 5;
     const AttnLens n(a, b);
-    const int far = a.bk.far, j0 = tile * 64 + wave * 32, j = j0 + col;
+    const int kw = wave & 1, r0 = 32 * (wave >> 1); // the wave's keys; its rows of a group
+    const int far = a.bk.far, j0 = tile * 64 + kw * 32, j = j0 + col;
     const bool ok = j < n.nk;
+    const int most = !ok ? INT32_MIN : a.causal ? 0 : INT32_MAX; // the furthest distance from which the key is seen
     Frag<T> k[CH], v[CH];
     {
         const T *const Kp = (const T *)a.K + b * a.ks[0] + kv * a.ks[2] + j * a.ks[1], *const Vp = (const T *)a.V + b * a.vs[0] + kv * a.vs[2] + j * a.vs[1];
@@ -329,34 +352,35 @@ __global__ __launch_bounds__(128, DP * sizeof(T) <= 128 ? 2 : 1) void attn_dkv_k
 
     const i64 grow = (i64)a.Hq * a.D;
     const Tl ql(a.qs[1], a.D, t), gl(grow, a.D, t);
-    // the groups of 32 queries that see a key of the workgroup, and of the wave
-    int begin = 0, end = (n.nq + 31) / 32, mine = 0;
+    // the groups of queries that see a key of the workgroup; the first query that sees one of the wave
+    int begin = 0, mine = 0;
+    const int end = (n.nq + ROWS - 1) / ROWS;
     if (a.causal) {
-        begin = clamped(tile * 64 - n.start, 0, a.Lq) / 32;
-        mine = clamped(j0 - n.start, 0, a.Lq) / 32;
+        begin = clamped(tile * 64 - n.start, 0, a.Lq) / ROWS;
+        mine = clamped(j0 - n.start, 0, a.Lq);
     }
     if (tile * 64 >= n.nk) begin = end;
-    if (j0 >= n.nk) mine = end;
+    if (j0 >= n.nk) mine = a.Lq;
     for (int g0 = 0; g0 < a.G && begin < end; ++g0) {
         const int head = kv * a.G + g0;
         const T *const Qp = (const T *)a.Q + b * a.qs[0] + head * a.qs[2], *const Gp = (const T *)a.dO + ((i64)b * a.Lq * a.Hq + head) * a.D;
         const i64 stat = ((i64)b * a.Hq + head) * a.Lq;
         const auto fetch = [&](int x, int slot) {
-            ql.fetch(qb + slot * Tl::SIZE, Qp + (i64)(32 * x) * a.qs[1], a.qs[1], n.nq - 32 * x, a.D, wave);
-            gl.fetch(gb + slot * Tl::SIZE, Gp + (i64)(32 * x) * grow, grow, n.nq - 32 * x, a.D, wave);
+            ql.fetch(qb + slot * Tl::SIZE, Qp + (i64)(ROWS * x) * a.qs[1], a.qs[1], n.nq - ROWS * x, a.D, wave);
+            gl.fetch(gb + slot * Tl::SIZE, Gp + (i64)(ROWS * x) * grow, grow, n.nq - ROWS * x, a.D, wave);
         };
-        // thread t: lse (t < 32) or delta (t < 64) of query t % 32 of group x
+        // thread t: lse (t < ROWS) or delta (t < 2 ROWS) of query t % ROWS of group x
         const auto stat_of = [&](int x) {
-            const int i = 32 * x + (t & 31);
-            if (t >= 64) return 0.f;
-            if (t >= 32) return i < n.nq ? a.delta[stat + i] : 0.f;
+            const int i = ROWS * x + t % ROWS;
+            if (t >= 2 * ROWS) return 0.f;
+            if (t >= ROWS) return i < n.nq ? a.delta[stat + i] : 0.f;
             const float y = i < n.nq ? a.lse_in[stat + i] : -INFINITY;
             return y > -INFINITY ? y * LOG2E : INFINITY;
         };
-        if constexpr (BIAS) fill_bias(a, bias, head, t, 128);
+        if constexpr (BIAS) fill_bias(a, bias, head, t, THREADS);
         int slot = (begin + 2) % 3;
         fetch(begin, begin % 3);
-        if (t < 64) stats[begin % 3 * 64 + t] = stat_of(begin);
+        if (t < 2 * ROWS) stats[begin % 3 * 2 * ROWS + t] = stat_of(begin);
         fetched();
         __syncthreads();
         float s[16];
@@ -370,34 +394,41 @@ __global__ __launch_bounds__(128, DP * sizeof(T) <= 128 ? 2 : 1) void attn_dkv_k
                 fetch(x0 + 2, s2);
                 coming = stat_of(x0 + 2);
             }
-            const bool now = x0 >= begin && x0 >= mine, then = x0 + 1 < end && x0 + 1 >= mine;
+            const int i0 = ROWS * x0 + r0; // the wave's first query
+            const bool now = x0 >= begin && i0 < n.nq && i0 + 31 >= mine, then = x0 + 1 < end && i0 + ROWS < n.nq && i0 + ROWS + 31 >= mine;
             if (now || then) {
                 const T *const qrow = qb + s1 * Tl::SIZE, *const grow_t = gb + s1 * Tl::SIZE, *const qcol = qb + slot * Tl::SIZE, *const gcol = gb + slot * Tl::SIZE;
-                const float *const st = stats + slot * 64;
-                const int p0 = 32 * x0 + n.start; // the position of the first row
+                const float *const st = stats + slot * 2 * ROWS + r0, *const st1 = stats + s1 * 2 * ROWS + r0;
+                const int p0 = i0 + n.start; // the position of the first row
                 const bool edge = j0 + 32 > n.nk || (a.causal && j0 + 31 > p0);
                 const bool near = BIAS && j0 + 31 - p0 > -far && j0 - (p0 + 31) < far;
                 const float flat = BIAS ? bias[j0 >= p0 ? 2 * far : 0] : 0.f;
                 const bool plain = !edge && !near;
                 if (now && !plain) {
+                    const int rel = anew(j - p0 - 4 * h); // distance of the first query that the lane holds
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
-                        const int pos = p0 + 8 * (e >> 2) + 4 * h + (e & 3);
-                        s[e] = s[e] * sl2 + (BIAS ? bias[clamped(j - pos, -far, far) + far] : 0.f);
-                        if (j >= n.nk || (a.causal && j > pos)) s[e] = -INFINITY;
+                        const int x = rel - 8 * (e >> 2) - (e & 3);
+                        s[e] = s[e] * sl2 + (BIAS ? bias[clamped(x, -far, far) + far] : 0.f);
+                        if (x > most) s[e] = -INFINITY;
                     }
                 }
                 const float mul = plain ? sl2 : 1.f, add = plain ? flat : 0.f;
-                f32x16_t next = {}, dnext = {};
+                f32x16_t next = {}, dnext; // (dP is formed on -delta: dS = P (dP - delta))
+#pragma unroll
+                for (int e = 0; e < 16; e += 4) {
+                    const float4 d4 = *(const float4 *)(st1 + ROWS + 2 * e + 4 * h);
+                    dnext[e] = -d4.x, dnext[e + 1] = -d4.y, dnext[e + 2] = -d4.z, dnext[e + 3] = -d4.w;
+                }
                 Frag<T> ring[AHEAD + 1], fp[2], fs[2];
                 float p[16];
-                float4 l4 = *(const float4 *)(st + 4 * h), d4 = *(const float4 *)(st + 32 + 4 * h);
+                float4 l4 = *(const float4 *)(st + 4 * h);
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int x = 0; x < AHEAD; ++x) ring[x] = Tl::by_rows(x & 1 ? grow_t : qrow, 0, x / 2, lane);
+                for (int x = 0; x < AHEAD; ++x) ring[x] = Tl::by_rows(x & 1 ? grow_t : qrow, r0, x / 2, lane);
 #pragma unroll
                 for (int x = 0; x < 2 * CH; ++x) {
-                    if (x + AHEAD < 2 * CH) ring[(x + AHEAD) % (AHEAD + 1)] = Tl::by_rows((x + AHEAD) & 1 ? grow_t : qrow, 0, (x + AHEAD) / 2, lane);
+                    if (x + AHEAD < 2 * CH) ring[(x + AHEAD) % (AHEAD + 1)] = Tl::by_rows((x + AHEAD) & 1 ? grow_t : qrow, r0, (x + AHEAD) / 2, lane);
                     if (x & 1)
                         mma(dnext, ring[x % (AHEAD + 1)], v[x / 2]);
                     else
@@ -405,23 +436,21 @@ __global__ __launch_bounds__(128, DP * sizeof(T) <= 128 ? 2 : 1) void attn_dkv_k
 #pragma unroll
                     for (int e = x * 16 / (2 * CH); e < (x + 1) * 16 / (2 * CH); ++e) {
                         const float ll = e % 4 == 0 ? l4.x : e % 4 == 1 ? l4.y : e % 4 == 2 ? l4.z : l4.w;
-                        const float dd = e % 4 == 0 ? d4.x : e % 4 == 1 ? d4.y : e % 4 == 2 ? d4.z : d4.w;
                         p[e] = exp2_fast(s[e] * mul + (add - ll));
-                        s[e] = p[e] * (dp[e] - dd);
+                        s[e] = p[e] * dp[e];
                         if (e % 8 == 7) {
                             pack(p, e / 8, fp[e / 8]);
                             pack(s, e / 8, fs[e / 8]);
+                            here(fp[e / 8]);
+                            here(fs[e / 8]);
                         }
-                        if (e % 4 == 3 && e < 15) {
-                            l4 = *(const float4 *)(st + 8 * (e / 4 + 1) + 4 * h);
-                            d4 = *(const float4 *)(st + 32 + 8 * (e / 4 + 1) + 4 * h);
-                        }
+                        if (e % 4 == 3 && e < 15) l4 = *(const float4 *)(st + 8 * (e / 4 + 1) + 4 * h);
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 }
                 if (now) {
                     // step x: rows 16 (x / 2 DB) .., dV and dK in turn
-                    const auto operand = [&](int x) { return Tl::by_cols(x & 1 ? qcol : gcol, 16 * (x / (2 * DB)), x / 2 % DB, lane); };
+                    const auto operand = [&](int x) { return Tl::by_cols(x & 1 ? qcol : gcol, r0 + 16 * (x / (2 * DB)), x / 2 % DB, lane); };
 #pragma unroll
                     for (int x = 0; x < AHEAD; ++x) ring[x] = operand(x);
 #pragma unroll
@@ -438,11 +467,32 @@ __global__ __launch_bounds__(128, DP * sizeof(T) <= 128 ? 2 : 1) void attn_dkv_k
 #pragma unroll
                 for (int e = 0; e < 16; ++e) s[e] = next[e];
             }
-            if (x0 + 2 < end && t < 64) stats[s2 * 64 + t] = coming;
+            if (x0 + 2 < end && t < 2 * ROWS) stats[s2 * 2 * ROWS + t] = coming;
             slot = s1;
             fetched();
             __syncthreads();
         }
+    }
+    if constexpr (QW == 2) { // (the loop ended with a barrier: the tiles' room is free)
+        float *const sum = (float *)lds + kw * DB * 2048 + lane;
+        if (wave >= 2) {
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    sum[(16 * d + e) * 64] = dk[d][e];
+                    sum[(16 * (DB + d) + e) * 64] = dv[d][e];
+                }
+        }
+        __syncthreads();
+        if (wave >= 2) return;
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                dk[d][e] += sum[(16 * d + e) * 64];
+                dv[d][e] += sum[(16 * (DB + d) + e) * 64];
+            }
     }
     if (j >= a.Lk) return;
     const i64 at = (((i64)b * a.Lk + j) * a.Hkv + kv) * a.D;
@@ -493,9 +543,9 @@ static int attn_bwd_launch(AttnArgs &a, float *dtable, int accumulate, hipStream
         const dim3 kgrid((unsigned)a.B * a.Hkv * a.tiles);
         const size_t klds = BwdLds<T, DP>::dkv(a.bk.far, bias);
         if (bias)
-            PF_LAUNCH_LDS(st, "attn_dkv", (attn_dkv_kernel<T, DP, true>), kgrid, dim3(128), klds, s, a);
+            PF_LAUNCH_LDS(st, "attn_dkv", (attn_dkv_kernel<T, DP, true>), kgrid, dim3(128 * BwdLds<T, DP>::QW), klds, s, a);
         else
-            PF_LAUNCH_LDS(st, "attn_dkv", (attn_dkv_kernel<T, DP, false>), kgrid, dim3(128), klds, s, a);
+            PF_LAUNCH_LDS(st, "attn_dkv", (attn_dkv_kernel<T, DP, false>), kgrid, dim3(128 * BwdLds<T, DP>::QW), klds, s, a);
     }
     if (tab)
         PF_LAUNCH(st, "attn_table", attn_table_kernel, dim3((unsigned)a.buckets * a.Hq), dim3(64), s, a.tab, parts, a.buckets, a.Hq, dtable, accumulate);

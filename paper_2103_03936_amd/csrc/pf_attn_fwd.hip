@@ -32,6 +32,7 @@ __device__ __forceinline__ void attn_fwd_tile(const AttnArgs &a, char *lds, int 
     const int block_last = (tile * 128 + 128 < n.nq ? tile * 128 + 128 : n.nq) - 1 + n.start; // positions
     if (a.causal && block_last + 1 < keys) keys = block_last + 1 < 0 ? 0 : block_last + 1;
     const int last = (i0 + 32 < n.nq ? i0 + 32 : n.nq) - 1, pmin = i0 + n.start, pmax = last + n.start, pos = i + n.start;
+    const int most = a.causal && n.nk > pos ? 0 : n.nk - 1 - pos; // the furthest distance seen
     int mine = i0 >= n.nq ? 0 : keys;
     if (a.causal && mine > 0 && pmax + 1 < mine) mine = pmax + 1 < 0 ? 0 : pmax + 1;
 
@@ -89,13 +90,14 @@ __device__ __forceinline__ void attn_fwd_tile(const AttnArgs &a, char *lds, int 
                 top = top * sl2 + flat;
             } else {
                 top = -INFINITY;
+                const int rel = anew(k0 + 4 * h - pos); // distance of the first key that the lane holds
 #pragma unroll
                 for (int u = 0; u < SUB; ++u)
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
-                        const int j = k0 + 32 * u + 8 * (e >> 2) + 4 * h + (e & 3);
-                        s[u][e] = s[u][e] * sl2 + (BIAS ? bias[clamped(j - pos, -far, far) + far] : 0.f);
-                        if (j >= n.nk || (a.causal && j > pos)) s[u][e] = -INFINITY;
+                        const int x = rel + 32 * u + 8 * (e >> 2) + (e & 3);
+                        s[u][e] = s[u][e] * sl2 + (BIAS ? bias[clamped(x, -far, far) + far] : 0.f);
+                        if (x > most) s[u][e] = -INFINITY;
                         top = fmaxf(top, s[u][e]);
                     }
             }
