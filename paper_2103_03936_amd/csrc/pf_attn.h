@@ -18,7 +18,7 @@ struct AttnArgs {
     const void *Q, *K, *V, *dO, *Oin;
     void *O, *dQ, *dK, *dV;
     const float *table, *lse_in;
-    float *lse, *delta, *tab; // delta[B, Hq, Lq]; tab[Hq][B * tiles][buckets]: sums of dS per workgroup
+    float *lse, *delta, *tab; // delta[B, Hq, Lq][2]: lse (base 2; infinity where a query takes no part) and delta; tab[Hq][B * tiles][buckets]: sums of dS per workgroup
     const int *q_start, *q_len, *kv_len;
     int B, Lq, Lk, Hq, Hkv, G, D, causal, buckets, two_sided, tiles;
     float scale;
@@ -96,7 +96,7 @@ __device__ __forceinline__ Frag<float> row_frag_buffer(const BufSrc &src, uint32
 
 // Eight values of a result (its registers 8 c .. 8 c + 7) as the operand for rows 16 c .. 16 c + 15; bf16: rounded to
 // nearest even, the one rounding of P and dS, half a step of 2^-8 each
-__device__ __forceinline__ void pack(const float (&x)[16], int c, Frag<bf16_t> &f)
+__device__ __forceinline__ void pack(const f32x16_t &x, int c, Frag<bf16_t> &f)
 {
     union {
         uint32_t u[4];
@@ -106,7 +106,7 @@ __device__ __forceinline__ void pack(const float (&x)[16], int c, Frag<bf16_t> &
     for (int i = 0; i < 4; ++i) w.u[i] = pack_bf16x2(x[8 * c + 2 * i], x[8 * c + 2 * i + 1]);
     f.v = w.v;
 }
-__device__ __forceinline__ void pack(const float (&x)[16], int c, Frag<float> &f)
+__device__ __forceinline__ void pack(const f32x16_t &x, int c, Frag<float> &f)
 {
 #pragma unroll
     for (int i = 0; i < 8; ++i) f.v[i] = x[8 * c + i];
@@ -188,39 +188,52 @@ struct Tile {
             if (PIECES % THREADS == 0 || i * THREADS + wave * 64 < PIECES)
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(src.r, (lds_ptr)((char *)lds + (i * THREADS + wave * 64) * 16), 16, (int)at[i], 0, 0, 0);
     }
-    // Operand with the index along the rows (the lane's: r0 + lane % 32) and the contraction along columns 16 c ..
-    static __device__ __forceinline__ Frag<T> by_rows(const T *lds, int r0, int c, int lane)
+    // Where a lane reads.  turn() permutes bits, so that a step along a row is an exclusive or of the place: one number for a lane
+    // and constants, not an address for every read.
+    static __device__ __forceinline__ int row_place(int lane)
     {
-        const int row = lane & 31, h = lane >> 5;
-        const T *const p = lds + (r0 + row) * PITCH;
-        Frag<T> f;
+        const int row = lane & 31;
+        return row * PITCH + ((lane >> 5) ^ turn(row)) * VEC;
+    }
+    static __device__ __forceinline__ int col_place(int lane)
+    {
         if constexpr (sizeof(T) == 2) {
-            f.v = *(const bf16x8_t *)(p + ((2 * c + h) ^ turn(row)) * VEC);
+            const int g = lane >> 4, i = lane & 15, row = 4 * (g >> 1) + (i >> 2);
+            return row * PITCH + ((2 * (g & 1) + (i >> 1 & 1)) ^ turn(row)) * VEC + 4 * (i & 1);
+        }
+        const int row = 4 * (lane >> 5);
+        return row * PITCH + ((lane >> 2 & 7) ^ turn(row)) * VEC + (lane & 3);
+    }
+    // Operand with the index along the 32 rows from r0 on and the contraction along columns 16 c ..; at: row_place plus the
+    // elements from `lds` to the tile
+    static __device__ __forceinline__ Frag<T> by_rows(const T *lds, int at, int r0, int c)
+    {
+        Frag<T> f;
+        const T *const p = lds + (at ^ (16 * c)) + r0 * PITCH;
+        if constexpr (sizeof(T) == 2) {
+            f.v = *(const bf16x8_t *)p;
         } else {
-            const float4 x = *(const float4 *)(p + ((4 * c + h) ^ turn(row)) * VEC), y = *(const float4 *)(p + ((4 * c + 2 + h) ^ turn(row)) * VEC);
+            const float4 x = *(const float4 *)p, y = *(const float4 *)(lds + (at ^ (16 * c + 8)) + r0 * PITCH);
             f.v[0] = x.x, f.v[1] = x.y, f.v[2] = x.z, f.v[3] = x.w, f.v[4] = y.x, f.v[5] = y.y, f.v[6] = y.z, f.v[7] = y.w;
         }
         return f;
     }
     // Operand with the index along the columns 32 d .. 32 d + 31 and the contraction along rows r0 .. r0 + 15 (r0 a multiple
-    // of 16), in the order in which a product's result lies in the lanes
-    static __device__ __forceinline__ Frag<T> by_cols(const T *lds, int r0, int d, int lane)
+    // of 16), in the order in which a product's result lies in the lanes; at: col_place plus the elements to the tile
+    static __device__ __forceinline__ Frag<T> by_cols(const T *lds, int at, int r0, int d)
     {
         Frag<T> f;
         if constexpr (sizeof(T) == 2) {
             typedef __attribute__((address_space(3))) bf16x4_t *lds_ptr;
-            const int g = lane >> 4, i = lane & 15, row = 4 * (g >> 1) + (i >> 2), c = 4 * d + 2 * (g & 1) + (i >> 1 & 1);
-            const T *const lo = lds + (r0 + row) * PITCH + (c ^ turn(row)) * VEC + 4 * (i & 1);
-            const T *const hi = lds + (r0 + row + 8) * PITCH + (c ^ turn(row + 8)) * VEC + 4 * (i & 1);
+            const T *const lo = lds + (at ^ (32 * d)) + r0 * PITCH, *const hi = lds + (at ^ (32 * d + turn(8) * VEC)) + (r0 + 8) * PITCH;
             const bf16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_ptr)lo), y = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_ptr)hi);
 #pragma unroll
             for (int e = 0; e < 4; ++e) f.v[e] = x[e], f.v[4 + e] = y[e];
         } else {
-            const int c = 8 * d + (lane >> 2 & 7);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const int row = 4 * (lane >> 5) + (e & 3) + 8 * (e >> 2);
-                f.v[e] = lds[(r0 + row) * PITCH + (c ^ turn(row)) * VEC + (lane & 3)];
+                const int row = (e & 3) + 8 * (e >> 2);
+                f.v[e] = lds[(at ^ (32 * d + turn(row) * VEC)) + (r0 + row) * PITCH];
             }
         }
         return f;

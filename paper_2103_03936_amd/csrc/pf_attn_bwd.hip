@@ -38,7 +38,8 @@ struct BwdLds {
 //
 // With the table's gradient there are two passes.  The first takes delta from O; in the far blocks, where one bucket holds all
 // distances, it keeps the sums of dS and of P of each row, and it sums all dS of a row: that sum is what delta is off by. The
-// second pass goes over the near blocks alone, with the delta that is now exact; the far sums are put right by their sums of P.
+// second pass goes over the near blocks alone, for their dS with the delta that is now exact (S and dP, two products of the
+// first pass's three); the far sums are put right by their sums of P.
 template <typename T, int DP, bool BIAS, bool TAB>
 __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b, int head, int tile)
 {
@@ -96,157 +97,107 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b
     float before = 0.f, after = 0.f, before_p = 0.f, after_p = 0.f, off = 0.f; // far sums of dS and P; the sum of all dS
 
     const Tl kl(a.ks[1], a.D, t), vl(a.vs[1], a.D, t);
-    const auto near_at = [&](int k0, int lo, int hi) { return BIAS && k0 + 31 - lo > -far && k0 - hi < far; };
-    for (int pass = 0; pass < (TAB ? 2 : 1); ++pass) {
-        // the groups of 32 keys that the workgroup goes through
-        int begin = 0, end = (keys + 31) / 32;
-        if (TAB && pass == 1 && keys > 0) { // (32 begin + 31 > first position - far; 32 (end - 1) < last position + far)
-            const int lo = tile * 128 + n.start - far - 31, hi = block_last + far;
-            if (lo >= 0) begin = lo / 32 + 1;
-            if (hi <= 0) end = 0;
-            else if ((hi + 31) / 32 < end) end = (hi + 31) / 32;
-        }
-        if (begin < end) {
-            kl.fetch(kb + begin % 3 * Tl::SIZE, Kp + (i64)(32 * begin) * a.ks[1], a.ks[1], n.nk - 32 * begin, a.D, wave);
-            vl.fetch(vb + (begin & 1) * Tl::SIZE, Vp + (i64)(32 * begin) * a.vs[1], a.vs[1], n.nk - 32 * begin, a.D, wave);
-            fetched();
-            __syncthreads();
-        }
-        float s[16];
-        f32x16_t dp = {};
+    const int rows = Tl::row_place(lane), cols = Tl::col_place(lane);
+    const auto near_at = [&](int k0) { return BIAS && k0 + 31 - pmin > -far && k0 - pmax < far; };
+    const auto fetch = [&](int j, int kslot, int vslot) {
+        kl.fetch(kb + kslot * Tl::SIZE, Kp + (i64)(32 * j) * a.ks[1], a.ks[1], n.nk - 32 * j, a.D, wave);
+        vl.fetch(vb + vslot * Tl::SIZE, Vp + (i64)(32 * j) * a.vs[1], a.vs[1], n.nk - 32 * j, a.D, wave);
+    };
+    // the scores of a block at an edge or near the diagonal, with bias and masks, less lse
+    const auto finish = [&](f32x16_t &s, int k0) {
+        const int rel = anew(k0 + 4 * h - pos); // distance of the first key that the lane holds
 #pragma unroll
-        for (int e = 0; e < 16; ++e) s[e] = 0.f;
-        int slot = (begin + 2) % 3; // of group j
-        for (int j = begin - 1; j < end; ++j) {
-            const int s1 = slot == 2 ? 0 : slot + 1, s2 = slot == 0 ? 2 : slot - 1; // of groups j + 1, j + 2
-            const int k0 = 32 * j;
-            if (j + 2 < end) {
-                kl.fetch(kb + s2 * Tl::SIZE, Kp + (i64)(k0 + 64) * a.ks[1], a.ks[1], n.nk - k0 - 64, a.D, wave);
-                vl.fetch(vb + (j & 1) * Tl::SIZE, Vp + (i64)(k0 + 64) * a.vs[1], a.vs[1], n.nk - k0 - 64, a.D, wave);
-            }
-            const bool near = near_at(k0, pmin, pmax), there = !TAB || pass == 0;
-            const bool now = j >= begin && k0 < mine && (there || near), then = k0 + 32 < mine && (there || near_at(k0 + 32, pmin, pmax));
-            if (now || then) {
-                const T *const krow = kb + s1 * Tl::SIZE, *const vrow = vb + ((j + 1) & 1) * Tl::SIZE, *const kcol = kb + slot * Tl::SIZE;
-                const bool edge = k0 + 32 > n.nk || (a.causal && k0 + 31 > pmin), plain = !edge && !near;
-                const float flat = BIAS ? bias[k0 >= pmin ? 2 * far : 0] : 0.f;
-                if (now && !plain) {
-                    const int rel = anew(k0 + 4 * h - pos); // distance of the first key that the lane holds
+        for (int e = 0; e < 16; ++e) {
+            const int x = rel + 8 * (e >> 2) + (e & 3);
+            s[e] = s[e] * sl2 + ((BIAS ? bias[clamped(x, -far, far) + far] : 0.f) - lse2);
+            if (x > most) s[e] = -INFINITY;
+        }
+    };
+    const int groups = (keys + 31) / 32; // of 32 keys
+    if (groups > 0) {
+        fetch(0, 0, 0);
+        fetched();
+        __syncthreads();
+    }
+    f32x16_t sA = {}, sB = {}, dpA = {}, dpB = {};
+    int slot = 2; // of group j
+    const auto turn = [&](int j, f32x16_t &s, f32x16_t &dp, f32x16_t &next, f32x16_t &dnext) {
+        const int s1 = slot == 2 ? 0 : slot + 1, s2 = slot == 0 ? 2 : slot - 1; // of groups j + 1, j + 2
+        const int k0 = 32 * j;
+        if (j + 2 < groups) fetch(j + 2, s2, j & 1);
+        const bool now = j >= 0 && k0 < mine, then = k0 + 32 < mine;
+        if (now || then) {
+            const int krow = s1 * Tl::SIZE + rows, vrow = ((j + 1) & 1) * Tl::SIZE + rows, kcol = slot * Tl::SIZE + cols;
+            const auto row_operand = [&](int x) { return Tl::by_rows(x & 1 ? vb : kb, x & 1 ? vrow : krow, 0, x / 2); };
+            const auto col_operand = [&](int x) { return Tl::by_cols(kb, kcol, 16 * (x / DB), x % DB); };
+            const bool near = near_at(k0), plain = !near && k0 + 32 <= n.nk && !(a.causal && k0 + 31 > pmin);
+            const float flat = BIAS ? bias[k0 >= pmin ? 2 * far : 0] : 0.f;
+            if (now && !plain) finish(s, k0);
+            const float mul = plain ? sl2 : 1.f, add = plain ? flat - lse2 : 0.f;
+            const float start = anew(-delta); // (dP is formed on -delta: dS = P (dP - delta))
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int x = rel + 8 * (e >> 2) + (e & 3);
-                        s[e] = s[e] * sl2 + ((BIAS ? bias[clamped(x, -far, far) + far] : 0.f) - lse2);
-                        if (x > most) s[e] = -INFINITY;
+            for (int e = 0; e < 16; ++e) next[e] = 0.f, dnext[e] = start;
+            Frag<T> ring[AHEAD + 1], f[2];
+            float sum = 0.f, sum_p = 0.f;
+            __builtin_amdgcn_sched_barrier(0);
+            // S and dP of the next keys (step 2 c: S, columns 16 c ..; 2 c + 1: dP) beside dS of these
+#pragma unroll
+            for (int x = 0; x < AHEAD; ++x) ring[x] = row_operand(x);
+#pragma unroll
+            for (int x = 0; x < 2 * CH; ++x) {
+                if (x + AHEAD < 2 * CH) ring[(x + AHEAD) % (AHEAD + 1)] = row_operand(x + AHEAD);
+                if (x & 1)
+                    mma(dnext, ring[x % (AHEAD + 1)], g[x / 2]);
+                else
+                    mma(next, ring[x % (AHEAD + 1)], q[x / 2]);
+#pragma unroll
+                for (int e = x * 16 / (2 * CH); e < (x + 1) * 16 / (2 * CH); ++e) {
+                    const float p = exp2_fast(s[e] * mul + add);
+                    s[e] = p * dp[e];
+                    if constexpr (TAB) {
+                        sum += s[e];
+                        sum_p += p;
+                    }
+                    if (e % 8 == 7) {
+                        pack(s, e / 8, f[e / 8]);
+                        here(f[e / 8]);
                     }
                 }
-                const float mul = plain ? sl2 : 1.f, add = plain ? flat - lse2 : 0.f;
-                f32x16_t next = {}, dnext; // (dP is formed on -delta: dS = P (dP - delta))
-                const float start = anew(-delta);
-#pragma unroll
-                for (int e = 0; e < 16; ++e) dnext[e] = start;
-                Frag<T> ring[AHEAD + 1], f[2];
-                float sum = 0.f, sum_p = 0.f;
                 __builtin_amdgcn_sched_barrier(0);
-                // S and dP of the next keys (step 2 c: S, columns 16 c ..; 2 c + 1: dP) beside dS of these
-#pragma unroll
-                for (int x = 0; x < AHEAD; ++x) ring[x] = Tl::by_rows(x & 1 ? vrow : krow, 0, x / 2, lane);
-#pragma unroll
-                for (int x = 0; x < 2 * CH; ++x) {
-                    if (x + AHEAD < 2 * CH) ring[(x + AHEAD) % (AHEAD + 1)] = Tl::by_rows((x + AHEAD) & 1 ? vrow : krow, 0, (x + AHEAD) / 2, lane);
-                    if (x & 1)
-                        mma(dnext, ring[x % (AHEAD + 1)], g[x / 2]);
-                    else
-                        mma(next, ring[x % (AHEAD + 1)], q[x / 2]);
-#pragma unroll
-                    for (int e = x * 16 / (2 * CH); e < (x + 1) * 16 / (2 * CH); ++e) {
-                        const float p = exp2_fast(s[e] * mul + add);
-                        s[e] = p * dp[e];
-                        if constexpr (TAB) {
-                            sum += s[e];
-                            sum_p += p;
-                        }
-                        if (e % 8 == 7) {
-                            pack(s, e / 8, f[e / 8]);
-                            here(f[e / 8]);
+            }
+            if (now) {
+                if constexpr (TAB) {
+                    off += sum;
+                    if (!near) {
+                        if (k0 >= pmin) {
+                            after += sum;
+                            after_p += sum_p;
+                        } else {
+                            before += sum;
+                            before_p += sum_p;
                         }
                     }
+                }
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int x = 0; x < AHEAD; ++x) ring[x] = col_operand(x);
+#pragma unroll
+                for (int x = 0; x < 2 * DB; ++x) {
+                    if (x + AHEAD < 2 * DB) ring[(x + AHEAD) % (AHEAD + 1)] = col_operand(x + AHEAD);
+                    mma(dq[x % DB], ring[x % (AHEAD + 1)], f[x / DB]);
                     __builtin_amdgcn_sched_barrier(0);
                 }
-                if (now) {
-                    bool add_dq = true;
-                    if constexpr (TAB) {
-                        if (pass == 0) {
-                            off += sum;
-                            add_dq = !near;
-                            if (!near) {
-                                if (k0 >= pmin) {
-                                    after += sum;
-                                    after_p += sum_p;
-                                } else {
-                                    before += sum;
-                                    before_p += sum_p;
-                                }
-                            }
-                        } else {
-                            // along the diagonals of the block: lane x has the distance x - 31 from that of its corner
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) diag[(8 * (e >> 2) + 4 * h + (e & 3)) * 63 + col + 31] = s[e];
-                            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-                            __builtin_amdgcn_wave_barrier();
-                            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-                            float y = 0.f;
-#pragma unroll
-                            for (int r0 = 0; r0 < 32; r0 += 8) {
-                                float v[8];
-#pragma unroll
-                                for (int r = 0; r < 8; ++r) v[r] = diag[(r0 + r) * 64 + lane];
-                                __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                                for (int r = 0; r < 8; ++r) y += v[r];
-                            }
-                            // (distances from far on have one place, several lanes' sums go there: by way of the lanes' own)
-                            const int dist = k0 - pmin + 31 - lane;
-                            if (lane < 63) {
-                                if (dist <= -far)
-                                    before += y;
-                                else if (dist >= far)
-                                    after += y;
-                                else
-                                    sums[dist + far] += y;
-                            }
-                            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-                            __builtin_amdgcn_wave_barrier();
-                            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-                        }
-                    }
-                    if (add_dq) {
-                        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                        for (int x = 0; x < AHEAD; ++x) ring[x] = Tl::by_cols(kcol, 16 * (x / DB), x % DB, lane);
-#pragma unroll
-                        for (int x = 0; x < 2 * DB; ++x) {
-                            if (x + AHEAD < 2 * DB) ring[(x + AHEAD) % (AHEAD + 1)] = Tl::by_cols(kcol, 16 * ((x + AHEAD) / DB), (x + AHEAD) % DB, lane);
-                            mma(dq[x % DB], ring[x % (AHEAD + 1)], f[x / DB]);
-                            __builtin_amdgcn_sched_barrier(0);
-                        }
-                    }
-                }
-                dp = dnext;
-#pragma unroll
-                for (int e = 0; e < 16; ++e) s[e] = next[e];
-            }
-            slot = s1;
-            fetched();
-            __syncthreads();
-        }
-        if constexpr (TAB) {
-            if (pass == 0) {
-                off += __shfl_xor(off, 32);
-                delta += off;
-                before -= off * before_p;
-                after -= off * after_p;
             }
         }
+        slot = s1;
+        fetched();
+        __syncthreads();
+    };
+    int start = -1; // (a number to the compiler: it would unroll the first turn for its own)
+    asm volatile("" : "+s"(start));
+    for (int j = start; j < groups; j += 2) {
+        turn(j, sA, dpA, sB, dpB);
+        if (j + 1 < groups) turn(j + 1, sB, dpB, sA, dpA);
     }
     if (i < a.Lq) {
         T *const out = (T *)a.dQ + at;
@@ -260,9 +211,71 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b
                 for (int x = 0; x < 4; ++x) v[x] = ok ? dq[d][e + x] * a.scale : 0.f;
                 if (c < a.D) put4(out + c, v[0], v[1], v[2], v[3]);
             }
-        if (h == 0) a.delta[stat] = ok ? delta : 0.f;
     }
     if constexpr (TAB) {
+        off += __shfl_xor(off, 32);
+        delta += off;
+        before -= off * before_p;
+        after -= off * after_p;
+    }
+    if (i < a.Lq && h == 0) *(float2 *)(a.delta + 2 * stat) = make_float2(lse2, ok ? delta : 0.f);
+    if constexpr (TAB) {
+        // the near blocks once more: 32 begin + 31 > first position - far, 32 (end - 1) < last position + far
+        int begin = 0, end = groups;
+        const int lo = tile * 128 + n.start - far - 31, hi = block_last + far;
+        if (lo >= 0) begin = lo / 32 + 1;
+        if (hi <= 0)
+            end = 0;
+        else if ((hi + 31) / 32 < end)
+            end = (hi + 31) / 32;
+        if (begin < end) {
+            fetch(begin, begin & 1, begin & 1);
+            fetched();
+            __syncthreads();
+        }
+        for (int j = begin; j < end; ++j) {
+            const int k0 = 32 * j;
+            if (j + 1 < end) fetch(j + 1, (j + 1) & 1, (j + 1) & 1);
+            if (k0 < mine && near_at(k0)) {
+                const int at_j = (j & 1) * Tl::SIZE + rows;
+                f32x16_t s = {}, dp;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) dp[e] = -delta;
+#pragma unroll
+                for (int c = 0; c < CH; ++c) {
+                    mma(s, Tl::by_rows(kb, at_j, 0, c), q[c]);
+                    mma(dp, Tl::by_rows(vb, at_j, 0, c), g[c]);
+                }
+                finish(s, k0);
+                // along the diagonals of the block
+#pragma unroll
+                for (int e = 0; e < 16; ++e) diag[(8 * (e >> 2) + 4 * h + (e & 3)) * 63 + col + 31] = exp2_fast(s[e]) * dp[e];
+                __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+                __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+                float v[32], y = 0.f;
+#pragma unroll
+                for (int r = 0; r < 32; ++r) v[r] = diag[r * 64 + lane];
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int r = 0; r < 32; ++r) y += v[r];
+                // (distances from far on have one place, several lanes' sums go there: by way of the lanes' own)
+                const int dist = k0 - pmin + 31 - lane;
+                if (lane < 63) {
+                    if (dist <= -far)
+                        before += y;
+                    else if (dist >= far)
+                        after += y;
+                    else
+                        sums[dist + far] += y;
+                }
+                __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+                __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+            }
+            fetched();
+            __syncthreads();
+        }
         for (int o = 32; o; o >>= 1) {
             before += __shfl_xor(before, o);
             after += __shfl_xor(after, o);
@@ -325,7 +338,7 @@ __global__ __launch_bounds__((128 * BwdLds<T, DP>::QW), (DP * sizeof(T) <= 128 ?
     constexpr int CH = DP / 16, DB = DP / 32, AHEAD = 3;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     T *const qb = (T *)lds, *const gb = qb + 3 * Tl::SIZE;
-    float *const stats = (float *)(lds + 6 * Tl::BYTES); // [3][2][ROWS]: lse (base 2) and delta
+    float *const stats = (float *)(lds + 6 * Tl::BYTES); // [3][ROWS][2]: lse (base 2) and delta of each query
     float *const bias = stats + 3 * 2 * ROWS;
 
     const unsigned w = xcd_order(blockIdx.x, gridDim.x);
@@ -352,6 +365,7 @@ __global__ __launch_bounds__((128 * BwdLds<T, DP>::QW), (DP * sizeof(T) <= 128 ?
 
     const i64 grow = (i64)a.Hq * a.D;
     const Tl ql(a.qs[1], a.D, t), gl(grow, a.D, t);
+    const int rows = Tl::row_place(lane), cols = Tl::col_place(lane);
     // the groups of queries that see a key of the workgroup; the first query that sees one of the wave
     int begin = 0, mine = 0;
     const int end = (n.nq + ROWS - 1) / ROWS;
@@ -369,25 +383,23 @@ __global__ __launch_bounds__((128 * BwdLds<T, DP>::QW), (DP * sizeof(T) <= 128 ?
             ql.fetch(qb + slot * Tl::SIZE, Qp + (i64)(ROWS * x) * a.qs[1], a.qs[1], n.nq - ROWS * x, a.D, wave);
             gl.fetch(gb + slot * Tl::SIZE, Gp + (i64)(ROWS * x) * grow, grow, n.nq - ROWS * x, a.D, wave);
         };
-        // thread t: lse (t < ROWS) or delta (t < 2 ROWS) of query t % ROWS of group x
+        // value t of the group's [ROWS][2]
         const auto stat_of = [&](int x) {
-            const int i = ROWS * x + t % ROWS;
-            if (t >= 2 * ROWS) return 0.f;
-            if (t >= ROWS) return i < n.nq ? a.delta[stat + i] : 0.f;
-            const float y = i < n.nq ? a.lse_in[stat + i] : -INFINITY;
-            return y > -INFINITY ? y * LOG2E : INFINITY;
+            const int left = a.Lq - ROWS * x;
+            const BufSrc src(a.delta + 2 * (stat + ROWS * x), 8 * (left < ROWS ? left : ROWS));
+            return src.load4(t < 2 * ROWS ? 4 * t : BUF_OUT);
+        };
+        const auto put_stat = [&](int x, int slot, float y) { // (behind the last query: lse = infinity, P = 0)
+            if (t < 2 * ROWS) stats[slot * 2 * ROWS + t] = !(t & 1) && ROWS * x + t / 2 >= a.Lq ? INFINITY : y;
         };
         if constexpr (BIAS) fill_bias(a, bias, head, t, THREADS);
         int slot = (begin + 2) % 3;
         fetch(begin, begin % 3);
-        if (t < 2 * ROWS) stats[begin % 3 * 2 * ROWS + t] = stat_of(begin);
+        put_stat(begin, begin % 3, stat_of(begin));
         fetched();
         __syncthreads();
-        float s[16];
-        f32x16_t dp = {};
-#pragma unroll
-        for (int e = 0; e < 16; ++e) s[e] = 0.f;
-        for (int x0 = begin - 1; x0 < end; ++x0) {
+        f32x16_t sA = {}, sB = {}, dpA = {}, dpB = {};
+        const auto turn = [&](int x0, f32x16_t &s, f32x16_t &dp, f32x16_t &next, f32x16_t &dnext) {
             const int s1 = slot == 2 ? 0 : slot + 1, s2 = slot == 0 ? 2 : slot - 1;
             float coming = 0.f;
             if (x0 + 2 < end) {
@@ -397,8 +409,11 @@ __global__ __launch_bounds__((128 * BwdLds<T, DP>::QW), (DP * sizeof(T) <= 128 ?
             const int i0 = ROWS * x0 + r0; // the wave's first query
             const bool now = x0 >= begin && i0 < n.nq && i0 + 31 >= mine, then = x0 + 1 < end && i0 + ROWS < n.nq && i0 + ROWS + 31 >= mine;
             if (now || then) {
-                const T *const qrow = qb + s1 * Tl::SIZE, *const grow_t = gb + s1 * Tl::SIZE, *const qcol = qb + slot * Tl::SIZE, *const gcol = gb + slot * Tl::SIZE;
-                const float *const st = stats + slot * 2 * ROWS + r0, *const st1 = stats + s1 * 2 * ROWS + r0;
+                const int row = s1 * Tl::SIZE + rows, colp = slot * Tl::SIZE + cols;
+                // S and dP in turn; dV and dK in turn, 16 rows after 16 rows
+                const auto row_operand = [&](int x) { return Tl::by_rows(x & 1 ? gb : qb, row, r0, x / 2); };
+                const auto col_operand = [&](int x) { return Tl::by_cols(x & 1 ? qb : gb, colp, r0 + 16 * (x / (2 * DB)), x / 2 % DB); };
+                const float *const st = stats + 2 * (slot * ROWS + r0 + 4 * h), *const st1 = stats + 2 * (s1 * ROWS + r0 + 4 * h);
                 const int p0 = i0 + n.start; // the position of the first row
                 const bool edge = j0 + 32 > n.nk || (a.causal && j0 + 31 > p0);
                 const bool near = BIAS && j0 + 31 - p0 > -far && j0 - (p0 + 31) < far;
@@ -414,29 +429,28 @@ __global__ __launch_bounds__((128 * BwdLds<T, DP>::QW), (DP * sizeof(T) <= 128 ?
                     }
                 }
                 const float mul = plain ? sl2 : 1.f, add = plain ? flat : 0.f;
-                f32x16_t next = {}, dnext; // (dP is formed on -delta: dS = P (dP - delta))
 #pragma unroll
-                for (int e = 0; e < 16; e += 4) {
-                    const float4 d4 = *(const float4 *)(st1 + ROWS + 2 * e + 4 * h);
-                    dnext[e] = -d4.x, dnext[e + 1] = -d4.y, dnext[e + 2] = -d4.z, dnext[e + 3] = -d4.w;
+                for (int e = 0; e < 16; e += 2) { // (dP is formed on -delta: dS = P (dP - delta))
+                    const float4 y = *(const float4 *)(st1 + 2 * (8 * (e >> 2) + (e & 3)));
+                    next[e] = next[e + 1] = 0.f;
+                    dnext[e] = -y.y, dnext[e + 1] = -y.w;
                 }
                 Frag<T> ring[AHEAD + 1], fp[2], fs[2];
-                float p[16];
-                float4 l4 = *(const float4 *)(st + 4 * h);
+                f32x16_t p;
+                float4 l2 = *(const float4 *)st;
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int x = 0; x < AHEAD; ++x) ring[x] = Tl::by_rows(x & 1 ? grow_t : qrow, r0, x / 2, lane);
+                for (int x = 0; x < AHEAD; ++x) ring[x] = row_operand(x);
 #pragma unroll
                 for (int x = 0; x < 2 * CH; ++x) {
-                    if (x + AHEAD < 2 * CH) ring[(x + AHEAD) % (AHEAD + 1)] = Tl::by_rows((x + AHEAD) & 1 ? grow_t : qrow, r0, (x + AHEAD) / 2, lane);
+                    if (x + AHEAD < 2 * CH) ring[(x + AHEAD) % (AHEAD + 1)] = row_operand(x + AHEAD);
                     if (x & 1)
                         mma(dnext, ring[x % (AHEAD + 1)], v[x / 2]);
                     else
                         mma(next, ring[x % (AHEAD + 1)], k[x / 2]);
 #pragma unroll
                     for (int e = x * 16 / (2 * CH); e < (x + 1) * 16 / (2 * CH); ++e) {
-                        const float ll = e % 4 == 0 ? l4.x : e % 4 == 1 ? l4.y : e % 4 == 2 ? l4.z : l4.w;
-                        p[e] = exp2_fast(s[e] * mul + (add - ll));
+                        p[e] = exp2_fast(s[e] * mul + (add - (e & 1 ? l2.z : l2.x)));
                         s[e] = p[e] * dp[e];
                         if (e % 8 == 7) {
                             pack(p, e / 8, fp[e / 8]);
@@ -444,18 +458,16 @@ __global__ __launch_bounds__((128 * BwdLds<T, DP>::QW), (DP * sizeof(T) <= 128 ?
                             here(fp[e / 8]);
                             here(fs[e / 8]);
                         }
-                        if (e % 4 == 3 && e < 15) l4 = *(const float4 *)(st + 8 * (e / 4 + 1) + 4 * h);
+                        if ((e & 1) && e < 15) l2 = *(const float4 *)(st + 2 * (8 * ((e + 1) >> 2) + ((e + 1) & 3)));
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 }
                 if (now) {
-                    // step x: rows 16 (x / 2 DB) .., dV and dK in turn
-                    const auto operand = [&](int x) { return Tl::by_cols(x & 1 ? qcol : gcol, r0 + 16 * (x / (2 * DB)), x / 2 % DB, lane); };
 #pragma unroll
-                    for (int x = 0; x < AHEAD; ++x) ring[x] = operand(x);
+                    for (int x = 0; x < AHEAD; ++x) ring[x] = col_operand(x);
 #pragma unroll
                     for (int x = 0; x < 4 * DB; ++x) {
-                        if (x + AHEAD < 4 * DB) ring[(x + AHEAD) % (AHEAD + 1)] = operand(x + AHEAD);
+                        if (x + AHEAD < 4 * DB) ring[(x + AHEAD) % (AHEAD + 1)] = col_operand(x + AHEAD);
                         if (x & 1)
                             mma(dk[x / 2 % DB], ring[x % (AHEAD + 1)], fs[x / (2 * DB)]);
                         else
@@ -463,14 +475,15 @@ __global__ __launch_bounds__((128 * BwdLds<T, DP>::QW), (DP * sizeof(T) <= 128 ?
                         __builtin_amdgcn_sched_barrier(0);
                     }
                 }
-                dp = dnext;
-#pragma unroll
-                for (int e = 0; e < 16; ++e) s[e] = next[e];
             }
-            if (x0 + 2 < end && t < 2 * ROWS) stats[s2 * 2 * ROWS + t] = coming;
+            if (x0 + 2 < end) put_stat(x0 + 2, s2, coming);
             slot = s1;
             fetched();
             __syncthreads();
+        };
+        for (int x0 = begin - 1; x0 < end; x0 += 2) {
+            turn(x0, sA, dpA, sB, dpB);
+            if (x0 + 1 < end) turn(x0 + 1, sB, dpB, sA, dpA);
         }
     }
     if constexpr (QW == 2) { // (the loop ended with a barrier: the tiles' room is free)
@@ -551,7 +564,7 @@ static int attn_bwd_launch(AttnArgs &a, float *dtable, int accumulate, hipStream
         PF_LAUNCH(st, "attn_table", attn_table_kernel, dim3((unsigned)a.buckets * a.Hq), dim3(64), s, a.tab, parts, a.buckets, a.Hq, dtable, accumulate);
     return st;
 }
-static size_t delta_bytes(const pf_attention_desc *d) { return align_up((size_t)d->B * d->heads_q * d->Lq * sizeof(float)); }
+static size_t delta_bytes(const pf_attention_desc *d) { return align_up((size_t)d->B * d->heads_q * d->Lq * 2 * sizeof(float)); }
 
 } // namespace pf
 

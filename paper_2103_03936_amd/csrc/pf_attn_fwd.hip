@@ -37,12 +37,12 @@ __device__ __forceinline__ void attn_fwd_tile(const AttnArgs &a, char *lds, int 
     if (a.causal && mine > 0 && pmax + 1 < mine) mine = pmax + 1 < 0 ? 0 : pmax + 1;
 
     const Tl kl(a.ks[1], a.D, t), vl(a.vs[1], a.D, t);
-    const auto fetch_keys = [&](int k0) { kl.fetch(kb + (k0 / KT & 1) * Tl::SIZE, Kp + (i64)k0 * a.ks[1], a.ks[1], n.nk - k0, a.D, wave); };
-    const auto fetch_values = [&](int k0) { vl.fetch(vb + (k0 / KT & 1) * Tl::SIZE, Vp + (i64)k0 * a.vs[1], a.vs[1], n.nk - k0, a.D, wave); };
+    const auto fetch_keys = [&](int k0, int odd) { kl.fetch(kb + odd * Tl::SIZE, Kp + (i64)k0 * a.ks[1], a.ks[1], n.nk - k0, a.D, wave); };
+    const auto fetch_values = [&](int k0, int odd) { vl.fetch(vb + odd * Tl::SIZE, Vp + (i64)k0 * a.vs[1], a.vs[1], n.nk - k0, a.D, wave); };
     if (keys > 0) {
-        fetch_keys(0);
-        fetch_values(0);
-        if (keys > KT) fetch_keys(KT);
+        fetch_keys(0, 0);
+        fetch_values(0, 0);
+        if (keys > KT) fetch_keys(KT, 1);
         if constexpr (BIAS) fill_bias(a, bias, head, t, 256);
     }
     Frag<T> q[DP / 16];
@@ -57,29 +57,28 @@ __device__ __forceinline__ void attn_fwd_tile(const AttnArgs &a, char *lds, int 
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d) o[d] = f32x16_t{};
     float m = -INFINITY, sum = 0.f; // the maximum that values are taken relative to (base 2); the sum of the lane's keys
-    float s[SUB][16], top = -INFINITY;
+    float top = -INFINITY;
+    f32x16_t s0[SUB], s1[SUB];
+    const int rows = Tl::row_place(lane), cols = Tl::col_place(lane);
+    constexpr int CH = DP / 16, SC = SUB * CH, DB = DP / 32, PV = 2 * SUB * DB, AHEAD = 3;
     fetched();
     __syncthreads();
     if (mine > 0) {
 #pragma unroll
         for (int u = 0; u < SUB; ++u) {
-            f32x16_t acc = {};
+            s0[u] = f32x16_t{};
 #pragma unroll
-            for (int c = 0; c < DP / 16; ++c) mma(acc, Tl::by_rows(kb, 32 * u, c, lane), q[c]);
+            for (int c = 0; c < CH; ++c) mma(s0[u], Tl::by_rows(kb, rows, 32 * u, c), q[c]);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) s[u][e] = acc[e];
+            for (int e = 0; e < 16; ++e) top = fmaxf(top, s0[u][e]);
         }
-#pragma unroll
-        for (int u = 0; u < SUB; ++u)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) top = fmaxf(top, s[u][e]);
     }
     __syncthreads();
-    for (int k0 = 0; k0 < keys; k0 += KT) {
-        if (k0 + 2 * KT < keys) fetch_keys(k0 + 2 * KT);
-        if (k0 + KT < keys) fetch_values(k0 + KT);
+    // keys k0 .. with their scores in s; `odd`: which of the two tiles they are in
+    const auto turn = [&](int k0, int odd, f32x16_t (&s)[SUB], f32x16_t (&next)[SUB]) {
+        if (k0 + 2 * KT < keys) fetch_keys(k0 + 2 * KT, odd);
+        if (k0 + KT < keys) fetch_values(k0 + KT, !odd);
         if (k0 < mine) {
-            const T *const knext = kb + (k0 / KT + 1 & 1) * Tl::SIZE, *const vt = vb + (k0 / KT & 1) * Tl::SIZE;
             const bool edge = k0 + KT > n.nk || (a.causal && k0 + KT - 1 > pmin);
             const bool near = BIAS && k0 + KT - 1 - pmin > -far && k0 - pmax < far;
             const float flat = BIAS ? bias[k0 >= pmin ? 2 * far : 0] : 0.f; // where no key is near
@@ -108,33 +107,31 @@ __device__ __forceinline__ void attn_fwd_tile(const AttnArgs &a, char *lds, int 
                 const float m_new = fmaxf(m, top), f = exp2_fast(m - (m_new == -INFINITY ? 0.f : m_new));
                 sum *= f;
 #pragma unroll
-                for (int d = 0; d < DP / 32; ++d)
+                for (int d = 0; d < DB; ++d)
 #pragma unroll
                     for (int e = 0; e < 16; ++e) o[d][e] *= f;
                 m = m_new;
             }
             const float base = m == -INFINITY ? 0.f : m, mul = plain ? sl2 : 1.f, add = plain ? flat - base : -base;
-            // The order of what follows is fixed step by step: a step is one product of each kind, the read of the operand of the
-            // product AHEAD steps on, and a share of the vector instructions.
-            constexpr int CH = DP / 16, SC = SUB * CH, DB = DP / 32, PV = 2 * SUB * DB;
-            constexpr int AHEAD = 3;
+            // The order of what follows is fixed step by step: a step is one product, the read of the operand of the product
+            // AHEAD steps on, and a share of the vector instructions.
             Frag<T> p[2 * SUB], ring[AHEAD + 1];
             float part[4] = {0.f, 0.f, 0.f, 0.f};
-            f32x16_t next[SUB];
 #pragma unroll
             for (int u = 0; u < SUB; ++u) next[u] = f32x16_t{};
             __builtin_amdgcn_sched_barrier(0);
             // the next keys' scores (of whatever lies there, after the last) beside this tile's exponentials
+            const int ka = rows + (odd ? 0 : Tl::SIZE), va = cols + (odd ? Tl::SIZE : 0);
 #pragma unroll
-            for (int x = 0; x < AHEAD; ++x) ring[x] = Tl::by_rows(knext, 32 * (x / CH), x % CH, lane);
+            for (int x = 0; x < AHEAD; ++x) ring[x] = Tl::by_rows(kb, ka, 32 * (x / CH), x % CH);
 #pragma unroll
             for (int x = 0; x < SC; ++x) {
-                if (x + AHEAD < SC) ring[(x + AHEAD) % (AHEAD + 1)] = Tl::by_rows(knext, 32 * ((x + AHEAD) / CH), (x + AHEAD) % CH, lane);
+                if (x + AHEAD < SC) ring[(x + AHEAD) % (AHEAD + 1)] = Tl::by_rows(kb, ka, 32 * ((x + AHEAD) / CH), (x + AHEAD) % CH);
                 mma(next[x / CH], ring[x % (AHEAD + 1)], q[x % CH]);
 #pragma unroll
                 for (int y = x * (16 * SUB) / SC; y < (x + 1) * (16 * SUB) / SC; ++y) {
-                    float &z = s[y / 16][y % 16];
-                    z = exp2_fast(z * mul + add);
+                    const float z = exp2_fast(s[y / 16][y % 16] * mul + add);
+                    s[y / 16][y % 16] = z;
                     part[y & 3] += z;
                     if (y % 8 == 7) pack(s[y / 16], y % 16 / 8, p[y / 8]);
                 }
@@ -143,22 +140,23 @@ __device__ __forceinline__ void attn_fwd_tile(const AttnArgs &a, char *lds, int 
             // P and V beside the largest of the next scores
             top = -INFINITY;
 #pragma unroll
-            for (int x = 0; x < AHEAD; ++x) ring[x] = Tl::by_cols(vt, 16 * (x / DB), x % DB, lane);
+            for (int x = 0; x < AHEAD; ++x) ring[x] = Tl::by_cols(vb, va, 16 * (x / DB), x % DB);
 #pragma unroll
             for (int x = 0; x < PV; ++x) {
-                if (x + AHEAD < PV) ring[(x + AHEAD) % (AHEAD + 1)] = Tl::by_cols(vt, 16 * ((x + AHEAD) / DB), (x + AHEAD) % DB, lane);
+                if (x + AHEAD < PV) ring[(x + AHEAD) % (AHEAD + 1)] = Tl::by_cols(vb, va, 16 * ((x + AHEAD) / DB), (x + AHEAD) % DB);
                 mma(o[x % DB], ring[x % (AHEAD + 1)], p[x / DB]);
 #pragma unroll
-                for (int y = x * (16 * SUB) / PV; y < (x + 1) * (16 * SUB) / PV; ++y) {
-                    s[y / 16][y % 16] = next[y / 16][y % 16];
-                    top = fmaxf(top, s[y / 16][y % 16]);
-                }
+                for (int y = x * (16 * SUB) / PV; y < (x + 1) * (16 * SUB) / PV; ++y) top = fmaxf(top, next[y / 16][y % 16]);
                 __builtin_amdgcn_sched_barrier(0);
             }
             sum += (part[0] + part[1]) + (part[2] + part[3]);
         }
         fetched();
         __syncthreads();
+    };
+    for (int k0 = 0; k0 < keys; k0 += 2 * KT) {
+        turn(k0, 0, s0, s1);
+        if (k0 + KT < keys) turn(k0 + KT, 1, s1, s0);
     }
     sum += __shfl_xor(sum, 32);
     if (i >= a.Lq) return;

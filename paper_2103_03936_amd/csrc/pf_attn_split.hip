@@ -66,6 +66,7 @@ __global__ __launch_bounds__(64 * SPLIT_WAVES<T>) void attn_split_kernel(AttnArg
     float m = -INFINITY, sum = 0.f;
 
     const Tl vl(a.vs[1], a.D, lane);
+    const int cols = Tl::col_place(lane);
     Frag<T> kr[DP / 16];
     const uint32_t kat = (uint32_t)(col * (int)a.ks[1]) * (uint32_t)sizeof(T);
     const auto fetch = [&](int k, int turn) {
@@ -87,7 +88,8 @@ __global__ __launch_bounds__(64 * SPLIT_WAVES<T>) void attn_split_kernel(AttnArg
         const bool edge = k0 + 32 > n.nk || (a.causal && k0 + 31 > pmin);
         const bool near = BIAS && k0 + 31 - pmin > -far && k0 - pmax < far;
         const float flat = k0 >= pmin ? flat_after : flat_before;
-        float s[16], top = -INFINITY;
+        f32x16_t s;
+        float top = -INFINITY;
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
             const int j = k0 + 8 * (e >> 2) + 4 * h + (e & 3);
@@ -123,7 +125,7 @@ __global__ __launch_bounds__(64 * SPLIT_WAVES<T>) void attn_split_kernel(AttnArg
             Frag<T> p;
             pack(s, c, p);
 #pragma unroll
-            for (int d = 0; d < DP / 32; ++d) mma(o[d], Tl::by_cols(vt, 16 * c, d, lane), p);
+            for (int d = 0; d < DP / 32; ++d) mma(o[d], Tl::by_cols(vt, cols, 16 * c, d), p);
         }
     }
     sum += __shfl_xor(sum, 32);

@@ -80,6 +80,7 @@ struct BufSrc {
         const v4 v = __builtin_amdgcn_raw_buffer_load_b128(r, (int)at, 0, 0);
         return make_uint4(v.x, v.y, v.z, v.w);
     }
+    __device__ __forceinline__ float load4(uint32_t at) const { return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(r, (int)at, 0, 0)); }
     __device__ __forceinline__ void store(uint32_t at, uint4 u) const
     {
         typedef unsigned int v4 __attribute__((ext_vector_type(4)));
