@@ -145,6 +145,12 @@ __device__ __forceinline__ void put4(bf16_t *p, float a, float b, float c, float
 }
 
 // ------------------------------------------------------------------ tiles
+// The transposing read.  __restrict__: nothing writes there meanwhile; without it every such read waits for all fetches into
+// LDS that are on their way (so does a read of a struct such as float4, which is why the tiles and tables here are read as
+// vectors of the language)
+typedef __attribute__((address_space(3))) bf16x4_t LdsBf16x4;
+__device__ inline bf16x4_t read_turned(const LdsBf16x4 *__restrict__ p) { return __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LdsBf16x4 *)p); }
+
 // ROWS rows of DP columns in LDS, fetched by THREADS threads straight into it (no registers; a wave's fetches end with
 // fetched()).  A fetch puts the lanes' 16-byte pieces one after the other, so there is no padding: piece c of row r lies at
 // c ^ turn(r).  The tile is read in two ways, as an operand by rows (bf16: 16 lanes that a cycle serves have one piece of 16
@@ -213,8 +219,9 @@ struct Tile {
         if constexpr (sizeof(T) == 2) {
             f.v = *(const bf16x8_t *)p;
         } else {
-            const float4 x = *(const float4 *)p, y = *(const float4 *)(lds + (at ^ (16 * c + 8)) + r0 * PITCH);
-            f.v[0] = x.x, f.v[1] = x.y, f.v[2] = x.z, f.v[3] = x.w, f.v[4] = y.x, f.v[5] = y.y, f.v[6] = y.z, f.v[7] = y.w;
+            const f32x4_t x = *(const f32x4_t *)p, y = *(const f32x4_t *)(lds + (at ^ (16 * c + 8)) + r0 * PITCH);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) f.v[e] = x[e], f.v[4 + e] = y[e];
         }
         return f;
     }
@@ -224,9 +231,8 @@ struct Tile {
     {
         Frag<T> f;
         if constexpr (sizeof(T) == 2) {
-            typedef __attribute__((address_space(3))) bf16x4_t *lds_ptr;
             const T *const lo = lds + (at ^ (32 * d)) + r0 * PITCH, *const hi = lds + (at ^ (32 * d + turn(8) * VEC)) + (r0 + 8) * PITCH;
-            const bf16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_ptr)lo), y = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_ptr)hi);
+            const bf16x4_t x = read_turned((const LdsBf16x4 *)lo), y = read_turned((const LdsBf16x4 *)hi);
 #pragma unroll
             for (int e = 0; e < 4; ++e) f.v[e] = x[e], f.v[4 + e] = y[e];
         } else {
@@ -276,6 +282,20 @@ __device__ __forceinline__ float bias_of(const AttnArgs &a, int bucket, int head
 __device__ __forceinline__ void fill_bias(const AttnArgs &a, float *bias, int head, int t, int threads)
 {
     for (int i = t; i <= 2 * a.bk.far; i += threads) bias[i] = bias_of(a, bucket_of(a, i - a.bk.far), head);
+}
+
+// Scores of a block at an edge or near the diagonal: s scale + bias (base 2) - less; register e holds the distance
+// rel + step (8 (e / 4) + e % 4), what is further than `most` is not seen
+template <bool BIAS>
+__device__ __forceinline__ void finish_scores(f32x16_t &s, float scale, float less, const float *bias, int far, int rel, int step, int most)
+{
+    float y[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) y[e] = BIAS ? bias[clamped(rel + step * (8 * (e >> 2) + (e & 3)), -far, far) + far] : 0.f;
+    __builtin_amdgcn_sched_barrier(0); // (all reads first)
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+        s[e] = fminf(s[e] * scale + (y[e] - less), rel + step * (8 * (e >> 2) + (e & 3)) > most ? -INFINITY : INFINITY);
 }
 
 // XCDs take workgroups in turn: consecutive pieces of work (the tiles of a head, which share keys and values) go to one XCD

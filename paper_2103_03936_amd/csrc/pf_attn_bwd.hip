@@ -21,13 +21,15 @@ constexpr int DIAG = 32 * 64;
 template <typename T, int DP>
 struct BwdLds {
     using Tq = Tile<T, DP, 32, 256>;
-    static size_t dq(int far, bool bias, bool tab)
+    static size_t dq(int far, bool tab)
     {
-        return 5 * Tq::BYTES + (bias ? (2 * far + 1) * 4 : 0) + (tab ? 4 * DIAG * 4 + 4 * (2 * far + 1) * 4 : 0);
+        // three groups of keys, two of values; then (over them) two of each and the waves' blocks
+        const size_t first = 5 * Tq::BYTES, second = 4 * Tq::BYTES + 4 * DIAG * 4;
+        return tab ? 4 * (2 * far + 1) * 4 + (second > first ? second : first) : first;
     }
     // dK and dV: how many waves share the queries (what six tiles of float rows take leaves room for one)
     static constexpr int QW = sizeof(T) == 4 && DP > 64 ? 1 : 2;
-    static size_t dkv(int far, bool bias) { return 6 * QW * Tq::BYTES + 3 * 2 * 32 * QW * 4 + (bias ? (2 * far + 1) * 4 : 0); }
+    static size_t dkv() { return 6 * QW * Tq::BYTES; }
 };
 
 // dQ, delta and the sums of dS by distance, for one tile of 128 queries of one head.  TAB: with the gradient of the table.
@@ -41,14 +43,15 @@ struct BwdLds {
 // second pass goes over the near blocks alone, for their dS with the delta that is now exact (S and dP, two products of the
 // first pass's three); the far sums are put right by their sums of P.
 template <typename T, int DP, bool BIAS, bool TAB>
-__device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b, int head, int tile)
+__device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, float *bias, int b, int head, int tile)
 {
     using Tl = Tile<T, DP, 32, 256>;
     constexpr int CH = DP / 16, DB = DP / 32, AHEAD = 2;
     const int far = a.bk.far, span = 2 * far + 1;
     T *const kb = (T *)lds, *const vb = kb + 3 * Tl::SIZE;
-    float *const bias = (float *)(lds + 5 * Tl::BYTES);
-    float *const diag_all = bias + span, *const sums_all = diag_all + 4 * DIAG; // a wave's block, a wave's [span]
+    // the waves' blocks of dS (second pass), their sums by distance [span]
+    float *const diag_all = (float *)(lds + 4 * Tl::BYTES);
+    float *const sums_all = (float *)(lds + (4 * Tl::BYTES + 4 * DIAG * 4 > 5 * Tl::BYTES ? 4 * Tl::BYTES + 4 * DIAG * 4 : 5 * Tl::BYTES));
 
     const int t = threadIdx.x, wave = wave_of(t), lane = t & 63, col = lane & 31, h = lane >> 5;
     float *const diag = diag_all + wave * DIAG, *const sums = sums_all + wave * span;
@@ -68,7 +71,7 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b
 
     if (BIAS && keys > 0) fill_bias(a, bias, head, t, 256);
     if constexpr (TAB)
-        for (int x = t; x < 4 * (DIAG + span); x += 256) diag_all[x] = 0.f;
+        for (int x = t; x < 4 * span; x += 256) sums_all[x] = 0.f;
     const i64 at = (((i64)b * a.Lq + i) * a.Hq + head) * a.D, stat = ((i64)b * a.Hq + head) * a.Lq + i;
     Frag<T> q[CH], g[CH];
     float delta = 0.f;
@@ -103,16 +106,7 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b
         kl.fetch(kb + kslot * Tl::SIZE, Kp + (i64)(32 * j) * a.ks[1], a.ks[1], n.nk - 32 * j, a.D, wave);
         vl.fetch(vb + vslot * Tl::SIZE, Vp + (i64)(32 * j) * a.vs[1], a.vs[1], n.nk - 32 * j, a.D, wave);
     };
-    // the scores of a block at an edge or near the diagonal, with bias and masks, less lse
-    const auto finish = [&](f32x16_t &s, int k0) {
-        const int rel = anew(k0 + 4 * h - pos); // distance of the first key that the lane holds
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const int x = rel + 8 * (e >> 2) + (e & 3);
-            s[e] = s[e] * sl2 + ((BIAS ? bias[clamped(x, -far, far) + far] : 0.f) - lse2);
-            if (x > most) s[e] = -INFINITY;
-        }
-    };
+    const auto finish = [&](f32x16_t &s, int k0) { finish_scores<BIAS>(s, sl2, lse2, bias, far, anew(k0 + 4 * h - pos), 1, most); };
     const int groups = (keys + 31) / 32; // of 32 keys
     if (groups > 0) {
         fetch(0, 0, 0);
@@ -220,6 +214,8 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b
     }
     if (i < a.Lq && h == 0) *(float2 *)(a.delta + 2 * stat) = make_float2(lse2, ok ? delta : 0.f);
     if constexpr (TAB) {
+        // (two groups of keys, two of values)
+        const auto fetch2 = [&](int j) { fetch(j, j & 1, (j & 1) - 1); };
         // the near blocks once more: 32 begin + 31 > first position - far, 32 (end - 1) < last position + far
         int begin = 0, end = groups;
         const int lo = tile * 128 + n.start - far - 31, hi = block_last + far;
@@ -229,13 +225,14 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b
         else if ((hi + 31) / 32 < end)
             end = (hi + 31) / 32;
         if (begin < end) {
-            fetch(begin, begin & 1, begin & 1);
+            for (int x = t; x < 4 * DIAG; x += 256) diag_all[x] = 0.f;
+            fetch2(begin);
             fetched();
             __syncthreads();
         }
         for (int j = begin; j < end; ++j) {
             const int k0 = 32 * j;
-            if (j + 1 < end) fetch(j + 1, (j + 1) & 1, (j + 1) & 1);
+            if (j + 1 < end) fetch2(j + 1);
             if (k0 < mine && near_at(k0)) {
                 const int at_j = (j & 1) * Tl::SIZE + rows;
                 f32x16_t s = {}, dp;
@@ -244,7 +241,7 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b
 #pragma unroll
                 for (int c = 0; c < CH; ++c) {
                     mma(s, Tl::by_rows(kb, at_j, 0, c), q[c]);
-                    mma(dp, Tl::by_rows(vb, at_j, 0, c), g[c]);
+                    mma(dp, Tl::by_rows(kb + 2 * Tl::SIZE, at_j, 0, c), g[c]);
                 }
                 finish(s, k0);
                 // along the diagonals of the block
@@ -315,12 +312,13 @@ template <typename T, int DP, bool BIAS, bool TAB>
 __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void attn_dq_kernel(AttnArgs a, int paired)
 {
     extern __shared__ __attribute__((aligned(16))) char lds[];
+    __shared__ float bias[BIAS ? 2 * ATTN_MAX_DISTANCE + 1 : 1]; // (an object of its own: see attn_dkv_kernel)
     const unsigned w = xcd_order(blockIdx.x, gridDim.x);
     const int each = paired ? (a.tiles + 1) / 2 : a.tiles, k = (int)(w % each), bh = w / each, b = bh / a.Hq, head = bh - b * a.Hq;
     const int count = paired && a.tiles - 1 - k != k ? 2 : 1;
 #pragma unroll 1
     for (int x = 0; x < count; ++x) {
-        attn_dq_tile<T, DP, BIAS, TAB>(a, lds, b, head, x ? k : a.tiles - 1 - k);
+        attn_dq_tile<T, DP, BIAS, TAB>(a, lds, bias, b, head, x ? k : a.tiles - 1 - k);
         __syncthreads();
     }
 }
@@ -338,8 +336,9 @@ __global__ __launch_bounds__((128 * BwdLds<T, DP>::QW), (DP * sizeof(T) <= 128 ?
     constexpr int CH = DP / 16, DB = DP / 32, AHEAD = 3;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     T *const qb = (T *)lds, *const gb = qb + 3 * Tl::SIZE;
-    float *const stats = (float *)(lds + 6 * Tl::BYTES); // [3][ROWS][2]: lse (base 2) and delta of each query
-    float *const bias = stats + 3 * 2 * ROWS;
+    // (objects of their own: a read from the array that fetches go to would wait for them)
+    __shared__ __attribute__((aligned(16))) float stats[3 * 2 * ROWS]; // lse (base 2) and delta of each query
+    __shared__ float bias[BIAS ? 2 * ATTN_MAX_DISTANCE + 1 : 1];
 
     const unsigned w = xcd_order(blockIdx.x, gridDim.x);
     const int tile = (int)(w % a.tiles), bk = w / a.tiles, b = bk / a.Hkv, kv = bk - b * a.Hkv;
@@ -383,14 +382,14 @@ __global__ __launch_bounds__((128 * BwdLds<T, DP>::QW), (DP * sizeof(T) <= 128 ?
             ql.fetch(qb + slot * Tl::SIZE, Qp + (i64)(ROWS * x) * a.qs[1], a.qs[1], n.nq - ROWS * x, a.D, wave);
             gl.fetch(gb + slot * Tl::SIZE, Gp + (i64)(ROWS * x) * grow, grow, n.nq - ROWS * x, a.D, wave);
         };
-        // value t of the group's [ROWS][2]
+        // thread t: lse (t even) or delta of query t / 2 of the group
         const auto stat_of = [&](int x) {
             const int left = a.Lq - ROWS * x;
             const BufSrc src(a.delta + 2 * (stat + ROWS * x), 8 * (left < ROWS ? left : ROWS));
             return src.load4(t < 2 * ROWS ? 4 * t : BUF_OUT);
         };
         const auto put_stat = [&](int x, int slot, float y) { // (behind the last query: lse = infinity, P = 0)
-            if (t < 2 * ROWS) stats[slot * 2 * ROWS + t] = !(t & 1) && ROWS * x + t / 2 >= a.Lq ? INFINITY : y;
+            if (t < 2 * ROWS) stats[(2 * slot + (t & 1)) * ROWS + t / 2] = !(t & 1) && ROWS * x + t / 2 >= a.Lq ? INFINITY : y;
         };
         if constexpr (BIAS) fill_bias(a, bias, head, t, THREADS);
         int slot = (begin + 2) % 3;
@@ -413,31 +412,23 @@ __global__ __launch_bounds__((128 * BwdLds<T, DP>::QW), (DP * sizeof(T) <= 128 ?
                 // S and dP in turn; dV and dK in turn, 16 rows after 16 rows
                 const auto row_operand = [&](int x) { return Tl::by_rows(x & 1 ? gb : qb, row, r0, x / 2); };
                 const auto col_operand = [&](int x) { return Tl::by_cols(x & 1 ? qb : gb, colp, r0 + 16 * (x / (2 * DB)), x / 2 % DB); };
-                const float *const st = stats + 2 * (slot * ROWS + r0 + 4 * h), *const st1 = stats + 2 * (s1 * ROWS + r0 + 4 * h);
+                const float *const st = stats + 2 * slot * ROWS + r0 + 4 * h, *const st1 = stats + (2 * s1 + 1) * ROWS + r0 + 4 * h;
                 const int p0 = i0 + n.start; // the position of the first row
                 const bool edge = j0 + 32 > n.nk || (a.causal && j0 + 31 > p0);
                 const bool near = BIAS && j0 + 31 - p0 > -far && j0 - (p0 + 31) < far;
                 const float flat = BIAS ? bias[j0 >= p0 ? 2 * far : 0] : 0.f;
                 const bool plain = !edge && !near;
-                if (now && !plain) {
-                    const int rel = anew(j - p0 - 4 * h); // distance of the first query that the lane holds
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int x = rel - 8 * (e >> 2) - (e & 3);
-                        s[e] = s[e] * sl2 + (BIAS ? bias[clamped(x, -far, far) + far] : 0.f);
-                        if (x > most) s[e] = -INFINITY;
-                    }
-                }
+                if (now && !plain) finish_scores<BIAS>(s, sl2, 0.f, bias, far, anew(j - p0 - 4 * h), -1, most);
                 const float mul = plain ? sl2 : 1.f, add = plain ? flat : 0.f;
 #pragma unroll
-                for (int e = 0; e < 16; e += 2) { // (dP is formed on -delta: dS = P (dP - delta))
-                    const float4 y = *(const float4 *)(st1 + 2 * (8 * (e >> 2) + (e & 3)));
-                    next[e] = next[e + 1] = 0.f;
-                    dnext[e] = -y.y, dnext[e + 1] = -y.w;
+                for (int e = 0; e < 16; e += 4) { // (dP is formed on -delta: dS = P (dP - delta))
+                    const f32x4_t y = *(const f32x4_t *)(st1 + 2 * e);
+                    next[e] = next[e + 1] = next[e + 2] = next[e + 3] = 0.f;
+                    dnext[e] = -y[0], dnext[e + 1] = -y[1], dnext[e + 2] = -y[2], dnext[e + 3] = -y[3];
                 }
                 Frag<T> ring[AHEAD + 1], fp[2], fs[2];
                 f32x16_t p;
-                float4 l2 = *(const float4 *)st;
+                f32x4_t l4 = *(const f32x4_t *)st;
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int x = 0; x < AHEAD; ++x) ring[x] = row_operand(x);
@@ -450,7 +441,7 @@ __global__ __launch_bounds__((128 * BwdLds<T, DP>::QW), (DP * sizeof(T) <= 128 ?
                         mma(next, ring[x % (AHEAD + 1)], k[x / 2]);
 #pragma unroll
                     for (int e = x * 16 / (2 * CH); e < (x + 1) * 16 / (2 * CH); ++e) {
-                        p[e] = exp2_fast(s[e] * mul + (add - (e & 1 ? l2.z : l2.x)));
+                        p[e] = exp2_fast(s[e] * mul + (add - l4[e % 4]));
                         s[e] = p[e] * dp[e];
                         if (e % 8 == 7) {
                             pack(p, e / 8, fp[e / 8]);
@@ -458,7 +449,7 @@ __global__ __launch_bounds__((128 * BwdLds<T, DP>::QW), (DP * sizeof(T) <= 128 ?
                             here(fp[e / 8]);
                             here(fs[e / 8]);
                         }
-                        if ((e & 1) && e < 15) l2 = *(const float4 *)(st + 2 * (8 * ((e + 1) >> 2) + ((e + 1) & 3)));
+                        if (e % 4 == 3 && e < 15) l4 = *(const f32x4_t *)(st + 2 * (e + 1));
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 }
@@ -542,7 +533,7 @@ static int attn_bwd_launch(AttnArgs &a, float *dtable, int accumulate, hipStream
     const int parts = a.B * a.tiles;
     const int paired = a.causal && (i64)a.B * a.Hq * a.tiles > 512; // (two workgroups to a compute unit are resident)
     const dim3 grid((unsigned)a.B * a.Hq * (paired ? (a.tiles + 1) / 2 : a.tiles));
-    const size_t lds = BwdLds<T, DP>::dq(a.bk.far, bias, tab);
+    const size_t lds = BwdLds<T, DP>::dq(a.bk.far, tab);
     if (a.Lq > 0) {
         if (tab)
             PF_LAUNCH_LDS(st, "attn_dq_tab", (attn_dq_kernel<T, DP, true, true>), grid, dim3(256), lds, s, a, paired);
@@ -554,7 +545,7 @@ static int attn_bwd_launch(AttnArgs &a, float *dtable, int accumulate, hipStream
     if (a.Lk > 0) {
         a.tiles = (a.Lk + 63) / 64;
         const dim3 kgrid((unsigned)a.B * a.Hkv * a.tiles);
-        const size_t klds = BwdLds<T, DP>::dkv(a.bk.far, bias);
+        const size_t klds = BwdLds<T, DP>::dkv();
         if (bias)
             PF_LAUNCH_LDS(st, "attn_dkv", (attn_dkv_kernel<T, DP, true>), kgrid, dim3(128 * BwdLds<T, DP>::QW), klds, s, a);
         else
