@@ -18,7 +18,7 @@ struct AttnArgs {
     const void *Q, *K, *V, *dO, *Oin;
     void *O, *dQ, *dK, *dV;
     const float *table, *lse_in;
-    float *lse, *delta, *tab; // delta[B, Hq, Lq][2]: lse (base 2; infinity where a query takes no part) and delta; tab[Hq][B * tiles][buckets]: sums of dS per workgroup
+    float *lse, *delta, *tab; // delta[B, Hq, Lq][2]: lse (base 2; infinity where a query takes no part) and -delta; tab[Hq][B * tiles][buckets]: sums of dS per workgroup
     const int *q_start, *q_len, *kv_len;
     int B, Lq, Lk, Hq, Hkv, G, D, causal, buckets, two_sided, tiles;
     float scale;
@@ -194,52 +194,54 @@ struct Tile {
             if (PIECES % THREADS == 0 || i * THREADS + wave * 64 < PIECES)
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(src.r, (lds_ptr)((char *)lds + (i * THREADS + wave * 64) * 16), 16, (int)at[i], 0, 0, 0);
     }
-    // Where a lane reads.  turn() permutes bits, so that a step along a row is an exclusive or of the place: one number for a lane
-    // and constants, not an address for every read.
+    // Where a lane reads, in bytes from the tile's start.  turn() permutes bits, so that a step along a row is an exclusive or of
+    // the place (tiles lie at multiples of their rows' lengths): one number for a lane and constants, not an address for every read.
+    static constexpr int RB = PITCH * (int)sizeof(T); // bytes from one row to the next
     static __device__ __forceinline__ int row_place(int lane)
     {
         const int row = lane & 31;
-        return row * PITCH + ((lane >> 5) ^ turn(row)) * VEC;
+        return row * RB + ((lane >> 5) ^ turn(row)) * 16;
     }
     static __device__ __forceinline__ int col_place(int lane)
     {
         if constexpr (sizeof(T) == 2) {
             const int g = lane >> 4, i = lane & 15, row = 4 * (g >> 1) + (i >> 2);
-            return row * PITCH + ((2 * (g & 1) + (i >> 1 & 1)) ^ turn(row)) * VEC + 4 * (i & 1);
+            return row * RB + ((2 * (g & 1) + (i >> 1 & 1)) ^ turn(row)) * 16 + 8 * (i & 1);
         }
         const int row = 4 * (lane >> 5);
-        return row * PITCH + ((lane >> 2 & 7) ^ turn(row)) * VEC + (lane & 3);
+        return row * RB + ((lane >> 2 & 7) ^ turn(row)) * 16 + 4 * (lane & 3);
     }
     // Operand with the index along the 32 rows from r0 on and the contraction along columns 16 c ..; at: row_place plus the
-    // elements from `lds` to the tile
-    static __device__ __forceinline__ Frag<T> by_rows(const T *lds, int at, int r0, int c)
+    // bytes from `lds` to the tile
+    static __device__ __forceinline__ Frag<T> by_rows(const char *lds, int at, int r0, int c)
     {
         Frag<T> f;
-        const T *const p = lds + (at ^ (16 * c)) + r0 * PITCH;
+        const char *const p = lds + r0 * RB;
         if constexpr (sizeof(T) == 2) {
-            f.v = *(const bf16x8_t *)p;
+            f.v = *(const bf16x8_t *)(p + (at ^ (32 * c)));
         } else {
-            const f32x4_t x = *(const f32x4_t *)p, y = *(const f32x4_t *)(lds + (at ^ (16 * c + 8)) + r0 * PITCH);
+            const f32x4_t x = *(const f32x4_t *)(p + (at ^ (64 * c))), y = *(const f32x4_t *)(p + (at ^ (64 * c + 32)));
 #pragma unroll
             for (int e = 0; e < 4; ++e) f.v[e] = x[e], f.v[4 + e] = y[e];
         }
         return f;
     }
     // Operand with the index along the columns 32 d .. 32 d + 31 and the contraction along rows r0 .. r0 + 15 (r0 a multiple
-    // of 16), in the order in which a product's result lies in the lanes; at: col_place plus the elements to the tile
-    static __device__ __forceinline__ Frag<T> by_cols(const T *lds, int at, int r0, int d)
+    // of 16), in the order in which a product's result lies in the lanes; at: col_place plus the bytes to the tile
+    static __device__ __forceinline__ Frag<T> by_cols(const char *lds, int at, int r0, int d)
     {
         Frag<T> f;
+        const char *const p = lds + r0 * RB;
         if constexpr (sizeof(T) == 2) {
-            const T *const lo = lds + (at ^ (32 * d)) + r0 * PITCH, *const hi = lds + (at ^ (32 * d + turn(8) * VEC)) + (r0 + 8) * PITCH;
-            const bf16x4_t x = read_turned((const LdsBf16x4 *)lo), y = read_turned((const LdsBf16x4 *)hi);
+            const bf16x4_t x = read_turned((const LdsBf16x4 *)(p + (at ^ (64 * d)))),
+                           y = read_turned((const LdsBf16x4 *)(p + 8 * RB + (at ^ (64 * d + 16 * turn(8)))));
 #pragma unroll
             for (int e = 0; e < 4; ++e) f.v[e] = x[e], f.v[4 + e] = y[e];
         } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const int row = (e & 3) + 8 * (e >> 2);
-                f.v[e] = lds[(at ^ (32 * d + turn(row) * VEC)) + (r0 + row) * PITCH];
+                f.v[e] = *(const float *)(p + row * RB + (at ^ (128 * d + 16 * turn(row))));
             }
         }
         return f;

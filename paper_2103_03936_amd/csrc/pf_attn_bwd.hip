@@ -121,9 +121,11 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, float
         if (j + 2 < groups) fetch(j + 2, s2, j & 1);
         const bool now = j >= 0 && k0 < mine, then = k0 + 32 < mine;
         if (now || then) {
-            const int krow = s1 * Tl::SIZE + rows, vrow = ((j + 1) & 1) * Tl::SIZE + rows, kcol = slot * Tl::SIZE + cols;
-            const auto row_operand = [&](int x) { return Tl::by_rows(x & 1 ? vb : kb, x & 1 ? vrow : krow, 0, x / 2); };
-            const auto col_operand = [&](int x) { return Tl::by_cols(kb, kcol, 16 * (x / DB), x % DB); };
+            const int krow = s1 * Tl::BYTES + rows, vrow = (3 + ((j + 1) & 1)) * Tl::BYTES + rows, kcol = slot * Tl::BYTES + cols;
+            // S and dP in turn, then dQ: 16 keys after 16 keys
+            const auto operand = [&](int x) {
+                return x < 2 * CH ? Tl::by_rows(lds, x & 1 ? vrow : krow, 0, x / 2) : Tl::by_cols(lds, kcol, 16 * ((x - 2 * CH) / DB), (x - 2 * CH) % DB);
+            };
             const bool near = near_at(k0), plain = !near && k0 + 32 <= n.nk && !(a.causal && k0 + 31 > pmin);
             const float flat = BIAS ? bias[k0 >= pmin ? 2 * far : 0] : 0.f;
             if (now && !plain) finish(s, k0);
@@ -136,10 +138,10 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, float
             __builtin_amdgcn_sched_barrier(0);
             // S and dP of the next keys (step 2 c: S, columns 16 c ..; 2 c + 1: dP) beside dS of these
 #pragma unroll
-            for (int x = 0; x < AHEAD; ++x) ring[x] = row_operand(x);
+            for (int x = 0; x < AHEAD; ++x) ring[x] = operand(x);
 #pragma unroll
             for (int x = 0; x < 2 * CH; ++x) {
-                if (x + AHEAD < 2 * CH) ring[(x + AHEAD) % (AHEAD + 1)] = row_operand(x + AHEAD);
+                ring[(x + AHEAD) % (AHEAD + 1)] = operand(x + AHEAD);
                 if (x & 1)
                     mma(dnext, ring[x % (AHEAD + 1)], g[x / 2]);
                 else
@@ -174,11 +176,9 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, float
                 }
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int x = 0; x < AHEAD; ++x) ring[x] = col_operand(x);
-#pragma unroll
                 for (int x = 0; x < 2 * DB; ++x) {
-                    if (x + AHEAD < 2 * DB) ring[(x + AHEAD) % (AHEAD + 1)] = col_operand(x + AHEAD);
-                    mma(dq[x % DB], ring[x % (AHEAD + 1)], f[x / DB]);
+                    if (x + AHEAD < 2 * DB) ring[(2 * CH + x + AHEAD) % (AHEAD + 1)] = operand(2 * CH + x + AHEAD);
+                    mma(dq[x % DB], ring[(2 * CH + x) % (AHEAD + 1)], f[x / DB]);
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
@@ -212,7 +212,7 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, float
         before -= off * before_p;
         after -= off * after_p;
     }
-    if (i < a.Lq && h == 0) *(float2 *)(a.delta + 2 * stat) = make_float2(lse2, ok ? delta : 0.f);
+    if (i < a.Lq && h == 0) *(float2 *)(a.delta + 2 * stat) = make_float2(lse2, ok ? -delta : 0.f);
     if constexpr (TAB) {
         // (two groups of keys, two of values)
         const auto fetch2 = [&](int j) { fetch(j, j & 1, (j & 1) - 1); };
@@ -234,14 +234,14 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, float
             const int k0 = 32 * j;
             if (j + 1 < end) fetch2(j + 1);
             if (k0 < mine && near_at(k0)) {
-                const int at_j = (j & 1) * Tl::SIZE + rows;
+                const int at_j = (j & 1) * Tl::BYTES + rows;
                 f32x16_t s = {}, dp;
 #pragma unroll
                 for (int e = 0; e < 16; ++e) dp[e] = -delta;
 #pragma unroll
                 for (int c = 0; c < CH; ++c) {
-                    mma(s, Tl::by_rows(kb, at_j, 0, c), q[c]);
-                    mma(dp, Tl::by_rows(kb + 2 * Tl::SIZE, at_j, 0, c), g[c]);
+                    mma(s, Tl::by_rows(lds, at_j, 0, c), q[c]);
+                    mma(dp, Tl::by_rows(lds, 2 * Tl::BYTES + at_j, 0, c), g[c]);
                 }
                 finish(s, k0);
                 // along the diagonals of the block
@@ -333,11 +333,11 @@ __global__ __launch_bounds__((128 * BwdLds<T, DP>::QW), (DP * sizeof(T) <= 128 ?
 {
     constexpr int QW = BwdLds<T, DP>::QW, ROWS = 32 * QW, THREADS = 128 * QW;
     using Tl = Tile<T, DP, ROWS, THREADS>;
-    constexpr int CH = DP / 16, DB = DP / 32, AHEAD = 3;
+    constexpr int CH = DP / 16, DB = DP / 32, AHEAD = DP * sizeof(T) <= 128 ? 3 : sizeof(T) == 2 ? 6 : 3; // (one wave to a unit needs more on the way)
     extern __shared__ __attribute__((aligned(16))) char lds[];
     T *const qb = (T *)lds, *const gb = qb + 3 * Tl::SIZE;
     // (objects of their own: a read from the array that fetches go to would wait for them)
-    __shared__ __attribute__((aligned(16))) float stats[3 * 2 * ROWS]; // lse (base 2) and delta of each query
+    __shared__ __attribute__((aligned(16))) float stats[3 * 2 * ROWS]; // lse (base 2) and -delta of each query
     __shared__ float bias[BIAS ? 2 * ATTN_MAX_DISTANCE + 1 : 1];
 
     const unsigned w = xcd_order(blockIdx.x, gridDim.x);
@@ -364,7 +364,7 @@ __global__ __launch_bounds__((128 * BwdLds<T, DP>::QW), (DP * sizeof(T) <= 128 ?
 
     const i64 grow = (i64)a.Hq * a.D;
     const Tl ql(a.qs[1], a.D, t), gl(grow, a.D, t);
-    const int rows = Tl::row_place(lane), cols = Tl::col_place(lane);
+    const int rows = Tl::row_place(lane) + r0 * Tl::RB, cols = Tl::col_place(lane) + r0 * Tl::RB; // (turn() repeats after 16 rows)
     // the groups of queries that see a key of the workgroup; the first query that sees one of the wave
     int begin = 0, mine = 0;
     const int end = (n.nq + ROWS - 1) / ROWS;
@@ -408,10 +408,12 @@ __global__ __launch_bounds__((128 * BwdLds<T, DP>::QW), (DP * sizeof(T) <= 128 ?
             const int i0 = ROWS * x0 + r0; // the wave's first query
             const bool now = x0 >= begin && i0 < n.nq && i0 + 31 >= mine, then = x0 + 1 < end && i0 + ROWS < n.nq && i0 + ROWS + 31 >= mine;
             if (now || then) {
-                const int row = s1 * Tl::SIZE + rows, colp = slot * Tl::SIZE + cols;
-                // S and dP in turn; dV and dK in turn, 16 rows after 16 rows
-                const auto row_operand = [&](int x) { return Tl::by_rows(x & 1 ? gb : qb, row, r0, x / 2); };
-                const auto col_operand = [&](int x) { return Tl::by_cols(x & 1 ? qb : gb, colp, r0 + 16 * (x / (2 * DB)), x / 2 % DB); };
+                // S and dP in turn, then dV and dK in turn, 16 rows after 16 rows
+                const int qrow = s1 * Tl::BYTES + rows, grow_at = qrow + 3 * Tl::BYTES, qcol = slot * Tl::BYTES + cols, gcol = qcol + 3 * Tl::BYTES;
+                const auto operand = [&](int x) {
+                    const int y = x - 2 * CH;
+                    return x < 2 * CH ? Tl::by_rows(lds, x & 1 ? grow_at : qrow, 0, x / 2) : Tl::by_cols(lds, y & 1 ? qcol : gcol, 16 * (y / (2 * DB)), y / 2 % DB);
+                };
                 const float *const st = stats + 2 * slot * ROWS + r0 + 4 * h, *const st1 = stats + (2 * s1 + 1) * ROWS + r0 + 4 * h;
                 const int p0 = i0 + n.start; // the position of the first row
                 const bool edge = j0 + 32 > n.nk || (a.causal && j0 + 31 > p0);
@@ -424,17 +426,17 @@ __global__ __launch_bounds__((128 * BwdLds<T, DP>::QW), (DP * sizeof(T) <= 128 ?
                 for (int e = 0; e < 16; e += 4) { // (dP is formed on -delta: dS = P (dP - delta))
                     const f32x4_t y = *(const f32x4_t *)(st1 + 2 * e);
                     next[e] = next[e + 1] = next[e + 2] = next[e + 3] = 0.f;
-                    dnext[e] = -y[0], dnext[e + 1] = -y[1], dnext[e + 2] = -y[2], dnext[e + 3] = -y[3];
+                    dnext[e] = y[0], dnext[e + 1] = y[1], dnext[e + 2] = y[2], dnext[e + 3] = y[3];
                 }
                 Frag<T> ring[AHEAD + 1], fp[2], fs[2];
                 f32x16_t p;
                 f32x4_t l4 = *(const f32x4_t *)st;
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int x = 0; x < AHEAD; ++x) ring[x] = row_operand(x);
+                for (int x = 0; x < AHEAD; ++x) ring[x] = operand(x);
 #pragma unroll
                 for (int x = 0; x < 2 * CH; ++x) {
-                    if (x + AHEAD < 2 * CH) ring[(x + AHEAD) % (AHEAD + 1)] = row_operand(x + AHEAD);
+                    ring[(x + AHEAD) % (AHEAD + 1)] = operand(x + AHEAD);
                     if (x & 1)
                         mma(dnext, ring[x % (AHEAD + 1)], v[x / 2]);
                     else
@@ -455,14 +457,12 @@ __global__ __launch_bounds__((128 * BwdLds<T, DP>::QW), (DP * sizeof(T) <= 128 ?
                 }
                 if (now) {
 #pragma unroll
-                    for (int x = 0; x < AHEAD; ++x) ring[x] = col_operand(x);
-#pragma unroll
                     for (int x = 0; x < 4 * DB; ++x) {
-                        if (x + AHEAD < 4 * DB) ring[(x + AHEAD) % (AHEAD + 1)] = col_operand(x + AHEAD);
+                        if (x + AHEAD < 4 * DB) ring[(2 * CH + x + AHEAD) % (AHEAD + 1)] = operand(2 * CH + x + AHEAD);
                         if (x & 1)
-                            mma(dk[x / 2 % DB], ring[x % (AHEAD + 1)], fs[x / (2 * DB)]);
+                            mma(dk[x / 2 % DB], ring[(2 * CH + x) % (AHEAD + 1)], fs[x / (2 * DB)]);
                         else
-                            mma(dv[x / 2 % DB], ring[x % (AHEAD + 1)], fp[x / (2 * DB)]);
+                            mma(dv[x / 2 % DB], ring[(2 * CH + x) % (AHEAD + 1)], fp[x / (2 * DB)]);
                         __builtin_amdgcn_sched_barrier(0);
                     }
                 }

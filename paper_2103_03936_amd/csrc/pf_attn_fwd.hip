@@ -67,7 +67,7 @@ __device__ __forceinline__ void attn_fwd_tile(const AttnArgs &a, char *lds, floa
         for (int u = 0; u < SUB; ++u) {
             s0[u] = f32x16_t{};
 #pragma unroll
-            for (int c = 0; c < CH; ++c) mma(s0[u], Tl::by_rows(kb, rows, 32 * u, c), q[c]);
+            for (int c = 0; c < CH; ++c) mma(s0[u], Tl::by_rows(lds, rows, 32 * u, c), q[c]);
 #pragma unroll
             for (int e = 0; e < 16; ++e) top = fmaxf(top, s0[u][e]);
         }
@@ -117,12 +117,15 @@ __device__ __forceinline__ void attn_fwd_tile(const AttnArgs &a, char *lds, floa
             for (int u = 0; u < SUB; ++u) next[u] = f32x16_t{};
             __builtin_amdgcn_sched_barrier(0);
             // the next keys' scores (of whatever lies there, after the last) beside this tile's exponentials
-            const int ka = rows + (odd ? 0 : Tl::SIZE), va = cols + (odd ? Tl::SIZE : 0);
+            const int ka = rows + (odd ? 0 : Tl::BYTES), va = cols + 2 * Tl::BYTES + (odd ? Tl::BYTES : 0);
+            const auto operand = [&](int x) {
+                return x < SC ? Tl::by_rows(lds, ka, 32 * (x / CH), x % CH) : Tl::by_cols(lds, va, 16 * ((x - SC) / DB), (x - SC) % DB);
+            };
 #pragma unroll
-            for (int x = 0; x < AHEAD; ++x) ring[x] = Tl::by_rows(kb, ka, 32 * (x / CH), x % CH);
+            for (int x = 0; x < AHEAD; ++x) ring[x] = operand(x);
 #pragma unroll
             for (int x = 0; x < SC; ++x) {
-                if (x + AHEAD < SC) ring[(x + AHEAD) % (AHEAD + 1)] = Tl::by_rows(kb, ka, 32 * ((x + AHEAD) / CH), (x + AHEAD) % CH);
+                ring[(x + AHEAD) % (AHEAD + 1)] = operand(x + AHEAD);
                 mma(next[x / CH], ring[x % (AHEAD + 1)], q[x % CH]);
 #pragma unroll
                 for (int y = x * (16 * SUB) / SC; y < (x + 1) * (16 * SUB) / SC; ++y) {
@@ -136,11 +139,9 @@ __device__ __forceinline__ void attn_fwd_tile(const AttnArgs &a, char *lds, floa
             // P and V beside the largest of the next scores
             top = -INFINITY;
 #pragma unroll
-            for (int x = 0; x < AHEAD; ++x) ring[x] = Tl::by_cols(vb, va, 16 * (x / DB), x % DB);
-#pragma unroll
             for (int x = 0; x < PV; ++x) {
-                if (x + AHEAD < PV) ring[(x + AHEAD) % (AHEAD + 1)] = Tl::by_cols(vb, va, 16 * ((x + AHEAD) / DB), (x + AHEAD) % DB);
-                mma(o[x % DB], ring[x % (AHEAD + 1)], p[x / DB]);
+                if (x + AHEAD < PV) ring[(SC + x + AHEAD) % (AHEAD + 1)] = operand(SC + x + AHEAD);
+                mma(o[x % DB], ring[(SC + x) % (AHEAD + 1)], p[x / DB]);
 #pragma unroll
                 for (int y = x * (16 * SUB) / PV; y < (x + 1) * (16 * SUB) / PV; ++y) top = fmaxf(top, next[y / 16][y % 16]);
                 __builtin_amdgcn_sched_barrier(0);

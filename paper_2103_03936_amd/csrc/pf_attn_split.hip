@@ -79,7 +79,6 @@ __global__ __launch_bounds__(64 * SPLIT_WAVES<T>) void attn_split_kernel(AttnArg
     if (first + wave < end) fetch(first + wave, 0);
     for (int k = first + wave, turn = 0; k < end; k += NW, turn ^= 1) {
         const int k0 = 32 * k;
-        const T *const vt = vb + turn * Tl::SIZE;
         f32x16_t acc = {};
         fetched(); // (K's registers, too)
 #pragma unroll
@@ -125,7 +124,7 @@ __global__ __launch_bounds__(64 * SPLIT_WAVES<T>) void attn_split_kernel(AttnArg
             Frag<T> p;
             pack(s, c, p);
 #pragma unroll
-            for (int d = 0; d < DP / 32; ++d) mma(o[d], Tl::by_cols(vt, cols, 16 * c, d), p);
+            for (int d = 0; d < DP / 32; ++d) mma(o[d], Tl::by_cols(lds, cols + (2 * wave + turn) * Tl::BYTES, 16 * c, d), p);
         }
     }
     sum += __shfl_xor(sum, 32);
