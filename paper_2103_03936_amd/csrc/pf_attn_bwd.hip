@@ -21,15 +21,15 @@ constexpr int DIAG = 32 * 64;
 template <typename T, int DP>
 struct BwdLds {
     using Tq = Tile<T, DP, 32, 256>;
-    static size_t dq(int far, bool tab)
+    static constexpr size_t TILES = 4 * Tq::BYTES + 4 * DIAG * 4 > 5 * Tq::BYTES ? 4 * Tq::BYTES + 4 * DIAG * 4 : 5 * Tq::BYTES;
+    static size_t dq(int far, bool bias, bool tab)
     {
-        // three groups of keys, two of values; then (over them) two of each and the waves' blocks
-        const size_t first = 5 * Tq::BYTES, second = 4 * Tq::BYTES + 4 * DIAG * 4;
-        return tab ? 4 * (2 * far + 1) * 4 + (second > first ? second : first) : first;
+        // three groups of keys, two of values; with the table's gradient then, over them, two of each and the waves' blocks
+        return (tab ? TILES + 4 * (2 * far + 1) * 4 : 5 * Tq::BYTES) + (bias ? (2 * far + 1) * 4 : 0);
     }
     // dK and dV: how many waves share the queries (what six tiles of float rows take leaves room for one)
     static constexpr int QW = sizeof(T) == 4 && DP > 64 ? 1 : 2;
-    static size_t dkv() { return 6 * QW * Tq::BYTES; }
+    static size_t dkv(int far, bool bias) { return 6 * QW * Tq::BYTES + 3 * 2 * 32 * QW * 4 + (bias ? (2 * far + 1) * 4 : 0); }
 };
 
 // dQ, delta and the sums of dS by distance, for one tile of 128 queries of one head.  TAB: with the gradient of the table.
@@ -43,7 +43,7 @@ struct BwdLds {
 // second pass goes over the near blocks alone, for their dS with the delta that is now exact (S and dP, two products of the
 // first pass's three); the far sums are put right by their sums of P.
 template <typename T, int DP, bool BIAS, bool TAB>
-__device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, float *bias, int b, int head, int tile)
+__device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b, int head, int tile)
 {
     using Tl = Tile<T, DP, 32, 256>;
     constexpr int CH = DP / 16, DB = DP / 32, AHEAD = 2;
@@ -51,7 +51,7 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, float
     T *const kb = (T *)lds, *const vb = kb + 3 * Tl::SIZE;
     // the waves' blocks of dS (second pass), their sums by distance [span]
     float *const diag_all = (float *)(lds + 4 * Tl::BYTES);
-    float *const sums_all = (float *)(lds + (4 * Tl::BYTES + 4 * DIAG * 4 > 5 * Tl::BYTES ? 4 * Tl::BYTES + 4 * DIAG * 4 : 5 * Tl::BYTES));
+    float *const bias = (float *)(lds + (TAB ? BwdLds<T, DP>::TILES : 5 * Tl::BYTES)), *const sums_all = bias + span;
 
     const int t = threadIdx.x, wave = wave_of(t), lane = t & 63, col = lane & 31, h = lane >> 5;
     float *const diag = diag_all + wave * DIAG, *const sums = sums_all + wave * span;
@@ -151,8 +151,8 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, float
                     const float p = exp2_fast(s[e] * mul + add);
                     s[e] = p * dp[e];
                     if constexpr (TAB) {
-                        sum += s[e];
-                        sum_p += p;
+                        sum = anew(sum + s[e]);
+                        sum_p = anew(sum_p + p);
                     }
                     if (e % 8 == 7) {
                         pack(s, e / 8, f[e / 8]);
@@ -312,13 +312,12 @@ template <typename T, int DP, bool BIAS, bool TAB>
 __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void attn_dq_kernel(AttnArgs a, int paired)
 {
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    __shared__ float bias[BIAS ? 2 * ATTN_MAX_DISTANCE + 1 : 1]; // (an object of its own: see attn_dkv_kernel)
     const unsigned w = xcd_order(blockIdx.x, gridDim.x);
     const int each = paired ? (a.tiles + 1) / 2 : a.tiles, k = (int)(w % each), bh = w / each, b = bh / a.Hq, head = bh - b * a.Hq;
     const int count = paired && a.tiles - 1 - k != k ? 2 : 1;
 #pragma unroll 1
     for (int x = 0; x < count; ++x) {
-        attn_dq_tile<T, DP, BIAS, TAB>(a, lds, bias, b, head, x ? k : a.tiles - 1 - k);
+        attn_dq_tile<T, DP, BIAS, TAB>(a, lds, b, head, x ? k : a.tiles - 1 - k);
         __syncthreads();
     }
 }
@@ -336,9 +335,8 @@ __global__ __launch_bounds__((128 * BwdLds<T, DP>::QW), (DP * sizeof(T) <= 128 ?
     constexpr int CH = DP / 16, DB = DP / 32, AHEAD = DP * sizeof(T) <= 128 ? 3 : sizeof(T) == 2 ? 6 : 3; // (one wave to a unit needs more on the way)
     extern __shared__ __attribute__((aligned(16))) char lds[];
     T *const qb = (T *)lds, *const gb = qb + 3 * Tl::SIZE;
-    // (objects of their own: a read from the array that fetches go to would wait for them)
-    __shared__ __attribute__((aligned(16))) float stats[3 * 2 * ROWS]; // lse (base 2) and -delta of each query
-    __shared__ float bias[BIAS ? 2 * ATTN_MAX_DISTANCE + 1 : 1];
+    float *const stats = (float *)(lds + 6 * Tl::BYTES); // [3][2][ROWS]: lse (base 2) and -delta of each query
+    float *const bias = stats + 3 * 2 * ROWS;
 
     const unsigned w = xcd_order(blockIdx.x, gridDim.x);
     const int tile = (int)(w % a.tiles), bk = w / a.tiles, b = bk / a.Hkv, kv = bk - b * a.Hkv;
@@ -533,7 +531,7 @@ static int attn_bwd_launch(AttnArgs &a, float *dtable, int accumulate, hipStream
     const int parts = a.B * a.tiles;
     const int paired = a.causal && (i64)a.B * a.Hq * a.tiles > 512; // (two workgroups to a compute unit are resident)
     const dim3 grid((unsigned)a.B * a.Hq * (paired ? (a.tiles + 1) / 2 : a.tiles));
-    const size_t lds = BwdLds<T, DP>::dq(a.bk.far, tab);
+    const size_t lds = BwdLds<T, DP>::dq(a.bk.far, bias, tab);
     if (a.Lq > 0) {
         if (tab)
             PF_LAUNCH_LDS(st, "attn_dq_tab", (attn_dq_kernel<T, DP, true, true>), grid, dim3(256), lds, s, a, paired);
@@ -545,7 +543,7 @@ static int attn_bwd_launch(AttnArgs &a, float *dtable, int accumulate, hipStream
     if (a.Lk > 0) {
         a.tiles = (a.Lk + 63) / 64;
         const dim3 kgrid((unsigned)a.B * a.Hkv * a.tiles);
-        const size_t klds = BwdLds<T, DP>::dkv();
+        const size_t klds = BwdLds<T, DP>::dkv(a.bk.far, bias);
         if (bias)
             PF_LAUNCH_LDS(st, "attn_dkv", (attn_dkv_kernel<T, DP, true>), kgrid, dim3(128 * BwdLds<T, DP>::QW), klds, s, a);
         else

@@ -13,11 +13,12 @@ constexpr int KEYS = sizeof(T) == 2 ? 64 : 32; // keys of a tile
 // One tile of queries.  A turn of the loop has the scores of its keys in registers; their exponentials are worked out while
 // the matrix unit makes the next turn's scores, and the largest of those is found while it multiplies P and V.
 template <typename T, int DP, bool BIAS>
-__device__ __forceinline__ void attn_fwd_tile(const AttnArgs &a, char *lds, float *bias, int b, int head, int tile)
+__device__ __forceinline__ void attn_fwd_tile(const AttnArgs &a, char *lds, int b, int head, int tile)
 {
     constexpr int KT = KEYS<T>, SUB = KT / 32;
     using Tl = Tile<T, DP, KT, 256>;
     T *const kb = (T *)lds, *const vb = kb + 2 * Tl::SIZE; // two tiles of keys, two of values
+    float *const bias = (float *)(lds + 4 * Tl::BYTES);
 
     const int t = threadIdx.x, wave = wave_of(t), lane = t & 63, col = lane & 31, h = lane >> 5;
     const AttnLens n(a, b);
@@ -179,13 +180,12 @@ template <typename T, int DP, bool BIAS>
 __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void attn_fwd_kernel(AttnArgs a, int paired)
 {
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    __shared__ float bias[BIAS ? 2 * ATTN_MAX_DISTANCE + 1 : 1]; // (an object of its own: a read from where fetches go would wait for them)
     const unsigned w = xcd_order(blockIdx.x, gridDim.x);
     const int each = paired ? (a.tiles + 1) / 2 : a.tiles, k = (int)(w % each), bh = w / each, b = bh / a.Hq, head = bh - b * a.Hq;
     const int other = paired && a.tiles - 1 - k != k ? 2 : 1;
 #pragma unroll 1
     for (int pass = 0; pass < other; ++pass) {
-        attn_fwd_tile<T, DP, BIAS>(a, lds, bias, b, head, pass ? k : a.tiles - 1 - k);
+        attn_fwd_tile<T, DP, BIAS>(a, lds, b, head, pass ? k : a.tiles - 1 - k);
         __syncthreads();
     }
 }
@@ -258,7 +258,7 @@ static int attn_fwd_launch(const AttnArgs &a, hipStream_t s)
     // two workgroups to a compute unit are resident: causal tiles are paired where there are more
     const bool paired = a.causal && (i64)a.B * a.Hq * a.tiles > 512;
     const unsigned blocks = (unsigned)a.B * a.Hq * (paired ? (a.tiles + 1) / 2 : a.tiles);
-    const size_t lds = 4 * Tl::BYTES;
+    const size_t lds = 4 * Tl::BYTES + (a.buckets ? (2 * a.bk.far + 1) * sizeof(float) : 0);
     int st = PF_OK;
     if (a.buckets)
         PF_LAUNCH_LDS(st, "attn_fwd", (attn_fwd_kernel<T, DP, true>), dim3(blocks), dim3(256), lds, s, a, (int)paired);
