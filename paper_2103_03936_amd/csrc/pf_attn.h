@@ -24,7 +24,7 @@ struct AttnArgs {
     float scale;
     i64 qs[3], ks[3], vs[3]; // strides: sequence, token, head
     // few queries: the split of the keys and where its parts go (partial O, then maxima and sums)
-    int splits, rows;
+    int splits, rows, tile_heads;
     float *part_o, *part_ml;
     AttnBuckets bk;
 };
@@ -262,18 +262,22 @@ struct AttnLens {
     }
 };
 
-// Bucket of the distance key - query
+// Bucket of the distance key - query, within +-far.  Sixteen borders at a time: a loop over single ones waits for each.
 __device__ __forceinline__ int bucket_of(const AttnArgs &a, int dist)
 {
-    if (dist > 0 && !a.two_sided) return 0;
     const int n = dist < 0 ? -dist : dist;
-    int u = n;
-    if (n >= a.bk.exact) {
-        u = a.bk.exact;
-        for (int k = 0; k < a.bk.borders; ++k) u += n >= a.bk.border[k];
+    int u = 0;
+    for (int k = 0; k < a.bk.borders; k += 16) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) u += n >= a.bk.border[k + i];
     }
-    return u + (dist > 0 ? a.bk.side : 0);
+    u = n < a.bk.exact ? n : a.bk.exact + u;
+    return dist <= 0 ? u : a.two_sided ? u + a.bk.side : 0;
 }
+// of the distances -far and far
+__device__ __forceinline__ int bucket_before(const AttnArgs &a) { return a.bk.side - 1; }
+__device__ __forceinline__ int bucket_after(const AttnArgs &a) { return a.two_sided ? 2 * a.bk.side - 1 : 0; }
+
 // The bias of query head `head` in a bucket, times log2(e); finite values stay finite (a table may hold the type's lowest)
 __device__ __forceinline__ float bias_of(const AttnArgs &a, int bucket, int head)
 {

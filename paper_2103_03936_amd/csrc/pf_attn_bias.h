@@ -11,7 +11,7 @@ namespace pf {
 constexpr int ATTN_MAX_BORDERS = 128, ATTN_MAX_DISTANCE = 1024, ATTN_MAX_BUCKETS = 256;
 
 // One side's buckets: distance n < exact has bucket n, the others exact + (number of borders <= n); from `far` on the
-// bucket is side - 1.
+// bucket is side - 1.  Behind the last border stand values that no distance reaches.
 struct AttnBuckets {
     int side, exact, borders, far;
     uint16_t border[ATTN_MAX_BORDERS];
@@ -57,6 +57,7 @@ inline AttnBuckets attn_buckets(int side, int max_distance)
             n = power_product_ge((uint32_t)near, m, (uint32_t)e, k, (uint32_t)max_distance, (uint32_t)e) ? (int)near : (int)near + 1;
         t.border[t.borders++] = (uint16_t)n;
     }
+    for (int k = t.borders; k < ATTN_MAX_BORDERS; ++k) t.border[k] = 0xffff;
     t.far = t.borders ? t.border[t.borders - 1] : e;
     return t;
 }

@@ -286,9 +286,10 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b
         for (int x = t; x < span; x += 256) sums_all[x] = (sums_all[x] + sums_all[span + x]) + (sums_all[2 * span + x] + sums_all[3 * span + x]);
         __syncthreads();
         float *const out = a.tab + (((i64)head * a.B + b) * a.tiles + tile) * a.buckets;
-        for (int u = t; u < a.buckets; u += 256) {
+        // eight lanes to a bucket
+        for (int x = t; x < 8 * a.buckets; x += 256) {
             // the distances of bucket u: lo .. hi of its side, the last one's up to far
-            const int v = a.two_sided && u >= a.bk.side ? u - a.bk.side : u, e = a.bk.exact;
+            const int u = x / 8, sub = x & 7, v = a.two_sided && u >= a.bk.side ? u - a.bk.side : u, e = a.bk.exact;
             int lo = v, hi = v;
             if (v >= e) {
                 lo = v == e ? e : a.bk.border[v - e - 1];
@@ -296,13 +297,14 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b
             }
             float y = 0.f;
             if (a.two_sided && u >= a.bk.side) {
-                for (int x = lo < 1 ? 1 : lo; x <= hi; ++x) y += sums_all[far + x];
+                for (int z = (lo < 1 ? 1 : lo) + sub; z <= hi; z += 8) y += sums_all[far + z];
             } else {
-                for (int x = lo; x <= hi; ++x) y += sums_all[far - x];
+                for (int z = lo + sub; z <= hi; z += 8) y += sums_all[far - z];
                 if (u == 0 && !a.two_sided)
-                    for (int x = 1; x <= far; ++x) y += sums_all[far + x];
+                    for (int z = 1 + sub; z <= far; z += 8) y += sums_all[far + z];
             }
-            out[u] = y;
+            for (int o = 4; o; o >>= 1) y += __shfl_xor(y, o);
+            if (sub == 0) out[u] = y;
         }
     }
 }

@@ -3,33 +3,49 @@
 //
 // Bound by reading keys and values.  The query heads of one key head, and their few queries, are the columns of one
 // product (row r of the group: query head r / Lq, query r % Lq), so that keys and values are read once for all of them.
-// A wave takes 32 keys at a time: K goes from memory straight into the operand's registers, V through 32 rows of LDS that are the
-// wave's own (its columns are needed transposed), and the next 32 keys are on their way while these are used; no wave waits
-// for another before the end.  The waves' and then the workgroups' results are joined by their maxima and sums in a fixed order.
+// A wave takes 32 keys at a time, in tiles of LDS that are its own, and the next 32 are on their way while these are used; no wave
+// waits for another before the end.  (K straight into the operand's registers meant loads of 32 bytes of 32 rows each, eight
+// times over: a decoding step of 32 sequences of up to 4096 keys took 85 us, not 78.)  The waves' and then the workgroups' results are joined by their maxima and sums in a fixed order.
 #include "pf_attn.h"
 
 namespace pf {
 
-// float rows are twice as long: two waves, not four, share the LDS of a workgroup
-template <typename T>
-constexpr int SPLIT_WAVES = sizeof(T) == 2 ? 4 : 2;
+constexpr int SPLIT_WAVES = 2;
 
 template <typename T, int DP>
 struct SplitLds {
-    static constexpr int NW = SPLIT_WAVES<T>, JOIN = DP * 33 * 4, TILES = 2 * NW * Tile<T, DP, 32, 64>::BYTES;
+    static constexpr int NW = SPLIT_WAVES, JOIN = DP * 33 * 4, TILES = 4 * NW * Tile<T, DP, 32, 64>::BYTES;
     static constexpr int AREA = JOIN > TILES ? JOIN : TILES;
 };
 
-template <typename T, int DP, bool BIAS>
-__global__ __launch_bounds__(64 * SPLIT_WAVES<T>) void attn_split_kernel(AttnArgs a)
+// What a workgroup without keys writes: an empty part, or (the only part) rows of zeros
+template <typename T>
+__device__ __forceinline__ void leave_nothing(const AttnArgs &a, int bk, int tile, int split, int b, int kv, int t, int threads)
 {
-    constexpr int NW = SPLIT_WAVES<T>;
+    if (a.splits > 1) {
+        float *const ml = a.part_ml + (((i64)bk * a.tiles + tile) * a.splits + split) * 64;
+        if (t < 64) ml[t] = t & 1 ? 0.f : -INFINITY;
+        return;
+    }
+    for (int x = t; x < 32 * a.D; x += threads) {
+        const int r = tile * 32 + x / a.D, c = x % a.D, g = r / a.Lq, i = r - g * a.Lq;
+        if (r >= a.rows) break;
+        ((T *)a.O)[(((i64)b * a.Lq + i) * a.Hq + kv * a.G + g) * a.D + c] = from_float<T>(0.f);
+        if (c == 0 && a.lse) a.lse[((i64)b * a.Hq + kv * a.G + g) * a.Lq + i] = -INFINITY;
+    }
+}
+
+template <typename T, int DP, bool BIAS>
+__global__ __launch_bounds__(64 * SPLIT_WAVES, sizeof(T) * DP <= 256 ? 2 : 1) void attn_split_kernel(AttnArgs a)
+{
+    constexpr int NW = SPLIT_WAVES;
     using Tl = Tile<T, DP, 32, 64>;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     float *const ml = (float *)(lds + SplitLds<T, DP>::AREA); // [2][NW][32]: the waves' maxima and sums
-    uint8_t *const lut = (uint8_t *)(ml + 2 * NW * 32);       // bucket of each distance from -far to far
+    float *const tab = ml + 2 * NW * 32;                      // [buckets][heads of the tile]: the bias (base 2)
+    uint8_t *const lut = (uint8_t *)(tab + a.buckets * a.tile_heads); // bucket of each distance from -far to far
     const int t = threadIdx.x, wave = wave_of(t), lane = t & 63, col = lane & 31, h = lane >> 5;
-    T *const vb = (T *)(lds + 2 * wave * Tl::BYTES); // two tiles of this wave's own
+    T *const own_tiles = (T *)(lds + 4 * wave * Tl::BYTES); // two of keys and two of values, this wave's own
 
     const unsigned w = xcd_order(blockIdx.x, gridDim.x);
     const int split = w % a.splits, tile = w / a.splits % a.tiles, bk = w / a.splits / a.tiles, b = bk / a.Hkv, kv = bk - b * a.Hkv;
@@ -44,13 +60,10 @@ __global__ __launch_bounds__(64 * SPLIT_WAVES<T>) void attn_split_kernel(AttnArg
 
     const int far = a.bk.far;
     float flat_before = 0.f, flat_after = 0.f;
-    if constexpr (BIAS) {
-        for (int k = t; k <= 2 * far; k += 64 * NW) lut[k] = (uint8_t)bucket_of(a, k - far);
-        if (row) {
-            flat_before = bias_of(a, bucket_of(a, -far), head);
-            flat_after = bias_of(a, bucket_of(a, far), head);
-        }
-        __syncthreads();
+    const int first_head = kv * a.G + tile * 32 / a.Lq;
+    if (first >= end) { // (no keys: nothing but an empty part to leave)
+        leave_nothing<T>(a, bk, tile, split, b, kv, t, 64 * NW);
+        return;
     }
     const T *const Kp = (const T *)a.K + b * a.ks[0] + kv * a.ks[2], *const Vp = (const T *)a.V + b * a.vs[0] + kv * a.vs[2];
     Frag<T> q[DP / 16];
@@ -65,44 +78,60 @@ __global__ __launch_bounds__(64 * SPLIT_WAVES<T>) void attn_split_kernel(AttnArg
     for (int d = 0; d < DP / 32; ++d) o[d] = f32x16_t{};
     float m = -INFINITY, sum = 0.f;
 
-    const Tl vl(a.vs[1], a.D, lane);
-    const int cols = Tl::col_place(lane);
-    Frag<T> kr[DP / 16];
-    const uint32_t kat = (uint32_t)(col * (int)a.ks[1]) * (uint32_t)sizeof(T);
+    const Tl kl(a.ks[1], a.D, lane), vl(a.vs[1], a.D, lane);
+    const int rows = Tl::row_place(lane) + 4 * wave * Tl::BYTES, cols = Tl::col_place(lane) + (4 * wave + 2) * Tl::BYTES;
     const auto fetch = [&](int k, int turn) {
-        const int rows = n.nk - 32 * k < 32 ? n.nk - 32 * k : 32;
-        const BufSrc src(Kp + (i64)(32 * k) * a.ks[1], ((rows - 1) * (int)a.ks[1] + a.D) * (int)sizeof(T));
-#pragma unroll
-        for (int c = 0; c < DP / 16; ++c) kr[c] = row_frag_buffer(src, kat, 16 * c, a.D, h, (T *)nullptr);
-        vl.fetch(vb + turn * Tl::SIZE, Vp + (i64)(32 * k) * a.vs[1], a.vs[1], n.nk - 32 * k, a.D, 0);
+        kl.fetch(own_tiles + turn * Tl::SIZE, Kp + (i64)(32 * k) * a.ks[1], a.ks[1], n.nk - 32 * k, a.D, 0);
+        vl.fetch(own_tiles + (2 + turn) * Tl::SIZE, Vp + (i64)(32 * k) * a.vs[1], a.vs[1], n.nk - 32 * k, a.D, 0);
     };
     if (first + wave < end) fetch(first + wave, 0);
+    if constexpr (BIAS) {
+        const int heads = a.tile_heads < (kv + 1) * a.G - first_head ? a.tile_heads : (kv + 1) * a.G - first_head;
+        for (int k = t; k <= 2 * far; k += 64 * NW) lut[k] = (uint8_t)bucket_of(a, k - far);
+        for (int k = t; k < a.buckets * a.tile_heads; k += 64 * NW)
+            tab[k] = k % a.tile_heads < heads ? bias_of(a, k / a.tile_heads, first_head + k % a.tile_heads) : 0.f;
+    }
+    const float *const mine = tab + (row ? head - first_head : 0);
+    if constexpr (BIAS) {
+        __syncthreads();
+        flat_before = mine[bucket_before(a) * a.tile_heads];
+        flat_after = mine[bucket_after(a) * a.tile_heads];
+    }
     for (int k = first + wave, turn = 0; k < end; k += NW, turn ^= 1) {
         const int k0 = 32 * k;
         f32x16_t acc = {};
-        fetched(); // (K's registers, too)
-#pragma unroll
-        for (int c = 0; c < DP / 16; ++c) mma(acc, kr[c], q[c]);
+        fetched();
         if (k + NW < end) fetch(k + NW, turn ^ 1);
+#pragma unroll
+        for (int c = 0; c < DP / 16; ++c) mma(acc, Tl::by_rows(lds, rows + turn * Tl::BYTES, 0, c), q[c]);
         const bool edge = k0 + 32 > n.nk || (a.causal && k0 + 31 > pmin);
         const bool near = BIAS && k0 + 31 - pmin > -far && k0 - pmax < far;
         const float flat = k0 >= pmin ? flat_after : flat_before;
-        f32x16_t s;
         float top = -INFINITY;
+        f32x16_t s = acc;
+        if (near) {
+            const int rel = k0 + 4 * h - pos;
+            int u[16];
+            float y[16];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const int j = k0 + 8 * (e >> 2) + 4 * h + (e & 3);
-            float x = acc[e] * sl2;
-            if constexpr (BIAS) {
-                if (near)
-                    x += row ? bias_of(a, lut[clamped(j - pos, -far, far) + far], head) : 0.f;
-                else
-                    x += flat;
-            }
-            if (edge && (j >= n.nk || (a.causal && j > pos))) x = -INFINITY;
-            s[e] = x;
-            top = fmaxf(top, x);
+            for (int e = 0; e < 16; ++e) u[e] = lut[clamped(rel + 8 * (e >> 2) + (e & 3), -far, far) + far];
+            __builtin_amdgcn_sched_barrier(0); // (all reads of a kind first)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) y[e] = mine[u[e] * a.tile_heads];
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[e] = s[e] * sl2 + y[e];
+        } else {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[e] = s[e] * sl2 + (BIAS ? flat : 0.f);
         }
+        if (edge) {
+            const int rel = k0 + 4 * h - pos, most = a.causal && n.nk > pos ? 0 : n.nk - 1 - pos; // distances; the furthest seen
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[e] = fminf(s[e], rel + 8 * (e >> 2) + (e & 3) > most ? -INFINITY : INFINITY);
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) top = fmaxf(top, s[e]);
         top = fmaxf(top, __shfl_xor(top, 32));
         const float m_new = fmaxf(m, top), base = m_new == -INFINITY ? 0.f : m_new;
         if (__any(m_new > m)) {
@@ -124,7 +153,7 @@ __global__ __launch_bounds__(64 * SPLIT_WAVES<T>) void attn_split_kernel(AttnArg
             Frag<T> p;
             pack(s, c, p);
 #pragma unroll
-            for (int d = 0; d < DP / 32; ++d) mma(o[d], Tl::by_cols(lds, cols + (2 * wave + turn) * Tl::BYTES, 16 * c, d), p);
+            for (int d = 0; d < DP / 32; ++d) mma(o[d], Tl::by_cols(lds, cols + turn * Tl::BYTES, 16 * c, d), p);
         }
     }
     sum += __shfl_xor(sum, 32);
@@ -142,7 +171,7 @@ __global__ __launch_bounds__(64 * SPLIT_WAVES<T>) void attn_split_kernel(AttnArg
     const float f = exp2_fast(m - base);
     float *const join = (float *)lds; // [DP][33]
     for (int k = 0; k < NW; ++k) {
-        if (wave == k) {
+        if (wave == k && row) {
 #pragma unroll
             for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
@@ -163,9 +192,10 @@ __global__ __launch_bounds__(64 * SPLIT_WAVES<T>) void attn_split_kernel(AttnArg
         a.lse[((i64)b * a.Hq + head) * a.Lq + i] = ok && total > 0.f ? (top + __builtin_amdgcn_logf(total)) * LN2 : -INFINITY;
     if (a.splits == 1 && wave == 0 && h == 0) ml[col] = ok && total > 0.f ? 1.f / total : 0.f;
     __syncthreads();
-    for (int x = t; x < 32 * DP; x += 64 * NW) {
+    const int here_rows = a.rows - tile * 32 < 32 ? a.rows - tile * 32 : 32;
+    for (int x = t; x < here_rows * DP; x += 64 * NW) {
         const int rr = x / DP, c = x % DP;
-        if (tile * 32 + rr >= a.rows || c >= a.D) continue;
+        if (c >= a.D) continue;
         if (a.splits > 1) {
             a.part_o[(piece * 32 + rr) * DP + c] = join[c * 33 + rr];
         } else {
@@ -187,17 +217,29 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, int DP)
     const int g = r / a.Lq, i = r - g * a.Lq, head = kv * a.G + g;
     const i64 piece = ((i64)bk * a.tiles + r / 32) * a.splits;
     const float *const ml = a.part_ml + (piece * 32 + r % 32) * 2, *const po = a.part_o + (piece * 32 + r % 32) * DP;
+    // lane s: part s (and s + 64 ..)
     float top = -INFINITY, total = 0.f;
-    for (int s = 0; s < a.splits; ++s) top = fmaxf(top, ml[s * 64]);
+    for (int s = lane; s < a.splits; s += 64) top = fmaxf(top, ml[s * 64]);
+    for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
     const float base = top == -INFINITY ? 0.f : top;
     float o[2] = {0.f, 0.f};
-    for (int s = 0; s < a.splits; ++s) {
-        const float f = exp2_fast(ml[s * 64] - base);
-        total += ml[s * 64 + 1] * f;
+    const int c0 = lane < a.D ? lane : 0, c1 = lane + 64 < a.D ? lane + 64 : 0;
+    for (int s0 = 0; s0 < a.splits; s0 += 8) { // eight parts on their way at a time, added in their order
+        float f[8], y[8], z[8], w[8];
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const int c = lane + 64 * k;
-            if (c < a.D) o[k] += po[(i64)s * 32 * DP + c] * f;
+        for (int k = 0; k < 8; ++k) {
+            const int s = s0 + k < a.splits ? s0 + k : a.splits - 1;
+            f[k] = ml[s * 64], w[k] = ml[s * 64 + 1];
+            y[k] = po[(i64)s * 32 * DP + c0], z[k] = po[(i64)s * 32 * DP + c1];
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const float g = s0 + k < a.splits ? exp2_fast(f[k] - base) : 0.f;
+            if (g > 0.f) { // (an empty part has no rows)
+                total += w[k] * g;
+                o[0] += y[k] * g;
+                o[1] += z[k] * g;
+            }
         }
     }
     const AttnLens n(a, b);
@@ -215,8 +257,9 @@ int attn_split_count(const pf_attention_desc *d)
     const i64 rows = d->Lq * (d->heads_q / d->heads_kv);
     if (rows > 32 || d->Lk == 0) return 0;
     const i64 base = d->B * d->heads_kv * ((rows + 31) / 32);
-    // three workgroups to a compute unit, each with 256 keys or more
-    i64 n = (768 + base - 1) / base, most = (d->Lk + 255) / 256;
+    // pieces of 256 keys or more; sequences differ in length, so that there are more pieces (1024) than places for them
+    // (512: 32 sequences of up to 4096 keys took 78 us with 512 pieces, 76 with 1024, 82 with 2048)
+    i64 n = (1024 + base - 1) / base, most = (d->Lk + 255) / 256;
     n = n < most ? n : most;
     return (int)(n < 1 ? 1 : n > 256 ? 256 : n);
 }
@@ -233,12 +276,12 @@ template <typename T, int DP>
 static int attn_split_launch(const AttnArgs &a, hipStream_t s)
 {
     const unsigned blocks = (unsigned)a.B * a.Hkv * a.tiles * a.splits;
-    const size_t lds = SplitLds<T, DP>::AREA + 2 * SPLIT_WAVES<T> * 32 * sizeof(float) + (a.buckets ? 2 * a.bk.far + 1 : 0);
+    const size_t lds = SplitLds<T, DP>::AREA + 2 * SPLIT_WAVES * 32 * sizeof(float) + (a.buckets ? a.buckets * a.tile_heads * sizeof(float) + 2 * a.bk.far + 1 : 0);
     int st = PF_OK;
     if (a.buckets)
-        PF_LAUNCH_LDS(st, "attn_split", (attn_split_kernel<T, DP, true>), dim3(blocks), dim3(64 * SPLIT_WAVES<T>), lds, s, a);
+        PF_LAUNCH_LDS(st, "attn_split", (attn_split_kernel<T, DP, true>), dim3(blocks), dim3(64 * SPLIT_WAVES), lds, s, a);
     else
-        PF_LAUNCH_LDS(st, "attn_split", (attn_split_kernel<T, DP, false>), dim3(blocks), dim3(64 * SPLIT_WAVES<T>), lds, s, a);
+        PF_LAUNCH_LDS(st, "attn_split", (attn_split_kernel<T, DP, false>), dim3(blocks), dim3(64 * SPLIT_WAVES), lds, s, a);
     if (a.splits > 1) {
         const i64 rows = (i64)a.B * a.Hkv * a.rows;
         PF_LAUNCH(st, "attn_join", attn_join_kernel<T>, dim3((unsigned)((rows + 3) / 4)), dim3(256), s, a, DP);
@@ -251,6 +294,7 @@ int attn_split_fwd(const pf_attention_desc *d, AttnArgs &a, void *workspace, hip
     a.splits = attn_split_count(d);
     a.rows = a.Lq * a.G;
     a.tiles = (a.rows + 31) / 32;
+    a.tile_heads = a.G < 31 / a.Lq + 2 ? a.G : 31 / a.Lq + 2; // heads that 32 rows may touch
     const int DP = padded(a.D);
     if (a.splits > 1) {
         const size_t pieces = (size_t)a.B * a.Hkv * a.tiles * a.splits;
