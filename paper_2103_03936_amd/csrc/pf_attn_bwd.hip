@@ -18,21 +18,26 @@ namespace pf {
 // to is zero from the start and stays so.
 constexpr int DIAG = 32 * 64;
 
-template <typename T, int DP>
-struct BwdLds {
-    using Tq = Tile<T, DP, 32, 256>;
-    static constexpr size_t TILES = 4 * Tq::BYTES + 4 * DIAG * 4 > 5 * Tq::BYTES ? 4 * Tq::BYTES + 4 * DIAG * 4 : 5 * Tq::BYTES;
-    static size_t dq(int far, bool bias, bool tab)
+template <typename T, int DP, int KW>
+struct DqLds {
+    using Tl = Tile<T, DP, 32 * KW, 256>;
+    // three groups of keys, two of values; with the table's gradient then, over them, two of each and the waves' blocks
+    static constexpr size_t TILES = 4 * Tl::BYTES + 4 * DIAG * 4 > 5 * Tl::BYTES ? 4 * Tl::BYTES + 4 * DIAG * 4 : 5 * Tl::BYTES;
+    static size_t bytes(int far, bool bias, bool tab)
     {
-        // three groups of keys, two of values; with the table's gradient then, over them, two of each and the waves' blocks
-        return (tab ? TILES + 4 * (2 * far + 1) * 4 : 5 * Tq::BYTES) + (bias ? (2 * far + 1) * 4 : 0);
+        return (tab ? TILES + 4 * (2 * far + 1) * 4 : 5 * Tl::BYTES) + (bias ? (2 * far + 1) * 4 : 0);
     }
+};
+template <typename T, int DP>
+struct DkvLds {
+    using Tq = Tile<T, DP, 32, 256>;
     // dK and dV: how many waves share the queries (what six tiles of float rows take leaves room for one)
     static constexpr int QW = sizeof(T) == 4 && DP > 64 ? 1 : 2;
-    static size_t dkv(int far, bool bias) { return 6 * QW * Tq::BYTES + 3 * 2 * 32 * QW * 4 + (bias ? (2 * far + 1) * 4 : 0); }
+    static size_t bytes(int far, bool bias) { return 6 * QW * Tq::BYTES + 3 * 2 * 32 * QW * 4 + (bias ? (2 * far + 1) * 4 : 0); }
 };
 
 // dQ, delta and the sums of dS by distance, for one tile of 128 queries of one head.  TAB: with the gradient of the table.
+// KW: waves that share queries, each with 32 keys of a group of 32 KW (the tile has 128 / KW queries).
 //
 // A turn of the loop has S and dP of 32 keys in registers.  It works out dS while the matrix unit makes S and dP of the next 32,
 // then adds dS K to dQ.  Three groups of keys and two of values are in LDS: those whose columns dQ needs, those whose rows S and dP
@@ -42,26 +47,27 @@ struct BwdLds {
 // distances, it keeps the sums of dS and of P of each row, and it sums all dS of a row: that sum is what delta is off by. The
 // second pass goes over the near blocks alone, for their dS with the delta that is now exact (S and dP, two products of the
 // first pass's three); the far sums are put right by their sums of P.
-template <typename T, int DP, bool BIAS, bool TAB>
+template <typename T, int DP, bool BIAS, bool TAB, int KW>
 __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b, int head, int tile)
 {
-    using Tl = Tile<T, DP, 32, 256>;
-    constexpr int CH = DP / 16, DB = DP / 32, AHEAD = 2;
+    using Tl = Tile<T, DP, 32 * KW, 256>;
+    constexpr int CH = DP / 16, DB = DP / 32, AHEAD = 2, STEP = 32 * KW, QUERIES = 128 / KW;
     const int far = a.bk.far, span = 2 * far + 1;
     T *const kb = (T *)lds, *const vb = kb + 3 * Tl::SIZE;
     // the waves' blocks of dS (second pass), their sums by distance [span]
     float *const diag_all = (float *)(lds + 4 * Tl::BYTES);
-    float *const bias = (float *)(lds + (TAB ? BwdLds<T, DP>::TILES : 5 * Tl::BYTES)), *const sums_all = bias + span;
+    float *const bias = (float *)(lds + (TAB ? DqLds<T, DP, KW>::TILES : 5 * Tl::BYTES)), *const sums_all = bias + span;
 
     const int t = threadIdx.x, wave = wave_of(t), lane = t & 63, col = lane & 31, h = lane >> 5;
     float *const diag = diag_all + wave * DIAG, *const sums = sums_all + wave * span;
     const AttnLens n(a, b);
-    const int i0 = tile * 128 + wave * 32, i = i0 + col;
+    const int kw = wave % KW, own = 32 * kw; // the wave's keys begin there in a group
+    const int i0 = tile * QUERIES + wave / KW * 32, i = i0 + col;
     const bool ok = i < n.nq;
     const T *const Kp = (const T *)a.K + b * a.ks[0] + head / a.G * a.ks[2], *const Vp = (const T *)a.V + b * a.vs[0] + head / a.G * a.vs[2];
     int keys = n.nk;
-    if (tile * 128 >= n.nq) keys = 0;
-    const int block_last = (tile * 128 + 128 < n.nq ? tile * 128 + 128 : n.nq) - 1 + n.start;
+    if (tile * QUERIES >= n.nq) keys = 0;
+    const int block_last = (tile * QUERIES + QUERIES < n.nq ? tile * QUERIES + QUERIES : n.nq) - 1 + n.start;
     if (a.causal && block_last + 1 < keys) keys = block_last + 1 < 0 ? 0 : block_last + 1;
     const int last = (i0 + 32 < n.nq ? i0 + 32 : n.nq) - 1, pmin = i0 + n.start, pmax = last + n.start, pos = i + n.start;
     int mine = i0 >= n.nq ? 0 : keys; // of the keys, those that the wave's queries see
@@ -91,7 +97,7 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b
     float lse2 = INFINITY;
     if (ok) {
         const float x = a.lse_in[stat];
-        if (x > -INFINITY) lse2 = x * LOG2E;
+        if (x != -INFINITY) lse2 = x * LOG2E;
     }
     const float sl2 = a.scale * LOG2E;
     f32x16_t dq[DB];
@@ -100,14 +106,14 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b
     float before = 0.f, after = 0.f, before_p = 0.f, after_p = 0.f, off = 0.f; // far sums of dS and P; the sum of all dS
 
     const Tl kl(a.ks[1], a.D, t), vl(a.vs[1], a.D, t);
-    const int rows = Tl::row_place(lane), cols = Tl::col_place(lane);
+    const int rows = Tl::row_place(lane) + own * Tl::RB, cols = Tl::col_place(lane) + own * Tl::RB; // (turn() repeats after 16 rows)
     const auto near_at = [&](int k0) { return BIAS && k0 + 31 - pmin > -far && k0 - pmax < far; };
     const auto fetch = [&](int j, int kslot, int vslot) {
-        kl.fetch(kb + kslot * Tl::SIZE, Kp + (i64)(32 * j) * a.ks[1], a.ks[1], n.nk - 32 * j, a.D, wave);
-        vl.fetch(vb + vslot * Tl::SIZE, Vp + (i64)(32 * j) * a.vs[1], a.vs[1], n.nk - 32 * j, a.D, wave);
+        kl.fetch(kb + kslot * Tl::SIZE, Kp + (i64)(STEP * j) * a.ks[1], a.ks[1], keys - STEP * j, a.D, wave);
+        vl.fetch(vb + vslot * Tl::SIZE, Vp + (i64)(STEP * j) * a.vs[1], a.vs[1], keys - STEP * j, a.D, wave);
     };
     const auto finish = [&](f32x16_t &s, int k0) { finish_scores<BIAS>(s, sl2, lse2, bias, far, anew(k0 + 4 * h - pos), 1, most); };
-    const int groups = (keys + 31) / 32; // of 32 keys
+    const int groups = (keys + STEP - 1) / STEP; // of STEP keys
     if (groups > 0) {
         fetch(0, 0, 0);
         fetched();
@@ -117,9 +123,9 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b
     int slot = 2; // of group j
     const auto turn = [&](int j, f32x16_t &s, f32x16_t &dp, f32x16_t &next, f32x16_t &dnext) {
         const int s1 = slot == 2 ? 0 : slot + 1, s2 = slot == 0 ? 2 : slot - 1; // of groups j + 1, j + 2
-        const int k0 = 32 * j;
+        const int k0 = STEP * j + own; // the wave's first key
         if (j + 2 < groups) fetch(j + 2, s2, j & 1);
-        const bool now = j >= 0 && k0 < mine, then = k0 + 32 < mine;
+        const bool now = j >= 0 && k0 < mine, then = k0 + STEP < mine;
         if (now || then) {
             const int krow = s1 * Tl::BYTES + rows, vrow = (3 + ((j + 1) & 1)) * Tl::BYTES + rows, kcol = slot * Tl::BYTES + cols;
             // S and dP in turn, then dQ: 16 keys after 16 keys
@@ -193,7 +199,26 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b
         turn(j, sA, dpA, sB, dpB);
         if (j + 1 < groups) turn(j + 1, sB, dpB, sA, dpA);
     }
-    if (i < a.Lq) {
+    if constexpr (KW == 2) { // the second wave's dQ to the first, the sums of dS to both (the loop ended with a barrier)
+        float *const part = (float *)lds + wave / KW * (DP / 2) * 64 + lane, *const sum = (float *)lds + DP * 64 + lane;
+        if (kw == 1) {
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) part[(16 * d + e) * 64] = dq[d][e];
+        }
+        sum[wave * 64] = off;
+        __syncthreads();
+        if (kw == 0) {
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) dq[d][e] += part[(16 * d + e) * 64];
+        }
+        off = sum[(wave & ~1) * 64] + sum[(wave | 1) * 64];
+        __syncthreads();
+    }
+    if (i < a.Lq && kw == 0) {
         T *const out = (T *)a.dQ + at;
 #pragma unroll
         for (int d = 0; d < DB; ++d)
@@ -212,18 +237,18 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b
         before -= off * before_p;
         after -= off * after_p;
     }
-    if (i < a.Lq && h == 0) *(float2 *)(a.delta + 2 * stat) = make_float2(lse2, ok ? -delta : 0.f);
+    if (i < a.Lq && h == 0 && kw == 0) *(float2 *)(a.delta + 2 * stat) = make_float2(lse2, ok ? -delta : 0.f);
     if constexpr (TAB) {
         // (two groups of keys, two of values)
         const auto fetch2 = [&](int j) { fetch(j, j & 1, (j & 1) - 1); };
-        // the near blocks once more: 32 begin + 31 > first position - far, 32 (end - 1) < last position + far
+        // the near blocks once more: STEP begin + STEP - 1 > first position - far, STEP (end - 1) < last position + far
         int begin = 0, end = groups;
-        const int lo = tile * 128 + n.start - far - 31, hi = block_last + far;
-        if (lo >= 0) begin = lo / 32 + 1;
+        const int lo = tile * QUERIES + n.start - far - (STEP - 1), hi = block_last + far;
+        if (lo >= 0) begin = lo / STEP + 1;
         if (hi <= 0)
             end = 0;
-        else if ((hi + 31) / 32 < end)
-            end = (hi + 31) / 32;
+        else if ((hi + STEP - 1) / STEP < end)
+            end = (hi + STEP - 1) / STEP;
         if (begin < end) {
             for (int x = t; x < 4 * DIAG; x += 256) diag_all[x] = 0.f;
             fetch2(begin);
@@ -231,7 +256,7 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b
             __syncthreads();
         }
         for (int j = begin; j < end; ++j) {
-            const int k0 = 32 * j;
+            const int k0 = STEP * j + own;
             if (j + 1 < end) fetch2(j + 1);
             if (k0 < mine && near_at(k0)) {
                 const int at_j = (j & 1) * Tl::BYTES + rows;
@@ -310,7 +335,7 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b
 }
 
 // paired: a long tile of queries and a short one to a workgroup, as forward
-template <typename T, int DP, bool BIAS, bool TAB>
+template <typename T, int DP, bool BIAS, bool TAB, int KW>
 __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void attn_dq_kernel(AttnArgs a, int paired)
 {
     extern __shared__ __attribute__((aligned(16))) char lds[];
@@ -319,9 +344,26 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void attn_dq_ke
     const int count = paired && a.tiles - 1 - k != k ? 2 : 1;
 #pragma unroll 1
     for (int x = 0; x < count; ++x) {
-        attn_dq_tile<T, DP, BIAS, TAB>(a, lds, b, head, x ? k : a.tiles - 1 - k);
+        attn_dq_tile<T, DP, BIAS, TAB, KW>(a, lds, b, head, x ? k : a.tiles - 1 - k);
         __syncthreads();
     }
+}
+
+// dtable[u][head] from the tiles' sums: one wave to a value, in double and always in one order
+struct TableSum {
+    float *dtable; // or none
+    int parts, accumulate;
+    unsigned after; // the workgroups of the launch that come before these
+};
+__device__ __forceinline__ void attn_table(const AttnArgs &a, const TableSum &z, int value, int lane)
+{
+    if (value >= a.buckets * a.Hq) return;
+    const int u = value % a.buckets, head = value / a.buckets;
+    double y = 0.0;
+    for (int p = lane; p < z.parts; p += 64) y += (double)a.tab[((i64)head * z.parts + p) * a.buckets + u];
+    for (int o = 32; o; o >>= 1) y += __shfl_xor(y, o);
+    float *const out = z.dtable + (i64)u * a.Hq + head;
+    if (lane == 0) *out = z.accumulate ? *out + (float)y : (float)y;
 }
 
 // dK and dV: a workgroup has 64 keys of one key head, a wave 32 of them in its columns; the query heads of the key head one
@@ -330,9 +372,9 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void attn_dq_ke
 // one wave, a causal mask's longest column alone, 512 blocks of 2 x 4096 tokens with four query heads to a key head, took 765 us:
 // the time of the whole kernel.)
 template <typename T, int DP, bool BIAS>
-__global__ __launch_bounds__((128 * BwdLds<T, DP>::QW), (DP * sizeof(T) <= 128 ? 2 : 1)) void attn_dkv_kernel(AttnArgs a)
+__global__ __launch_bounds__((128 * DkvLds<T, DP>::QW), (DP * sizeof(T) <= 128 ? 2 : 1)) void attn_dkv_kernel(AttnArgs a, TableSum z)
 {
-    constexpr int QW = BwdLds<T, DP>::QW, ROWS = 32 * QW, THREADS = 128 * QW;
+    constexpr int QW = DkvLds<T, DP>::QW, ROWS = 32 * QW, THREADS = 128 * QW;
     using Tl = Tile<T, DP, ROWS, THREADS>;
     constexpr int CH = DP / 16, DB = DP / 32, AHEAD = DP * sizeof(T) <= 128 ? 3 : sizeof(T) == 2 ? 6 : 3; // (one wave to a unit needs more on the way)
     extern __shared__ __attribute__((aligned(16))) char lds[];
@@ -340,7 +382,8 @@ __global__ __launch_bounds__((128 * BwdLds<T, DP>::QW), (DP * sizeof(T) <= 128 ?
     float *const stats = (float *)(lds + 6 * Tl::BYTES); // [3][2][ROWS]: lse (base 2) and -delta of each query
     float *const bias = stats + 3 * 2 * ROWS;
 
-    const unsigned w = xcd_order(blockIdx.x, gridDim.x);
+    if (blockIdx.x >= z.after) return attn_table(a, z, (int)(blockIdx.x - z.after) * 2 * QW + (threadIdx.x >> 6), threadIdx.x & 63);
+    const unsigned w = xcd_order(blockIdx.x, z.after);
     const int tile = (int)(w % a.tiles), bk = w / a.tiles, b = bk / a.Hkv, kv = bk - b * a.Hkv;
     const int t = threadIdx.x, wave = wave_of(t), lane = t & 63, col = lane & 31, h = lane >> 5;
     const AttnLens n(a, b);
@@ -512,47 +555,59 @@ __global__ __launch_bounds__((128 * BwdLds<T, DP>::QW), (DP * sizeof(T) <= 128 ?
         }
 }
 
-// dtable[u][head] from the workgroups' sums: one wave to a value, in double and always in one order
-__global__ __launch_bounds__(64) void attn_table_kernel(const float *tab, int parts, int buckets, int heads, float *dtable, int accumulate)
+// ------------------------------------------------------------------ host
+template <typename T, int DP, int KW>
+static int attn_dq_launch(AttnArgs &a, bool tab, hipStream_t s)
 {
-    const int u = blockIdx.x % buckets, head = blockIdx.x / buckets, lane = threadIdx.x;
-    double y = 0.0;
-    for (int p = lane; p < parts; p += 64) y += (double)tab[((i64)head * parts + p) * buckets + u];
-    for (int o = 32; o; o >>= 1) y += __shfl_xor(y, o);
-    float *const out = dtable + (i64)u * heads + head;
-    if (lane == 0) *out = accumulate ? *out + (float)y : (float)y;
+    int st = PF_OK;
+    a.tiles = (a.Lq + 128 / KW - 1) / (128 / KW);
+    const int paired = a.causal && (i64)a.B * a.Hq * a.tiles > 512; // (two workgroups to a compute unit are resident)
+    const dim3 grid((unsigned)a.B * a.Hq * (paired ? (a.tiles + 1) / 2 : a.tiles));
+    const size_t lds = DqLds<T, DP, KW>::bytes(a.bk.far, a.buckets, tab);
+    if (a.Lq == 0) return st;
+    if (tab)
+        PF_LAUNCH_LDS(st, "attn_dq_tab", (attn_dq_kernel<T, DP, true, true, KW>), grid, dim3(256), lds, s, a, paired);
+    else if (a.buckets)
+        PF_LAUNCH_LDS(st, "attn_dq", (attn_dq_kernel<T, DP, true, false, KW>), grid, dim3(256), lds, s, a, paired);
+    else
+        PF_LAUNCH_LDS(st, "attn_dq", (attn_dq_kernel<T, DP, false, false, KW>), grid, dim3(256), lds, s, a, paired);
+    return st;
+}
+// Waves that share queries: as forward, two where that makes no more workgroups than fit the card at once (rows of more than 128
+// bytes: one to a compute unit; of more than 256: no room for it).  us, bf16, 8 heads of 64 with the table: 2 x 1024 tokens, 128
+// tiles, 50 alone and 33 shared; 4 x 1024, 256 tiles, 51 and 40; 6 x 1024 64 and 62; float, 8 x 512, 256 tiles, 105 and 117.
+static int dq_sharing(i64 B, i64 Hq, i64 Lq, size_t row)
+{
+    return row <= 256 && B * Hq * ((Lq + 127) / 128) <= (row <= 128 ? 256 : 128) ? 2 : 1;
+}
+static int padded(int D) { return (D + 31) / 32 * 32; }
+static i64 dq_tiles(i64 B, i64 Hq, i64 Lq, size_t row)
+{
+    const int queries = 128 / dq_sharing(B, Hq, Lq, row);
+    return (Lq + queries - 1) / queries;
 }
 
-// ------------------------------------------------------------------ host
 template <typename T, int DP>
 static int attn_bwd_launch(AttnArgs &a, float *dtable, int accumulate, hipStream_t s)
 {
     const bool bias = a.buckets > 0, tab = bias && dtable;
-    int st = PF_OK;
-    a.tiles = (a.Lq + 127) / 128;
+    int st;
+    if constexpr (DP * sizeof(T) <= 256)
+        st = dq_sharing(a.B, a.Hq, a.Lq, DP * sizeof(T)) == 2 ? attn_dq_launch<T, DP, 2>(a, tab, s) : attn_dq_launch<T, DP, 1>(a, tab, s);
+    else
+        st = attn_dq_launch<T, DP, 1>(a, tab, s);
     const int parts = a.B * a.tiles;
-    const int paired = a.causal && (i64)a.B * a.Hq * a.tiles > 512; // (two workgroups to a compute unit are resident)
-    const dim3 grid((unsigned)a.B * a.Hq * (paired ? (a.tiles + 1) / 2 : a.tiles));
-    const size_t lds = BwdLds<T, DP>::dq(a.bk.far, bias, tab);
-    if (a.Lq > 0) {
-        if (tab)
-            PF_LAUNCH_LDS(st, "attn_dq_tab", (attn_dq_kernel<T, DP, true, true>), grid, dim3(256), lds, s, a, paired);
-        else if (bias)
-            PF_LAUNCH_LDS(st, "attn_dq", (attn_dq_kernel<T, DP, true, false>), grid, dim3(256), lds, s, a, paired);
-        else
-            PF_LAUNCH_LDS(st, "attn_dq", (attn_dq_kernel<T, DP, false, false>), grid, dim3(256), lds, s, a, paired);
-    }
-    if (a.Lk > 0) {
-        a.tiles = (a.Lk + 63) / 64;
-        const dim3 kgrid((unsigned)a.B * a.Hkv * a.tiles);
-        const size_t klds = BwdLds<T, DP>::dkv(a.bk.far, bias);
-        if (bias)
-            PF_LAUNCH_LDS(st, "attn_dkv", (attn_dkv_kernel<T, DP, true>), kgrid, dim3(128 * BwdLds<T, DP>::QW), klds, s, a);
-        else
-            PF_LAUNCH_LDS(st, "attn_dkv", (attn_dkv_kernel<T, DP, false>), kgrid, dim3(128 * BwdLds<T, DP>::QW), klds, s, a);
-    }
-    if (tab)
-        PF_LAUNCH(st, "attn_table", attn_table_kernel, dim3((unsigned)a.buckets * a.Hq), dim3(64), s, a.tab, parts, a.buckets, a.Hq, dtable, accumulate);
+    // behind the workgroups for the keys, those that sum up the table's gradient (a launch of their own took 5 us)
+    constexpr int WAVES = 2 * DkvLds<T, DP>::QW;
+    a.tiles = (a.Lk + 63) / 64;
+    const TableSum z = {dtable, parts, accumulate, (unsigned)a.B * a.Hkv * a.tiles};
+    const dim3 kgrid(z.after + (tab ? (a.buckets * a.Hq + WAVES - 1) / WAVES : 0));
+    const size_t klds = DkvLds<T, DP>::bytes(a.bk.far, bias);
+    if (kgrid.x == 0) return st;
+    if (bias)
+        PF_LAUNCH_LDS(st, "attn_dkv", (attn_dkv_kernel<T, DP, true>), kgrid, dim3(64 * WAVES), klds, s, a, z);
+    else
+        PF_LAUNCH_LDS(st, "attn_dkv", (attn_dkv_kernel<T, DP, false>), kgrid, dim3(64 * WAVES), klds, s, a, z);
     return st;
 }
 static size_t delta_bytes(const pf_attention_desc *d) { return align_up((size_t)d->B * d->heads_q * d->Lq * 2 * sizeof(float)); }
@@ -566,7 +621,8 @@ using namespace pf;
 size_t pf_attention_bwd_workspace_bytes(const pf_attention_desc *d)
 {
     if (attn_check(d) != PF_OK || d->B == 0 || d->Lq == 0) return 0;
-    return delta_bytes(d) + align_up((size_t)d->heads_q * d->B * ((d->Lq + 127) / 128) * d->buckets * sizeof(float));
+    const i64 tiles = dq_tiles(d->B, d->heads_q, d->Lq, padded(d->head_dim) * (d->dtype == PF_BF16 ? 2 : 4));
+    return delta_bytes(d) + align_up((size_t)d->heads_q * d->B * tiles * d->buckets * sizeof(float));
 }
 
 int pf_attention_bwd(const pf_attention_desc *d, const void *Q, const void *K, const void *V, const void *table, const void *q_start,

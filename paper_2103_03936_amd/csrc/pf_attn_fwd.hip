@@ -1,7 +1,8 @@
 // Attention with a relative position bias by buckets, forward: pf_attention_fwd.
 //
 // A workgroup has 128 queries of one head, a wave 32 of them in its columns (pf_attn.h); keys and values pass through LDS
-// in tiles, the next one loaded into registers while this one is used.  One pass over the keys with the running maximum and
+// in tiles, the next ones on their way while this one is used.  Where that makes too few workgroups, it has 64, and two waves
+// share their queries, each with half of the keys of a tile.  One pass over the keys with the running maximum and
 // sum of each query; the score matrix, the bias and P exist in registers only.
 #include "pf_attn.h"
 
@@ -12,24 +13,26 @@ constexpr int KEYS = sizeof(T) == 2 ? 64 : 32; // keys of a tile
 
 // One tile of queries.  A turn of the loop has the scores of its keys in registers; their exponentials are worked out while
 // the matrix unit makes the next turn's scores, and the largest of those is found while it multiplies P and V.
-template <typename T, int DP, bool BIAS>
+// KW: waves that share queries.
+template <typename T, int DP, bool BIAS, int KW>
 __device__ __forceinline__ void attn_fwd_tile(const AttnArgs &a, char *lds, int b, int head, int tile)
 {
-    constexpr int KT = KEYS<T>, SUB = KT / 32;
-    using Tl = Tile<T, DP, KT, 256>;
+    constexpr int KT = KEYS<T>, SUB = KT / 32, STEP = KT * KW, QUERIES = 128 / KW; // a wave's keys of a tile; all; the workgroup's queries
+    using Tl = Tile<T, DP, STEP, 256>;
     T *const kb = (T *)lds, *const vb = kb + 2 * Tl::SIZE; // two tiles of keys, two of values
     float *const bias = (float *)(lds + 4 * Tl::BYTES);
 
     const int t = threadIdx.x, wave = wave_of(t), lane = t & 63, col = lane & 31, h = lane >> 5;
     const AttnLens n(a, b);
-    const int i0 = tile * 128 + wave * 32, i = i0 + col; // the lane's query
+    const int kw = wave % KW, own = KT * kw;                           // the wave's keys begin there in a tile
+    const int i0 = tile * QUERIES + wave / KW * 32, i = i0 + col; // the lane's query
     const bool ok = i < n.nq;
 
     const T *const Kp = (const T *)a.K + b * a.ks[0] + head / a.G * a.ks[2], *const Vp = (const T *)a.V + b * a.vs[0] + head / a.G * a.vs[2];
     // keys that some query of the workgroup sees, and that some query of the wave sees
     int keys = n.nk;
-    if (tile * 128 >= n.nq) keys = 0;
-    const int block_last = (tile * 128 + 128 < n.nq ? tile * 128 + 128 : n.nq) - 1 + n.start; // positions
+    if (tile * QUERIES >= n.nq) keys = 0;
+    const int block_last = (tile * QUERIES + QUERIES < n.nq ? tile * QUERIES + QUERIES : n.nq) - 1 + n.start; // positions
     if (a.causal && block_last + 1 < keys) keys = block_last + 1 < 0 ? 0 : block_last + 1;
     const int last = (i0 + 32 < n.nq ? i0 + 32 : n.nq) - 1, pmin = i0 + n.start, pmax = last + n.start, pos = i + n.start;
     const int most = a.causal && n.nk > pos ? 0 : n.nk - 1 - pos; // the furthest distance seen
@@ -37,12 +40,12 @@ __device__ __forceinline__ void attn_fwd_tile(const AttnArgs &a, char *lds, int 
     if (a.causal && mine > 0 && pmax + 1 < mine) mine = pmax + 1 < 0 ? 0 : pmax + 1;
 
     const Tl kl(a.ks[1], a.D, t), vl(a.vs[1], a.D, t);
-    const auto fetch_keys = [&](int k0, int odd) { kl.fetch(kb + odd * Tl::SIZE, Kp + (i64)k0 * a.ks[1], a.ks[1], n.nk - k0, a.D, wave); };
-    const auto fetch_values = [&](int k0, int odd) { vl.fetch(vb + odd * Tl::SIZE, Vp + (i64)k0 * a.vs[1], a.vs[1], n.nk - k0, a.D, wave); };
+    const auto fetch_keys = [&](int k0, int odd) { kl.fetch(kb + odd * Tl::SIZE, Kp + (i64)k0 * a.ks[1], a.ks[1], keys - k0, a.D, wave); };
+    const auto fetch_values = [&](int k0, int odd) { vl.fetch(vb + odd * Tl::SIZE, Vp + (i64)k0 * a.vs[1], a.vs[1], keys - k0, a.D, wave); };
     if (keys > 0) {
         fetch_keys(0, 0);
         fetch_values(0, 0);
-        if (keys > KT) fetch_keys(KT, 1);
+        if (keys > STEP) fetch_keys(STEP, 1);
         if constexpr (BIAS) fill_bias(a, bias, head, t, 256);
     }
     Frag<T> q[DP / 16];
@@ -59,11 +62,11 @@ __device__ __forceinline__ void attn_fwd_tile(const AttnArgs &a, char *lds, int 
     float m = -INFINITY, sum = 0.f; // the maximum that values are taken relative to (base 2); the sum of the lane's keys
     float top = -INFINITY;
     f32x16_t s0[SUB], s1[SUB];
-    const int rows = Tl::row_place(lane), cols = Tl::col_place(lane);
+    const int rows = Tl::row_place(lane) + own * Tl::RB, cols = Tl::col_place(lane) + own * Tl::RB; // (turn() repeats after 16 rows)
     constexpr int CH = DP / 16, SC = SUB * CH, DB = DP / 32, PV = 2 * SUB * DB, AHEAD = 3;
     fetched();
     __syncthreads();
-    if (mine > 0) {
+    if (own < mine) {
 #pragma unroll
         for (int u = 0; u < SUB; ++u) {
             s0[u] = f32x16_t{};
@@ -74,10 +77,11 @@ __device__ __forceinline__ void attn_fwd_tile(const AttnArgs &a, char *lds, int 
         }
     }
     __syncthreads();
-    // keys k0 .. with their scores in s; `odd`: which of the two tiles they are in
-    const auto turn = [&](int k0, int odd, f32x16_t (&s)[SUB], f32x16_t (&next)[SUB]) {
-        if (k0 + 2 * KT < keys) fetch_keys(k0 + 2 * KT, odd);
-        if (k0 + KT < keys) fetch_values(k0 + KT, !odd);
+    // the tile from key t0 on with the scores of the wave's keys in s; `odd`: which of the two places it is in
+    const auto turn = [&](int t0, int odd, f32x16_t (&s)[SUB], f32x16_t (&next)[SUB]) {
+        if (t0 + 2 * STEP < keys) fetch_keys(t0 + 2 * STEP, odd);
+        if (t0 + STEP < keys) fetch_values(t0 + STEP, !odd);
+        const int k0 = t0 + own;
         if (k0 < mine) {
             const bool edge = k0 + KT > n.nk || (a.causal && k0 + KT - 1 > pmin);
             const bool near = BIAS && k0 + KT - 1 - pmin > -far && k0 - pmax < far;
@@ -152,13 +156,33 @@ __device__ __forceinline__ void attn_fwd_tile(const AttnArgs &a, char *lds, int 
         fetched();
         __syncthreads();
     };
-    for (int k0 = 0; k0 < keys; k0 += 2 * KT) {
-        turn(k0, 0, s0, s1);
-        if (k0 + KT < keys) turn(k0 + KT, 1, s1, s0);
+    for (int t0 = 0; t0 < keys; t0 += 2 * STEP) {
+        turn(t0, 0, s0, s1);
+        if (t0 + STEP < keys) turn(t0 + STEP, 1, s1, s0);
     }
     sum += __shfl_xor(sum, 32);
+    if constexpr (KW == 2) { // the second wave's part to the first (the loop ended with a barrier: the tiles' room is free)
+        float *const part = (float *)lds + wave / KW * (DP / 2 + 2) * 64 + lane;
+        if (kw == 1) {
+            part[0] = m, part[64] = sum;
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) part[(2 + 16 * d + e) * 64] = o[d][e];
+        }
+        __syncthreads();
+        if (kw == 1) return;
+        const float m1 = part[0], both = fmaxf(m, m1), base = both == -INFINITY ? 0.f : both;
+        const float f = exp2_fast(m - base), f1 = exp2_fast(m1 - base);
+        sum = sum * f + part[64] * f1;
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[d][e] = o[d][e] * f + part[(2 + 16 * d + e) * 64] * f1;
+        m = both;
+    }
     if (i >= a.Lq) return;
-    const bool some = ok && sum > 0.f;
+    const bool some = ok && sum != 0.f;
     const float inv = some ? 1.f / sum : 0.f;
     T *const Op = (T *)a.O + (((i64)b * a.Lq + i) * a.Hq + head) * a.D;
 #pragma unroll
@@ -176,7 +200,7 @@ __device__ __forceinline__ void attn_fwd_tile(const AttnArgs &a, char *lds, int 
 
 // paired: a workgroup has a long tile of queries and a short one (causal; a.tiles of them to a head), so that all take the
 // same time
-template <typename T, int DP, bool BIAS>
+template <typename T, int DP, bool BIAS, int KW>
 __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void attn_fwd_kernel(AttnArgs a, int paired)
 {
     extern __shared__ __attribute__((aligned(16))) char lds[];
@@ -185,7 +209,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void attn_f
     const int other = paired && a.tiles - 1 - k != k ? 2 : 1;
 #pragma unroll 1
     for (int pass = 0; pass < other; ++pass) {
-        attn_fwd_tile<T, DP, BIAS>(a, lds, b, head, pass ? k : a.tiles - 1 - k);
+        attn_fwd_tile<T, DP, BIAS, KW>(a, lds, b, head, pass ? k : a.tiles - 1 - k);
         __syncthreads();
     }
 }
@@ -251,20 +275,30 @@ void attn_fill(const pf_attention_desc *d, AttnArgs &a)
     }
 }
 
-template <typename T, int DP>
-static int attn_fwd_launch(const AttnArgs &a, hipStream_t s)
+template <typename T, int DP, int KW>
+static int attn_fwd_launch(AttnArgs &a, hipStream_t s)
 {
-    using Tl = Tile<T, DP, KEYS<T>, 256>;
+    using Tl = Tile<T, DP, KEYS<T> * KW, 256>;
+    a.tiles = (a.Lq + 128 / KW - 1) / (128 / KW);
     // two workgroups to a compute unit are resident: causal tiles are paired where there are more
     const bool paired = a.causal && (i64)a.B * a.Hq * a.tiles > 512;
     const unsigned blocks = (unsigned)a.B * a.Hq * (paired ? (a.tiles + 1) / 2 : a.tiles);
     const size_t lds = 4 * Tl::BYTES + (a.buckets ? (2 * a.bk.far + 1) * sizeof(float) : 0);
     int st = PF_OK;
     if (a.buckets)
-        PF_LAUNCH_LDS(st, "attn_fwd", (attn_fwd_kernel<T, DP, true>), dim3(blocks), dim3(256), lds, s, a, (int)paired);
+        PF_LAUNCH_LDS(st, "attn_fwd", (attn_fwd_kernel<T, DP, true, KW>), dim3(blocks), dim3(256), lds, s, a, (int)paired);
     else
-        PF_LAUNCH_LDS(st, "attn_fwd", (attn_fwd_kernel<T, DP, false>), dim3(blocks), dim3(256), lds, s, a, (int)paired);
+        PF_LAUNCH_LDS(st, "attn_fwd", (attn_fwd_kernel<T, DP, false, KW>), dim3(blocks), dim3(256), lds, s, a, (int)paired);
     return st;
+}
+// Two waves share queries where that makes no more workgroups than fit the card at once, two to a compute unit if the tiles of
+// both fit its LDS (us, bf16, 8 heads: 2 x 1024 tokens of 64 columns, 128 tiles, 25 alone and 18 shared; 4 x 1024, 256 tiles,
+// 26 and 23; 6 x 1024 34 and 33; 512 queries of 32 heads of 128 over 4096 keys, 128 tiles, 80 and 54; twice those 84 and 104)
+template <typename T, int DP>
+static int attn_fwd_launch(AttnArgs &a, hipStream_t s)
+{
+    const bool few = (i64)a.B * a.Hq * ((a.Lq + 127) / 128) <= (DP <= 64 ? 256 : 128);
+    return few ? attn_fwd_launch<T, DP, 2>(a, s) : attn_fwd_launch<T, DP, 1>(a, s);
 }
 
 } // namespace pf
@@ -300,7 +334,6 @@ int pf_attention_fwd(const pf_attention_desc *d, const void *Q, const void *K, c
     a.q_len = (const int *)q_len;
     a.kv_len = (const int *)kv_len;
     if (attn_split_count(d)) return attn_split_fwd(d, a, workspace, (hipStream_t)stream);
-    a.tiles = (a.Lq + 127) / 128;
     const hipStream_t s = (hipStream_t)stream;
     const int DP = (a.D + 31) / 32 * 32;
     if (d->dtype == PF_BF16)

@@ -259,3 +259,37 @@ def test_another_stream_and_graph_replay():
             torch.cuda.synchronize()
             for x, y in zip(outs, eager):
                 assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("c", [(9, 300, 300, 32, 8, 64, False, 32, 128, "pad"), (11, 260, 260, 24, 8, 128, True, 32, 128, None)], ids=str)
+def test_many_tiles(c, dtype):
+    """More tiles of queries than fit the card at once: no two waves share queries; causal tiles are taken in pairs."""
+    test_against_definition(c, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("Lq", [1, 150])
+def test_nan_stays_in_what_uses_it(Lq, dtype):
+    """A NaN in a query reaches that query's results and none else; NaN in keys and values that no query sees reaches none."""
+    import paper_2103_03936_amd as pf
+    d, g, _, kw = _case((2, Lq, 200, 2, 1, 64, True, 32, 128, None), dtype, 77)
+    start = np.asarray([20, 5], dtype=np.int32)
+    kw["q_start"] = torch.from_numpy(start).cuda()
+    o = O.Attention(*(d[k].astype(np.float64) for k in "QKV"), d["table"].astype(np.float64), causal=True, max_distance=128,
+                    bidirectional=False, q_start=start)
+    for b in range(2):
+        g["K"][b, start[b] + Lq:] = float("nan")
+        g["V"][b, start[b] + Lq:] = float("nan")
+    got, lse = pf.pf_attention_fwd(g["Q"], g["K"], g["V"], g["table"], **kw)
+    assert_within(got, o.O, attention_bounds(o, d["dO"].astype(np.float64), dtype)[0], "O")
+    last = (1, Lq - 1, 1), (1, 1, Lq - 1)
+    g["Q"][1, Lq - 1, 1, 3] = float("nan")
+    O2, lse2 = pf.pf_attention_fwd(g["Q"], g["K"], g["V"], g["table"], **kw)
+    assert O2[last[0]].isnan().all() and lse2[last[1]].isnan()
+    dQ = pf.pf_attention_bwd(g["Q"], g["K"], g["V"], O2, lse2, g["dO"], g["table"], **kw)[0]
+    O2[last[0]], lse2[last[1]] = got[last[0]], lse[last[1]]
+    assert torch.equal(O2, got) and torch.equal(lse2, lse)
+    assert dQ[last[0]].isnan().all()
+    dQ[last[0]] = 0
+    assert not dQ.isnan().any()
