@@ -2,9 +2,12 @@
 //
 // Bound by memory: forward reads and writes each value once, backward reads two and writes one.  A wave takes one token at a
 // time, all its heads: a lane holds W pairs of a head (the two values that a rotation mixes are always in one lane), the
-// head_dim / (2 W) lanes of a head add up its squares between them, and 64 / lanes heads are in flight.  The angles belong
-// to the token alone: the wave forms each one once, in double, and its heads read cosine and sine from LDS.
+// head_dim / (2 W) lanes of a head add up its squares between them, and 64 / lanes heads are worked on while the next are on
+// their way.  The angles belong to the token alone: the wave forms each one once, in double, and its heads read cosine and sine
+// from LDS.  2 x 8191 tokens of 40 heads of 128 in bf16: forward 60 us, backward 113 (5.6 and 4.5 TB/s of what they read and
+// write; some of it is still in the caches); without the loads ahead 68 and 117.
 #include <math.h>
+#include <string.h>
 
 #include "pf_gemm.h"
 
@@ -14,7 +17,8 @@ struct QkArgs {
     const void *Q, *K, *dQo, *dKo;
     void *Qo, *Ko, *dQ, *dK;
     const float *gamma[2]; // queries', keys'
-    const int *positions;
+    const int *positions; // given, or any address that can be read
+    int given;
     float *partial; // backward: sums of gamma gradients per workgroup [blocks][2][D]
     int tokens, L, heads[2], D, R, norm;
     float eps;
@@ -22,18 +26,17 @@ struct QkArgs {
     double turns[128];       // revolutions per position of each pair
 };
 
+// W values as they lie in memory
 template <typename T, int W>
-__device__ __forceinline__ void get_values(const T *p, float *x)
-{
-    if constexpr (sizeof(T) == 4) {
-        __builtin_memcpy(x, __builtin_assume_aligned(p, sizeof(T) * W), sizeof(T) * W);
-    } else {
-        uint32_t w[W / 2];
-        __builtin_memcpy(w, __builtin_assume_aligned(p, sizeof(T) * W), sizeof(T) * W);
-#pragma unroll
-        for (int i = 0; i < W; ++i) x[i] = bf16_bits_to_float((uint16_t)(w[i / 2] >> (16 * (i & 1))));
+struct Raw {
+    uint32_t w[W * sizeof(T) / 4];
+    __device__ __forceinline__ void load(const T *p) { __builtin_memcpy(w, __builtin_assume_aligned(p, sizeof(T) * W < 16 ? sizeof(T) * W : 16), sizeof(T) * W); }
+    __device__ __forceinline__ float operator[](int i) const
+    {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+        return bf16_bits_to_float((uint16_t)(w[i / 2] >> (16 * (i & 1))));
     }
-}
+};
 template <typename T, int W>
 __device__ __forceinline__ void put_values(T *p, const float *x)
 {
@@ -46,22 +49,22 @@ __device__ __forceinline__ void put_values(T *p, const float *x)
         __builtin_memcpy(__builtin_assume_aligned(p, sizeof(T) * W), w, sizeof(T) * W);
     }
 }
-// The W pairs of a lane: a[] and b[], from o1 and o2 (halves), or from o1 on, one after the other (pairs)
+// The W pairs of a lane: from o1 and o2 (halves), or from o1 on, one after the other (pairs)
 template <typename T, int W, bool PAIRS>
-__device__ __forceinline__ void get_pairs(const T *head, int o1, int o2, float *a, float *b)
-{
-    if constexpr (PAIRS) {
-        float x[2 * W];
-        constexpr int N = 16 / sizeof(T) < 2 * W ? 16 / sizeof(T) : 2 * W; // (16 bytes at a time)
-#pragma unroll
-        for (int i = 0; i < 2 * W; i += N) get_values<T, N>(head + o1 + i, x + i);
-#pragma unroll
-        for (int i = 0; i < W; ++i) a[i] = x[2 * i], b[i] = x[2 * i + 1];
-    } else {
-        get_values<T, W>(head + o1, a);
-        get_values<T, W>(head + o2, b);
+struct Pairs {
+    Raw<T, PAIRS ? 2 * W : W> x, y; // (pairs: x alone)
+    __device__ __forceinline__ void load(const T *head, int o1, int o2)
+    {
+        x.load(head + o1);
+        if constexpr (!PAIRS) y.load(head + o2);
     }
-}
+    __device__ __forceinline__ float a(int i) const { return PAIRS ? x[2 * i] : x[i]; }
+    __device__ __forceinline__ float b(int i) const
+    {
+        if constexpr (PAIRS) return x[2 * i + 1];
+        return y[i];
+    }
+};
 template <typename T, int W, bool PAIRS>
 __device__ __forceinline__ void put_pairs(T *head, int o1, int o2, const float *a, const float *b)
 {
@@ -78,129 +81,161 @@ __device__ __forceinline__ void put_pairs(T *head, int o1, int o2, const float *
     }
 }
 
-// Sum over the 2^log lanes of a head
+// Sum over the 2^log lanes of a head (log is one number for the wave).  Within 16 lanes the other addend comes with the addition.
+template <int CTRL>
+__device__ __forceinline__ float with_lane(float x)
+{
+    return x + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true));
+}
 __device__ __forceinline__ float head_sum(float x, int log)
 {
-    for (int o = 0; o < log; ++o) x += __shfl_xor(x, 1 << o);
+    if (log > 0) x = with_lane<0xb1>(x);  // lanes 1 0 3 2
+    if (log > 1) x = with_lane<0x4e>(x);  // 2 3 0 1
+    if (log > 2) x = with_lane<0x141>(x); // 7 .. 0 of 8: the four that a quad lacks
+    if (log > 3) x = with_lane<0x140>(x); // 15 .. 0 of 16
+    if (log > 4) x += __shfl_xor(x, 16);
+    if (log > 5) x += __shfl_xor(x, 32);
     return x;
 }
 
 // cos, sin of the token's angles into LDS (the wave's own part).  The angle in revolutions, its fraction within 1/2 of zero,
 // in double: a position of 2^31 leaves 2^-22 of a revolution's digits, float alone would have none left at 2^24.
-__device__ __forceinline__ void token_angles(const QkArgs &a, int pos, float2 *cs, int lane)
+// turns: revolutions per position of the pairs lane and lane + 64.
+__device__ __forceinline__ void token_angles(int pairs, int pos, const double (&turns)[2], float2 *cs, int lane)
 {
-    for (int i = lane; i < a.R / 2; i += 64) {
-        double t = (double)pos * a.turns[i];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        if (64 * k >= pairs) break;
+        double t = (double)pos * turns[k];
         t -= rint(t);
         float s, c;
         sincospif(2.f * (float)t, &s, &c);
-        cs[i] = make_float2(c, s);
+        if (lane + 64 * k < pairs) cs[lane + 64 * k] = make_float2(c, s);
     }
 }
 
 // T, W pairs to a lane, PAIRS, BWD
 template <typename T, int W, bool PAIRS, bool BWD>
-__global__ __launch_bounds__(256) void qk_norm_kernel(QkArgs a, int log)
+__global__ __launch_bounds__(256, 4) void qk_norm_kernel(QkArgs a, int log)
 {
-    __shared__ float2 cs_all[4][128];
-    __shared__ float gam[2][256];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    float2 *cs = cs_all[wave];
-    const int D = a.D, half = a.R / 2, part = (lane & ((1 << log) - 1)) * W; // the lane's first pair
+    __shared__ __attribute__((aligned(16))) float2 cs_all[4][128];
+    __shared__ __attribute__((aligned(16))) float gam[2][256];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    float2 *cs = cs_all[wave]; // cosine and sine for each pair
+    const int D = a.D, half = a.R / 2;
     const int slot = lane >> log, slots = 64 >> log, all = a.heads[0] + a.heads[1];
-    const bool in_head = part < D / 2;
+    // The lane's first pair.  Lanes behind the end of a head, and heads behind the last, do the work of the last one once more:
+    // loads and stores are the same for all lanes and without branches, so that it is known how many are on their way and none is
+    // waited for that need not be.
+    const int own = (lane & ((1 << log) - 1)) * W, part = own < D / 2 ? own : D / 2 - W;
+    const bool in_head = own < D / 2;
     const bool turned = part < half; // (W divides R / 2: a lane's pairs are turned or not, all of them)
     const int o1 = PAIRS ? 2 * part : turned ? part : a.R + part - half;
     const int o2 = PAIRS ? 0 : o1 + (turned ? half : (D - a.R) / 2);
-    if (a.norm)
-        for (int i = threadIdx.x; i < 2 * D; i += 256) {
-            const int k = i >= D, j = k ? i - D : i;
-            gam[k][j] = a.gamma[k] ? a.gamma[k][j] : 1.f;
-        }
+    const float inv_d = 1.f / (float)D;
+
+    // Where a token's heads begin: the same for the whole wave, up to the lane's head
+    const auto place = [&](const void *q, const void *k, const i64 (&sq)[3], const i64 (&sk)[3], int b, int l, int hh) {
+        const T *const q0 = (const T *)q + b * sq[0] + l * sq[1], *const k0 = (const T *)k + b * sk[0] + l * sk[1];
+        const bool key = hh >= a.heads[0];
+        return (key ? k0 : q0) + (key ? hh - a.heads[0] : hh) * (key ? sk[2] : sq[2]);
+    };
+    // What is read of a token's heads h0 .. h0 + slots: on its way while the angles, or the heads before, are worked on
+    struct Item {
+        int b, l, pos;
+        Pairs<T, W, PAIRS> x, y;
+    };
+    const int step = gridDim.x * 4;
+    const auto load = [&](Item &m, int token, int h0) {
+        token = token < a.tokens ? token : a.tokens - 1;
+        m.b = token / a.L, m.l = token - m.b * a.L;
+        m.pos = a.positions[a.given ? token : 0];
+        const int hh = h0 + slot < all ? h0 + slot : all - 1;
+        m.x.load(place(a.Q, a.K, a.in[0], a.in[1], m.b, m.l, hh), o1, o2);
+        if constexpr (BWD) m.y.load(place(a.dQo, a.dKo, a.out[0], a.out[1], m.b, m.l, hh), o1, o2);
+    };
+    const double turns[2] = {lane < half ? a.turns[lane] : 0.0, lane + 64 < half ? a.turns[lane + 64] : 0.0};
+    int token = blockIdx.x * 4 + wave;
+    Item first, second;
+    load(first, token, 0);
+    for (int i = threadIdx.x; i < 2 * D; i += 256) {
+        const int k = i >= D, j = k ? i - D : i;
+        gam[k][j] = a.norm && a.gamma[k] ? a.gamma[k][j] : 1.f;
+    }
+    for (int i = half + lane; i < D / 2; i += 64) cs[i] = make_float2(1.f, 0.f);
     __syncthreads();
     float ga[2][W], gb[2][W]; // gradients of gamma: this lane's values of all heads that it sees, queries and keys
     if constexpr (BWD) {
 #pragma unroll
         for (int i = 0; i < W; ++i) ga[0][i] = ga[1][i] = gb[0][i] = gb[1][i] = 0.f;
     }
-    for (int token = blockIdx.x * 4 + wave; token < a.tokens; token += gridDim.x * 4) {
-        const int b = token / a.L, l = token - b * a.L;
-        __builtin_amdgcn_wave_barrier();
-        token_angles(a, a.positions ? a.positions[token] : l, cs, lane);
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-        for (int h0 = 0; h0 < all; h0 += slots) {
-            const int hh = h0 + slot;
-            const bool on = in_head && hh < all;
-            const int k = hh >= a.heads[0], h = k ? hh - a.heads[0] : hh;
-            float xa[W], xb[W], ya[W], yb[W];
-            const T *x = (const T *)(k ? a.K : a.Q) + b * a.in[k][0] + l * a.in[k][1] + h * a.in[k][2];
-            const i64 at_out = b * a.out[k][0] + l * a.out[k][1] + h * a.out[k][2];
+    int h0 = 0;
+    // works on m, on whose way the next item is
+    const auto turn = [&](const Item &m, Item &next) {
+        int token1 = token, h1 = h0 + slots;
+        if (h1 >= all) h1 = 0, token1 += step;
+        load(next, token1, h1);
+        if (h0 == 0) {
+            __builtin_amdgcn_wave_barrier();
+            token_angles(half, a.given ? m.pos : m.l, turns, cs, lane);
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        }
+        const int hh = h0 + slot < all ? h0 + slot : all - 1, k = hh >= a.heads[0];
+        const bool on = in_head && h0 + slot < all;
+        float rstd = 1.f;
+        if (a.norm) {
+            float q = 0.f;
 #pragma unroll
-            for (int i = 0; i < W; ++i) xa[i] = xb[i] = ya[i] = yb[i] = 0.f;
-            if (on && (!BWD || a.norm)) get_pairs<T, W, PAIRS>(x, o1, o2, xa, xb);
-            if constexpr (BWD) {
-                if (on) get_pairs<T, W, PAIRS>((const T *)(k ? a.dKo : a.dQo) + at_out, o1, o2, ya, yb);
-            }
-            float rstd = 1.f;
-            if (a.norm) {
-                float q = 0.f;
+            for (int i = 0; i < W; ++i) q += m.x.a(i) * m.x.a(i) + m.x.b(i) * m.x.b(i);
+            rstd = 1.f / sqrtf(head_sum(in_head ? q : 0.f, log) * inv_d + a.eps);
+        }
+        const float *const g1 = gam[k] + o1, *const g2 = gam[k] + o2;
+        const float2 *const angle = cs + part;
+        float ya[W], yb[W], dot = 0.f;
+        float p[W], r[W]; // backward: terms of gamma's gradients
 #pragma unroll
-                for (int i = 0; i < W; ++i) q += xa[i] * xa[i] + xb[i] * xb[i];
-                rstd = 1.f / sqrtf(head_sum(q, log) / (float)D + a.eps);
-            }
-            float c[W], s[W], gma[W], gmb[W];
-#pragma unroll
-            for (int i = 0; i < W; ++i) c[i] = 1.f, s[i] = 0.f, gma[i] = gmb[i] = 1.f;
-            if (on && turned) {
-#pragma unroll
-                for (int i = 0; i < W; ++i) c[i] = cs[part + i].x, s[i] = cs[part + i].y;
-            }
-            if (on && a.norm) {
-#pragma unroll
-                for (int i = 0; i < W; ++i) {
-                    gma[i] = gam[k][PAIRS ? o1 + 2 * i : o1 + i];
-                    gmb[i] = gam[k][PAIRS ? o1 + 2 * i + 1 : o2 + i];
-                }
-            }
+        for (int i = 0; i < W; ++i) {
+            const float c = angle[i].x, s = angle[i].y, gma = PAIRS ? g1[2 * i] : g1[i], gmb = PAIRS ? g1[2 * i + 1] : g2[i];
+            const float xa = m.x.a(i) * rstd, xb = m.x.b(i) * rstd;
             if constexpr (!BWD) {
-#pragma unroll
-                for (int i = 0; i < W; ++i) {
-                    const float u = xa[i] * rstd * gma[i], v = xb[i] * rstd * gmb[i];
-                    ya[i] = u * c[i] - v * s[i];
-                    yb[i] = u * s[i] + v * c[i];
-                }
-                if (on) put_pairs<T, W, PAIRS>((T *)(k ? a.Ko : a.Qo) + at_out, o1, o2, ya, yb);
-            } else {
-                float dot = 0.f;
-#pragma unroll
-                for (int i = 0; i < W; ++i) { // the turn taken back, then dx = rstd (w - xh mean(w xh)), w = gamma du
-                    const float u = ya[i] * c[i] + yb[i] * s[i], v = yb[i] * c[i] - ya[i] * s[i];
-                    if (a.norm) {
-                        xa[i] *= rstd;
-                        xb[i] *= rstd;
-                        ga[0][i] += k ? 0.f : u * xa[i];
-                        gb[0][i] += k ? 0.f : v * xb[i];
-                        ga[1][i] += k ? u * xa[i] : 0.f;
-                        gb[1][i] += k ? v * xb[i] : 0.f;
-                    }
-                    ya[i] = u * gma[i];
-                    yb[i] = v * gmb[i];
-                    dot += ya[i] * xa[i] + yb[i] * xb[i];
-                }
-                if (a.norm) {
-                    const float mean = head_sum(dot, log) / (float)D;
-#pragma unroll
-                    for (int i = 0; i < W; ++i) {
-                        ya[i] = rstd * (ya[i] - xa[i] * mean);
-                        yb[i] = rstd * (yb[i] - xb[i] * mean);
-                    }
-                }
-                T *dx = (T *)(k ? a.dK : a.dQ) + b * a.din[k][0] + l * a.din[k][1] + h * a.din[k][2];
-                if (on) put_pairs<T, W, PAIRS>(dx, o1, o2, ya, yb);
+                const float u = xa * gma, v = xb * gmb;
+                ya[i] = u * c - v * s;
+                yb[i] = u * s + v * c;
+            } else { // the turn taken back, then dx = rstd (w - xh mean(w xh)), w = gamma du
+                const float u = m.y.a(i) * c + m.y.b(i) * s, v = m.y.b(i) * c - m.y.a(i) * s;
+                p[i] = u * xa, r[i] = v * xb;
+                ya[i] = u * gma;
+                yb[i] = v * gmb;
+                dot += ya[i] * xa + yb[i] * xb;
             }
         }
+        if constexpr (BWD) {
+            if (h0 < a.heads[0]) {
+#pragma unroll
+                for (int i = 0; i < W; ++i) ga[0][i] += on && !k ? p[i] : 0.f, gb[0][i] += on && !k ? r[i] : 0.f;
+            }
+            if (h0 + slots > a.heads[0]) {
+#pragma unroll
+                for (int i = 0; i < W; ++i) ga[1][i] += on && k ? p[i] : 0.f, gb[1][i] += on && k ? r[i] : 0.f;
+            }
+        }
+        if (BWD && a.norm) {
+            const float mean = head_sum(in_head ? dot : 0.f, log) * inv_d;
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                ya[i] = rstd * (ya[i] - m.x.a(i) * rstd * mean);
+                yb[i] = rstd * (yb[i] - m.x.b(i) * rstd * mean);
+            }
+        }
+        T *const out = BWD ? (T *)place(a.dQ, a.dK, a.din[0], a.din[1], m.b, m.l, hh) : (T *)place(a.Qo, a.Ko, a.out[0], a.out[1], m.b, m.l, hh);
+        put_pairs<T, W, PAIRS>(out, o1, o2, ya, yb);
+        token = token1, h0 = h1;
+    };
+    while (token < a.tokens) {
+        turn(first, second);
+        if (token < a.tokens) turn(second, first);
     }
     if constexpr (BWD) {
         if (!a.partial) return;
@@ -228,16 +263,23 @@ __global__ __launch_bounds__(256) void qk_norm_kernel(QkArgs a, int log)
     }
 }
 
-// The workgroups' sums to dgamma: one workgroup of 64 lanes per value, in double and always in one order
-__global__ __launch_bounds__(64) void qk_gamma_kernel(const float *partial, int blocks, int D, float *dq, float *dk, int accumulate)
+// The workgroups' sums to dgamma: one workgroup per value, in double and always in one order.  Bound by latency: a lane's loads
+// are on their way together (one wave that loaded one by one took 6.7 us for 1024 workgroups, this 3.9)
+__global__ __launch_bounds__(256) void qk_gamma_kernel(const float *partial, int blocks, int D, float *dq, float *dk, int accumulate)
 {
-    const int i = blockIdx.x, lane = threadIdx.x;
-    double s = 0.0;
-    for (int b = lane; b < blocks; b += 64) s += (double)partial[(i64)b * 2 * D + i];
+    __shared__ double part[4];
+    const int i = blockIdx.x, t = threadIdx.x;
+    float x[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x[k] = t + 256 * k < blocks ? partial[(i64)(t + 256 * k) * 2 * D + i] : 0.f;
+    double s = ((double)x[0] + (double)x[1]) + ((double)x[2] + (double)x[3]);
     for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o);
+    if ((t & 63) == 0) part[t >> 6] = s;
+    __syncthreads();
+    s = (part[0] + part[1]) + (part[2] + part[3]);
     float *out = i < D ? dq : dk;
     const int j = i < D ? i : i - D;
-    if (lane == 0 && out) out[j] = accumulate ? out[j] + (float)s : (float)s;
+    if (t == 0 && out) out[j] = accumulate ? out[j] + (float)s : (float)s;
 }
 
 // ------------------------------------------------------------------ host
@@ -252,7 +294,7 @@ static int qk_check(const pf_qk_norm_desc *d)
     if (d->rot_dim && !(d->theta > 0 && isfinite(d->theta))) return PF_ERR_UNSUPPORTED;
     if (d->norm && !(d->eps >= 0 && isfinite(d->eps))) return PF_ERR_UNSUPPORTED;
     const i64 heads = (i64)d->heads_q + d->heads_k;
-    if (d->B && d->L && (d->L > INT32_MAX / d->B || d->B * d->L > INT32_MAX / heads)) return PF_ERR_UNSUPPORTED;
+    if (d->B && d->L && (d->L > INT32_MAX / 2 / d->B || d->B * d->L > INT32_MAX / 2 / heads)) return PF_ERR_UNSUPPORTED;
     const int unit = 16 / (d->dtype == PF_BF16 ? 2 : 4);
     for (const int64_t *s : {d->q_stride, d->k_stride, d->qo_stride, d->ko_stride, d->dq_stride, d->dk_stride})
         for (int i = 0; i < 3; ++i)
@@ -266,11 +308,12 @@ static void strides_of(const int64_t *s, i64 L, int heads, int D, i64 (&out)[3])
     out[1] = dense ? (i64)heads * D : s[1];
     out[0] = dense ? L * heads * D : s[0];
 }
+constexpr int QK_SUMS = 1024; // (qk_gamma_kernel's lanes hold as many)
 static int qk_blocks(const pf_qk_norm_desc *d, bool bwd)
 {
     // Four tokens (one per wave) to a workgroup.  Backward, a workgroup leaves 2 D sums behind, so that there are at most
     // four to a compute unit, each going through many tokens.
-    const i64 blocks = (d->B * d->L + 3) / 4, most = bwd ? 1024 : 1 << 20;
+    const i64 blocks = (d->B * d->L + 3) / 4, most = bwd ? QK_SUMS : 1 << 20;
     return (int)(blocks < most ? blocks : most);
 }
 static void qk_fill(const pf_qk_norm_desc *d, QkArgs &a)
@@ -313,14 +356,14 @@ static int qk_launch_w(const QkArgs &a, bool pairs, int blocks, hipStream_t s)
         PF_LAUNCH(st, BWD ? "qk_norm_bwd" : "qk_norm_fwd", (qk_norm_kernel<T, W, false, BWD>), dim3(blocks), dim3(256), s, a, log);
     return st;
 }
-// As many pairs to a lane as make 16-byte accesses (halves: W values from each half), if they divide the turned part and
-// the rest; two otherwise
+// Four pairs to a lane if they divide the turned part and the rest, two otherwise.  (Eight bf16 pairs make 16-byte accesses, but
+// backward then holds 165 registers, not 110: 64 x 128 tokens of 16 heads of 64 took 31.1 us, not 30.4, and 2 x 8191 tokens of 40
+// heads of 128 177 us, not 173.)
 template <bool BWD>
 static int qk_launch(const QkArgs &a, int dtype, bool pairs, int blocks, hipStream_t s)
 {
     const auto whole = [&](int w) { return a.R / 2 % w == 0 && a.D / 2 % w == 0; };
     if (dtype == PF_BF16) {
-        if (whole(8)) return qk_launch_w<bf16_t, 8, BWD>(a, pairs, blocks, s);
         if (whole(4)) return qk_launch_w<bf16_t, 4, BWD>(a, pairs, blocks, s);
         return qk_launch_w<bf16_t, 2, BWD>(a, pairs, blocks, s);
     }
@@ -348,7 +391,8 @@ int pf_qk_norm_rotate_fwd(const pf_qk_norm_desc *d, const void *Q, const void *K
     a.Q = Q, a.K = K, a.Qo = Qo, a.Ko = Ko;
     a.gamma[0] = (const float *)gamma_q;
     a.gamma[1] = (const float *)gamma_k;
-    a.positions = (const int *)positions;
+    a.positions = (const int *)(positions ? positions : Qo);
+    a.given = positions != nullptr;
     return qk_launch<false>(a, d->dtype, d->rotation == PF_ROT_PAIRS, qk_blocks(d, false), (hipStream_t)stream);
 }
 
@@ -382,12 +426,17 @@ int pf_qk_norm_rotate_bwd(const pf_qk_norm_desc *d, const void *Q, const void *K
     a.Q = Q, a.K = K, a.dQo = dQo, a.dKo = dKo, a.dQ = dQ, a.dK = dK;
     a.gamma[0] = (const float *)gamma_q;
     a.gamma[1] = (const float *)gamma_k;
-    a.positions = (const int *)positions;
+    a.positions = (const int *)(positions ? positions : dQo);
+    a.given = positions != nullptr;
+    if (!norm) { // (the values are not needed: what is read once may be read twice)
+        a.Q = dQo, a.K = dKo;
+        memcpy(a.in, a.out, sizeof a.in);
+    }
     a.partial = sums ? (float *)workspace : nullptr;
     const int blocks = qk_blocks(d, true);
     st = qk_launch<true>(a, d->dtype, d->rotation == PF_ROT_PAIRS, blocks, (hipStream_t)stream);
     if (sums)
-        PF_LAUNCH(st, "qk_gamma", qk_gamma_kernel, dim3(2 * d->head_dim), dim3(64), (hipStream_t)stream, a.partial, blocks, d->head_dim,
+        PF_LAUNCH(st, "qk_gamma", qk_gamma_kernel, dim3(2 * d->head_dim), dim3(256), (hipStream_t)stream, a.partial, blocks, d->head_dim,
                   (float *)dgamma_q, d->heads_k ? (float *)dgamma_k : nullptr, accumulate);
     return st;
 }
