@@ -475,7 +475,7 @@ int pf_lowrank_lstm_stack_bwd(const pf_lstm_stack_desc *d, const void *x,
 /*   positions: int32[B, L], nullable (token l of a sequence stands at l)*/
 /* heads_k == 0: no keys, K and all that belongs to it are not touched.  */
 /* head_dim: a multiple of 8, 8 .. 256; rot_dim: a multiple of 4,        */
-/* 0 .. head_dim; B L heads < 2^31 (PF_ERR_UNSUPPORTED otherwise).       */
+/* 0 .. head_dim; B L heads < 2^30 (PF_ERR_UNSUPPORTED otherwise).       */
 /* Outputs may be the inputs themselves (same strides).                  */
 /* ------------------------------------------------------------------ */
 typedef enum { PF_NORM_NONE = 0, PF_NORM_RMS = 1 } pf_norm;

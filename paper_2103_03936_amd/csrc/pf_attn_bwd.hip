@@ -28,12 +28,11 @@ struct DqLds {
         return (tab ? TILES + 4 * (2 * far + 1) * 4 : 5 * Tl::BYTES) + (bias ? (2 * far + 1) * 4 : 0);
     }
 };
-template <typename T, int DP>
+// dK and dV: KW waves have keys of their own, QW share the queries
+template <typename T, int DP, int KW, int QW>
 struct DkvLds {
-    using Tq = Tile<T, DP, 32, 256>;
-    // dK and dV: how many waves share the queries (what six tiles of float rows take leaves room for one)
-    static constexpr int QW = sizeof(T) == 4 && DP > 64 ? 1 : 2;
-    static size_t bytes(int far, bool bias) { return 6 * QW * Tq::BYTES + 3 * 2 * 32 * QW * 4 + (bias ? (2 * far + 1) * 4 : 0); }
+    using Tl = Tile<T, DP, 32 * QW, 64 * KW * QW>;
+    static size_t bytes(int far, bool bias) { return 6 * Tl::BYTES + 3 * 2 * 32 * QW * 4 + (bias ? (2 * far + 1) * 4 : 0); }
 };
 
 // dQ, delta and the sums of dS by distance, for one tile of 128 queries of one head.  TAB: with the gradient of the table.
@@ -75,9 +74,14 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b
 
     const int most = a.causal && n.nk > pos ? 0 : n.nk - 1 - pos; // the furthest distance seen
 
-    if (BIAS && keys > 0) fill_bias(a, bias, head, t, 256);
-    if constexpr (TAB)
-        for (int x = t; x < 4 * span; x += 256) sums_all[x] = 0.f;
+    const Tl kl(a.ks[1], a.D, t), vl(a.vs[1], a.D, t);
+    const int rows = Tl::row_place(lane) + own * Tl::RB, cols = Tl::col_place(lane) + own * Tl::RB; // (turn() repeats after 16 rows)
+    const auto fetch = [&](int j, int kslot, int vslot) {
+        kl.fetch(kb + kslot * Tl::SIZE, Kp + (i64)(STEP * j) * a.ks[1], a.ks[1], keys - STEP * j, a.D, wave);
+        vl.fetch(vb + vslot * Tl::SIZE, Vp + (i64)(STEP * j) * a.vs[1], a.vs[1], keys - STEP * j, a.D, wave);
+    };
+    const int groups = (keys + STEP - 1) / STEP; // of STEP keys
+    if (groups > 0) fetch(0, 0, 0);
     const i64 at = (((i64)b * a.Lq + i) * a.Hq + head) * a.D, stat = ((i64)b * a.Hq + head) * a.Lq + i;
     Frag<T> q[CH], g[CH];
     float delta = 0.f;
@@ -105,17 +109,12 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b
     for (int d = 0; d < DB; ++d) dq[d] = f32x16_t{};
     float before = 0.f, after = 0.f, before_p = 0.f, after_p = 0.f, off = 0.f; // far sums of dS and P; the sum of all dS
 
-    const Tl kl(a.ks[1], a.D, t), vl(a.vs[1], a.D, t);
-    const int rows = Tl::row_place(lane) + own * Tl::RB, cols = Tl::col_place(lane) + own * Tl::RB; // (turn() repeats after 16 rows)
     const auto near_at = [&](int k0) { return BIAS && k0 + 31 - pmin > -far && k0 - pmax < far; };
-    const auto fetch = [&](int j, int kslot, int vslot) {
-        kl.fetch(kb + kslot * Tl::SIZE, Kp + (i64)(STEP * j) * a.ks[1], a.ks[1], keys - STEP * j, a.D, wave);
-        vl.fetch(vb + vslot * Tl::SIZE, Vp + (i64)(STEP * j) * a.vs[1], a.vs[1], keys - STEP * j, a.D, wave);
-    };
     const auto finish = [&](f32x16_t &s, int k0) { finish_scores<BIAS>(s, sl2, lse2, bias, far, anew(k0 + 4 * h - pos), 1, most); };
-    const int groups = (keys + STEP - 1) / STEP; // of STEP keys
+    if (BIAS && keys > 0) fill_bias(a, bias, head, t, 256); // (behind the loads that it need not wait for)
+    if constexpr (TAB)
+        for (int x = t; x < 4 * span; x += 256) sums_all[x] = 0.f;
     if (groups > 0) {
-        fetch(0, 0, 0);
         fetched();
         __syncthreads();
     }
@@ -250,7 +249,7 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b
         else if ((hi + STEP - 1) / STEP < end)
             end = (hi + STEP - 1) / STEP;
         if (begin < end) {
-            for (int x = t; x < 4 * DIAG; x += 256) diag_all[x] = 0.f;
+            for (int x = t; x < DIAG; x += 256) ((f32x4_t *)diag_all)[x] = f32x4_t{};
             fetch2(begin);
             fetched();
             __syncthreads();
@@ -366,15 +365,13 @@ __device__ __forceinline__ void attn_table(const AttnArgs &a, const TableSum &z,
     if (lane == 0) *out = z.accumulate ? *out + (float)y : (float)y;
 }
 
-// dK and dV: a workgroup has 64 keys of one key head, a wave 32 of them in its columns; the query heads of the key head one
+// dK and dV: a workgroup has 32 KW keys of one key head, a wave 32 of them in its columns; the query heads of the key head one
 // after the other, each in groups of 32 QW queries, of which a wave has 32.  As above, dS and P of 32 queries are worked out
-// while S and dP of the next are made.  The waves that share keys add up what they have at the end.  (With all queries in
-// one wave, a causal mask's longest column alone, 512 blocks of 2 x 4096 tokens with four query heads to a key head, took 765 us:
-// the time of the whole kernel.)
-template <typename T, int DP, bool BIAS>
-__global__ __launch_bounds__((128 * DkvLds<T, DP>::QW), (DP * sizeof(T) <= 128 ? 2 : 1)) void attn_dkv_kernel(AttnArgs a, TableSum z)
+// while S and dP of the next are made.  The waves that share keys add up what they have at the end.
+template <typename T, int DP, bool BIAS, int KW, int QW>
+__global__ __launch_bounds__((64 * KW * QW), (DP * sizeof(T) <= 128 ? 2 : 1)) void attn_dkv_kernel(AttnArgs a, TableSum z)
 {
-    constexpr int QW = DkvLds<T, DP>::QW, ROWS = 32 * QW, THREADS = 128 * QW;
+    constexpr int ROWS = 32 * QW, THREADS = 64 * KW * QW, KEYS = 32 * KW;
     using Tl = Tile<T, DP, ROWS, THREADS>;
     constexpr int CH = DP / 16, DB = DP / 32, AHEAD = DP * sizeof(T) <= 128 ? 3 : sizeof(T) == 2 ? 6 : 3; // (one wave to a unit needs more on the way)
     extern __shared__ __attribute__((aligned(16))) char lds[];
@@ -382,13 +379,13 @@ __global__ __launch_bounds__((128 * DkvLds<T, DP>::QW), (DP * sizeof(T) <= 128 ?
     float *const stats = (float *)(lds + 6 * Tl::BYTES); // [3][2][ROWS]: lse (base 2) and -delta of each query
     float *const bias = stats + 3 * 2 * ROWS;
 
-    if (blockIdx.x >= z.after) return attn_table(a, z, (int)(blockIdx.x - z.after) * 2 * QW + (threadIdx.x >> 6), threadIdx.x & 63);
+    if (blockIdx.x >= z.after) return attn_table(a, z, (int)(blockIdx.x - z.after) * KW * QW + (threadIdx.x >> 6), threadIdx.x & 63);
     const unsigned w = xcd_order(blockIdx.x, z.after);
     const int tile = (int)(w % a.tiles), bk = w / a.tiles, b = bk / a.Hkv, kv = bk - b * a.Hkv;
     const int t = threadIdx.x, wave = wave_of(t), lane = t & 63, col = lane & 31, h = lane >> 5;
     const AttnLens n(a, b);
-    const int kw = wave & 1, r0 = 32 * (wave >> 1); // the wave's keys; its rows of a group
-    const int far = a.bk.far, j0 = tile * 64 + kw * 32, j = j0 + col;
+    const int kw = wave % KW, r0 = 32 * (wave / KW); // the wave's keys; its rows of a group
+    const int far = a.bk.far, j0 = tile * KEYS + kw * 32, j = j0 + col;
     const bool ok = j < n.nk;
     const int most = !ok ? INT32_MIN : a.causal ? 0 : INT32_MAX; // the furthest distance from which the key is seen
     Frag<T> k[CH], v[CH];
@@ -412,10 +409,10 @@ __global__ __launch_bounds__((128 * DkvLds<T, DP>::QW), (DP * sizeof(T) <= 128 ?
     int begin = 0, mine = 0;
     const int end = (n.nq + ROWS - 1) / ROWS;
     if (a.causal) {
-        begin = clamped(tile * 64 - n.start, 0, a.Lq) / ROWS;
+        begin = clamped(tile * KEYS - n.start, 0, a.Lq) / ROWS;
         mine = clamped(j0 - n.start, 0, a.Lq);
     }
-    if (tile * 64 >= n.nk) begin = end;
+    if (tile * KEYS >= n.nk) begin = end;
     if (j0 >= n.nk) mine = a.Lq;
     for (int g0 = 0; g0 < a.G && begin < end; ++g0) {
         const int head = kv * a.G + g0;
@@ -434,10 +431,11 @@ __global__ __launch_bounds__((128 * DkvLds<T, DP>::QW), (DP * sizeof(T) <= 128 ?
         const auto put_stat = [&](int x, int slot, float y) { // (behind the last query: lse = infinity, P = 0)
             if (t < 2 * ROWS) stats[(2 * slot + (t & 1)) * ROWS + t / 2] = !(t & 1) && ROWS * x + t / 2 >= a.Lq ? INFINITY : y;
         };
-        if constexpr (BIAS) fill_bias(a, bias, head, t, THREADS);
         int slot = (begin + 2) % 3;
         fetch(begin, begin % 3);
-        put_stat(begin, begin % 3, stat_of(begin));
+        const float early = stat_of(begin);
+        if constexpr (BIAS) fill_bias(a, bias, head, t, THREADS);
+        put_stat(begin, begin % 3, early);
         fetched();
         __syncthreads();
         f32x16_t sA = {}, sB = {}, dpA = {}, dpB = {};
@@ -522,7 +520,7 @@ __global__ __launch_bounds__((128 * DkvLds<T, DP>::QW), (DP * sizeof(T) <= 128 ?
     }
     if constexpr (QW == 2) { // (the loop ended with a barrier: the tiles' room is free)
         float *const sum = (float *)lds + kw * DB * 2048 + lane;
-        if (wave >= 2) {
+        if (wave >= KW) {
 #pragma unroll
             for (int d = 0; d < DB; ++d)
 #pragma unroll
@@ -532,7 +530,7 @@ __global__ __launch_bounds__((128 * DkvLds<T, DP>::QW), (DP * sizeof(T) <= 128 ?
                 }
         }
         __syncthreads();
-        if (wave >= 2) return;
+        if (wave >= KW) return;
 #pragma unroll
         for (int d = 0; d < DB; ++d)
 #pragma unroll
@@ -587,6 +585,32 @@ static i64 dq_tiles(i64 B, i64 Hq, i64 Lq, size_t row)
     return (Lq + queries - 1) / queries;
 }
 
+template <typename T, int DP, int KW, int QW>
+static int attn_dkv_launch(AttnArgs &a, TableSum z, hipStream_t s)
+{
+    int st = PF_OK;
+    a.tiles = (a.Lk + 32 * KW - 1) / (32 * KW);
+    z.after = (unsigned)a.B * a.Hkv * a.tiles;
+    // behind the workgroups for the keys, those that sum up the table's gradient (a launch of their own took 5 us)
+    const dim3 grid(z.after + (z.dtable ? (a.buckets * a.Hq + KW * QW - 1) / (KW * QW) : 0));
+    const size_t lds = DkvLds<T, DP, KW, QW>::bytes(a.bk.far, a.buckets);
+    if (grid.x == 0) return st;
+    if (a.buckets)
+        PF_LAUNCH_LDS(st, "attn_dkv", (attn_dkv_kernel<T, DP, true, KW, QW>), grid, dim3(64 * KW * QW), lds, s, a, z);
+    else
+        PF_LAUNCH_LDS(st, "attn_dkv", (attn_dkv_kernel<T, DP, false, KW, QW>), grid, dim3(64 * KW * QW), lds, s, a, z);
+    return st;
+}
+
+// Keys of a workgroup: 128, a wave's own 32 queries at a time, where that makes as many workgroups as fit the card at once (queries and
+// dO are read half as often); 64 shared by two waves each where it does not, and with a causal mask, whose first keys have
+// the most queries.  us, bf16: 64 x 128 tokens of 8 heads of 64, 512 tiles of 128, 19 and 24 with tiles of 64; 6 x 1024, 384 tiles,
+// 54 and 51; 4 x 1024 with heads of 128, 256 tiles (one to a compute unit), 61 and 68; 2 x 4096 causal, 512 tiles, 675 and 408.
+static bool dkv_wide(const AttnArgs &a, size_t row)
+{
+    return (!a.causal || a.Lk <= 128) && (i64)a.B * a.Hkv * ((a.Lk + 127) / 128) >= (row <= 128 ? 512 : 256);
+}
+
 template <typename T, int DP>
 static int attn_bwd_launch(AttnArgs &a, float *dtable, int accumulate, hipStream_t s)
 {
@@ -597,18 +621,11 @@ static int attn_bwd_launch(AttnArgs &a, float *dtable, int accumulate, hipStream
     else
         st = attn_dq_launch<T, DP, 1>(a, tab, s);
     const int parts = a.B * a.tiles;
-    // behind the workgroups for the keys, those that sum up the table's gradient (a launch of their own took 5 us)
-    constexpr int WAVES = 2 * DkvLds<T, DP>::QW;
-    a.tiles = (a.Lk + 63) / 64;
-    const TableSum z = {dtable, parts, accumulate, (unsigned)a.B * a.Hkv * a.tiles};
-    const dim3 kgrid(z.after + (tab ? (a.buckets * a.Hq + WAVES - 1) / WAVES : 0));
-    const size_t klds = DkvLds<T, DP>::bytes(a.bk.far, bias);
-    if (kgrid.x == 0) return st;
-    if (bias)
-        PF_LAUNCH_LDS(st, "attn_dkv", (attn_dkv_kernel<T, DP, true>), kgrid, dim3(64 * WAVES), klds, s, a, z);
-    else
-        PF_LAUNCH_LDS(st, "attn_dkv", (attn_dkv_kernel<T, DP, false>), kgrid, dim3(64 * WAVES), klds, s, a, z);
-    return st;
+    if (st != PF_OK) return st;
+    const TableSum z = {tab ? dtable : nullptr, parts, accumulate, 0};
+    // (what six tiles of more than 256 bytes a row take leaves no room for two waves' queries)
+    if constexpr (DP * sizeof(T) > 256) return attn_dkv_launch<T, DP, 2, 1>(a, z, s);
+    return dkv_wide(a, DP * sizeof(T)) ? attn_dkv_launch<T, DP, 4, 1>(a, z, s) : attn_dkv_launch<T, DP, 2, 2>(a, z, s);
 }
 static size_t delta_bytes(const pf_attention_desc *d) { return align_up((size_t)d->B * d->heads_q * d->Lq * 2 * sizeof(float)); }
 

@@ -46,7 +46,6 @@ __device__ __forceinline__ void attn_fwd_tile(const AttnArgs &a, char *lds, int 
         fetch_keys(0, 0);
         fetch_values(0, 0);
         if (keys > STEP) fetch_keys(STEP, 1);
-        if constexpr (BIAS) fill_bias(a, bias, head, t, 256);
     }
     Frag<T> q[DP / 16];
     {
@@ -54,6 +53,7 @@ __device__ __forceinline__ void attn_fwd_tile(const AttnArgs &a, char *lds, int 
 #pragma unroll
         for (int c = 0; c < DP / 16; ++c) q[c] = row_frag_global(Qp, 16 * c, a.D, h, ok);
     }
+    if (BIAS && keys > 0) fill_bias(a, bias, head, t, 256); // (behind the loads that it need not wait for)
     const float sl2 = a.scale * LOG2E;
     const int far = a.bk.far;
     f32x16_t o[DP / 32];

@@ -262,9 +262,11 @@ def test_another_stream_and_graph_replay():
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("c", [(9, 300, 300, 32, 8, 64, False, 32, 128, "pad"), (11, 260, 260, 24, 8, 128, True, 32, 128, None)], ids=str)
+@pytest.mark.parametrize("c", [(9, 300, 300, 32, 8, 64, False, 32, 128, "pad"), (11, 260, 260, 24, 8, 128, True, 32, 128, None),
+                               (65, 140, 135, 8, 4, 40, False, 16, 64, "pad"), (130, 60, 90, 4, 4, 64, True, 32, 128, "append")], ids=str)
 def test_many_tiles(c, dtype):
-    """More tiles of queries than fit the card at once: no two waves share queries; causal tiles are taken in pairs."""
+    """More tiles of queries than fit the card at once: no two waves share queries; causal tiles are taken in pairs.  Then more
+    tiles of 128 keys than fit it: the waves of dK and dV have keys of their own."""
     test_against_definition(c, dtype)
 
 
