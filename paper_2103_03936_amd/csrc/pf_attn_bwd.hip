@@ -97,6 +97,13 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b
         }
         delta += __shfl_xor(delta, 32);
     }
+    // A query that sees one key has dS = 0: here by dO = 0, not by what rounding leaves of dP - delta
+    float kept = 0.f;
+    if (pos + most == 0) {
+        kept = delta, delta = 0.f;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) g[c] = {};
+    }
     // exp2(S - lse) is 0 for a query that takes no part
     float lse2 = INFINITY;
     if (ok) {
@@ -236,7 +243,7 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b
         before -= off * before_p;
         after -= off * after_p;
     }
-    if (i < a.Lq && h == 0 && kw == 0) *(float2 *)(a.delta + 2 * stat) = make_float2(lse2, ok ? -delta : 0.f);
+    if (i < a.Lq && h == 0 && kw == 0) *(float2 *)(a.delta + 2 * stat) = make_float2(lse2, ok ? -(delta + kept) : 0.f);
     if constexpr (TAB) {
         // (two groups of keys, two of values)
         const auto fetch2 = [&](int j) { fetch(j, j & 1, (j & 1) - 1); };
@@ -540,6 +547,7 @@ __global__ __launch_bounds__((64 * KW * QW), (DP * sizeof(T) <= 128 ? 2 : 1)) vo
             }
     }
     if (j >= a.Lk) return;
+    const float scale = n.nk == 1 ? 0.f : a.scale; // (one key: P = 1 and dS = 0, not what rounding leaves of dP - delta)
     const i64 at = (((i64)b * a.Lk + j) * a.Hkv + kv) * a.D;
     T *const ok_ = (T *)a.dK + at, *const ov = (T *)a.dV + at;
 #pragma unroll
@@ -548,7 +556,7 @@ __global__ __launch_bounds__((64 * KW * QW), (DP * sizeof(T) <= 128 ? 2 : 1)) vo
         for (int e = 0; e < 16; e += 4) {
             const int c = 32 * d + 8 * (e >> 2) + 4 * h;
             if (c >= a.D) continue;
-            put4(ok_ + c, dk[d][e] * a.scale, dk[d][e + 1] * a.scale, dk[d][e + 2] * a.scale, dk[d][e + 3] * a.scale);
+            put4(ok_ + c, dk[d][e] * scale, dk[d][e + 1] * scale, dk[d][e + 2] * scale, dk[d][e + 3] * scale);
             put4(ov + c, dv[d][e], dv[d][e + 1], dv[d][e + 2], dv[d][e + 3]);
         }
 }

@@ -295,3 +295,19 @@ def test_nan_stays_in_what_uses_it(Lq, dtype):
     assert dQ[last[0]].isnan().all()
     dQ[last[0]] = 0
     assert not dQ.isnan().any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("c", [(3, 70, 1, 4, 2, 64, False, 32, 128, None), (5, 1, 1, 2, 2, 32, True, 16, 64, None),
+                               (200, 70, 1, 8, 4, 64, False, 32, 128, None)], ids=str)
+def test_one_key(c, dtype):
+    """The softmax of one score is 1 whatever the score: no gradient, not even rounding's."""
+    import paper_2103_03936_amd as pf
+    d, g, o, kw = _case(c, dtype, 19)
+    got, lse = pf.pf_attention_fwd(g["Q"], g["K"], g["V"], g["table"], **kw)
+    assert torch.equal(got, g["V"].repeat_interleave(c[3] // c[4], 2).expand_as(got))
+    dQ, dK, dV, dtable = pf.pf_attention_bwd(g["Q"], g["K"], g["V"], got, lse, g["dO"], g["table"], **kw)
+    for x in (dQ, dK, dtable):
+        assert not x.any()
+    dO = d["dO"].astype(np.float64)
+    assert_within(dV, o.backward(dO)[2], attention_bounds(o, dO, dtype)[4], "dV")
