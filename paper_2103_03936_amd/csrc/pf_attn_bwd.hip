@@ -6,9 +6,9 @@
 // and dP each (seven products where one kernel with atomic sums of dQ would have five).
 //
 // delta = sum P dP of a row is sum O dO, too, but O is rounded to bf16 there and P was before O was formed: dS is off by about
-// 2^-9 of delta then, which is below what rounding dS itself costs dQ and dK, but not good enough for dtable, a float32 sum over
-// all pairs in which the rows' errors would stay.  What delta is off by is the sum of the row's dS, so that it is known once the
-// row is through.
+// 2^-9 of delta then.  For queries that see many keys that is below what rounding dS itself costs dQ and dK; where some see few,
+// delta is formed from P and dP first.  For dtable, a float32 sum over all pairs in which the rows' errors would stay, it is never
+// good enough.  What delta is off by is the sum of the row's dS, so that it is known once the row is through.
 #include "pf_attn.h"
 #include "pf_gemm.h"
 
@@ -81,7 +81,15 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b
         vl.fetch(vb + vslot * Tl::SIZE, Vp + (i64)(STEP * j) * a.vs[1], a.vs[1], keys - STEP * j, a.D, wave);
     };
     const int groups = (keys + STEP - 1) / STEP; // of STEP keys
-    if (groups > 0) fetch(0, 0, 0);
+    // A query that sees few keys: there delta is not small beside dP, nor is what it is off by beside dP - delta (2 x 3 causal
+    // tokens: dQ off by 6e-3, by 3e-3 with the exact one; the rounding of dS alone makes 2.4e-3 of any length)
+    const int position0 = tile * QUERIES + n.start, fewest = a.causal && position0 + 1 < keys ? position0 + 1 : keys;
+    const bool few = sizeof(T) == 2 && groups > 0 && fewest <= 128;
+    const auto fetch2 = [&](int j) { fetch(j, j & 1, (j & 1) - 1); }; // (two groups of keys, two of values)
+    if (few)
+        fetch2(0);
+    else if (groups > 0)
+        fetch(0, 0, 0);
     const i64 at = (((i64)b * a.Lq + i) * a.Hq + head) * a.D, stat = ((i64)b * a.Hq + head) * a.Lq + i;
     Frag<T> q[CH], g[CH];
     float delta = 0.f;
@@ -124,6 +132,108 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b
     if (groups > 0) {
         fetched();
         __syncthreads();
+    }
+    // S of group j, finished, and dP on `start`, from what fetch2 fetched
+    const auto form = [&](int j, float start, f32x16_t &s, f32x16_t &dp) {
+        const int at_j = (j & 1) * Tl::BYTES + rows;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[e] = 0.f, dp[e] = start;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            mma(s, Tl::by_rows(lds, at_j, 0, c), q[c]);
+            mma(dp, Tl::by_rows(lds, 2 * Tl::BYTES + at_j, 0, c), g[c]);
+        }
+        finish(s, STEP * j + own);
+    };
+    // The sum over the waves that share queries (between two barriers the tiles' room is free)
+    const auto over_waves = [&](float x) {
+        if constexpr (KW == 1) return x;
+        float *const y = (float *)lds + DP * 64 + lane;
+        y[wave * 64] = x;
+        __syncthreads();
+        x = y[(wave & ~1) * 64] + y[(wave | 1) * 64];
+        __syncthreads();
+        return x;
+    };
+    // The sums of a near block's dS along its diagonals
+    const auto diagonals = [&](int k0, const f32x16_t &ds) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) diag[(8 * (e >> 2) + 4 * h + (e & 3)) * 63 + col + 31] = ds[e];
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        float v[32], y = 0.f;
+#pragma unroll
+        for (int r = 0; r < 32; ++r) v[r] = diag[r * 64 + lane];
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int r = 0; r < 32; ++r) y += v[r];
+        // (distances from far on have one place, several lanes' sums go there: by way of the lanes' own)
+        const int dist = k0 - pmin + 31 - lane;
+        if (lane < 63) {
+            if (dist <= -far)
+                before += y;
+            else if (dist >= far)
+                after += y;
+            else
+                sums[dist + far] += y;
+        }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    };
+    const auto clear_blocks = [&] { // (what no value of a block is written to stays zero)
+        for (int x = t; x < DIAG; x += 256) ((f32x4_t *)diag_all)[x] = f32x4_t{};
+    };
+    if (few) { // twice over the keys: delta = sum P dP, then all that takes it
+        delta = 0.f;
+#pragma unroll 1
+        for (int j = 0; j < groups; ++j) {
+            if (j + 1 < groups) fetch2(j + 1);
+            if (STEP * j + own < mine) {
+                f32x16_t s, dp;
+                form(j, 0.f, s, dp);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) delta += exp2_fast(s[e]) * dp[e];
+            }
+            fetched();
+            __syncthreads();
+        }
+        delta = over_waves(delta + __shfl_xor(delta, 32));
+        if constexpr (TAB) clear_blocks();
+        fetch2(0);
+        fetched();
+        __syncthreads();
+#pragma unroll 1
+        for (int j = 0; j < groups; ++j) {
+            const int k0 = STEP * j + own;
+            if (j + 1 < groups) fetch2(j + 1);
+            if (k0 < mine) {
+                f32x16_t s, dp;
+                form(j, -delta, s, dp);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[e] = exp2_fast(s[e]) * dp[e];
+                if constexpr (TAB) {
+                    if (near_at(k0)) {
+                        diagonals(k0, s);
+                    } else {
+                        float y = 0.f;
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) y += s[e];
+                        (k0 >= pmin ? after : before) += y;
+                    }
+                }
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    Frag<T> f;
+                    pack(s, c, f);
+#pragma unroll
+                    for (int d = 0; d < DB; ++d) mma(dq[d], Tl::by_cols(lds, (j & 1) * Tl::BYTES + cols, 16 * c, d), f);
+                }
+            }
+            fetched();
+            __syncthreads();
+        }
     }
     f32x16_t sA = {}, sB = {}, dpA = {}, dpB = {};
     int slot = 2; // of group j
@@ -201,19 +311,18 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b
     };
     int start = -1; // (a number to the compiler: it would unroll the first turn for its own)
     asm volatile("" : "+s"(start));
-    for (int j = start; j < groups; j += 2) {
+    for (int j = few ? groups : start; j < groups; j += 2) {
         turn(j, sA, dpA, sB, dpB);
         if (j + 1 < groups) turn(j + 1, sB, dpB, sA, dpA);
     }
-    if constexpr (KW == 2) { // the second wave's dQ to the first, the sums of dS to both (the loop ended with a barrier)
-        float *const part = (float *)lds + wave / KW * (DP / 2) * 64 + lane, *const sum = (float *)lds + DP * 64 + lane;
+    if constexpr (KW == 2) { // the second wave's dQ to the first (the loop ended with a barrier)
+        float *const part = (float *)lds + wave / KW * (DP / 2) * 64 + lane;
         if (kw == 1) {
 #pragma unroll
             for (int d = 0; d < DB; ++d)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) part[(16 * d + e) * 64] = dq[d][e];
         }
-        sum[wave * 64] = off;
         __syncthreads();
         if (kw == 0) {
 #pragma unroll
@@ -221,8 +330,7 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b
 #pragma unroll
                 for (int e = 0; e < 16; ++e) dq[d][e] += part[(16 * d + e) * 64];
         }
-        off = sum[(wave & ~1) * 64] + sum[(wave | 1) * 64];
-        __syncthreads();
+        off = over_waves(off);
     }
     if (i < a.Lq && kw == 0) {
         T *const out = (T *)a.dQ + at;
@@ -245,18 +353,16 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b
     }
     if (i < a.Lq && h == 0 && kw == 0) *(float2 *)(a.delta + 2 * stat) = make_float2(lse2, ok ? -(delta + kept) : 0.f);
     if constexpr (TAB) {
-        // (two groups of keys, two of values)
-        const auto fetch2 = [&](int j) { fetch(j, j & 1, (j & 1) - 1); };
         // the near blocks once more: STEP begin + STEP - 1 > first position - far, STEP (end - 1) < last position + far
         int begin = 0, end = groups;
         const int lo = tile * QUERIES + n.start - far - (STEP - 1), hi = block_last + far;
         if (lo >= 0) begin = lo / STEP + 1;
-        if (hi <= 0)
+        if (few || hi <= 0)
             end = 0;
         else if ((hi + STEP - 1) / STEP < end)
             end = (hi + STEP - 1) / STEP;
         if (begin < end) {
-            for (int x = t; x < DIAG; x += 256) ((f32x4_t *)diag_all)[x] = f32x4_t{};
+            clear_blocks();
             fetch2(begin);
             fetched();
             __syncthreads();
@@ -265,41 +371,11 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b
             const int k0 = STEP * j + own;
             if (j + 1 < end) fetch2(j + 1);
             if (k0 < mine && near_at(k0)) {
-                const int at_j = (j & 1) * Tl::BYTES + rows;
-                f32x16_t s = {}, dp;
+                f32x16_t s, dp;
+                form(j, -delta, s, dp);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) dp[e] = -delta;
-#pragma unroll
-                for (int c = 0; c < CH; ++c) {
-                    mma(s, Tl::by_rows(lds, at_j, 0, c), q[c]);
-                    mma(dp, Tl::by_rows(lds, 2 * Tl::BYTES + at_j, 0, c), g[c]);
-                }
-                finish(s, k0);
-                // along the diagonals of the block
-#pragma unroll
-                for (int e = 0; e < 16; ++e) diag[(8 * (e >> 2) + 4 * h + (e & 3)) * 63 + col + 31] = exp2_fast(s[e]) * dp[e];
-                __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-                __builtin_amdgcn_wave_barrier();
-                __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-                float v[32], y = 0.f;
-#pragma unroll
-                for (int r = 0; r < 32; ++r) v[r] = diag[r * 64 + lane];
-                __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                for (int r = 0; r < 32; ++r) y += v[r];
-                // (distances from far on have one place, several lanes' sums go there: by way of the lanes' own)
-                const int dist = k0 - pmin + 31 - lane;
-                if (lane < 63) {
-                    if (dist <= -far)
-                        before += y;
-                    else if (dist >= far)
-                        after += y;
-                    else
-                        sums[dist + far] += y;
-                }
-                __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-                __builtin_amdgcn_wave_barrier();
-                __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+                for (int e = 0; e < 16; ++e) s[e] = exp2_fast(s[e]) * dp[e];
+                diagonals(k0, s);
             }
             fetched();
             __syncthreads();
