@@ -707,8 +707,9 @@ static int attn_bwd_launch(AttnArgs &a, float *dtable, int accumulate, hipStream
     const int parts = a.B * a.tiles;
     if (st != PF_OK) return st;
     const TableSum z = {tab ? dtable : nullptr, parts, accumulate, 0};
-    // (what six tiles of more than 256 bytes a row take leaves no room for two waves' queries)
-    if constexpr (DP * sizeof(T) > 256) return attn_dkv_launch<T, DP, 2, 1>(a, z, s);
+    // (Six tiles of more than 256 bytes a row leave no room for two waves' queries, nor for a second workgroup: four waves where
+    // there are more tiles of 64 keys than compute units.  16 x 512 tokens of 8 heads of 128: 320 us, with two waves 591)
+    if constexpr (DP * sizeof(T) > 256) return (i64)a.B * a.Hkv * ((a.Lk + 63) / 64) > 256 ? attn_dkv_launch<T, DP, 4, 1>(a, z, s) : attn_dkv_launch<T, DP, 2, 1>(a, z, s);
     return dkv_wide(a, DP * sizeof(T)) ? attn_dkv_launch<T, DP, 4, 1>(a, z, s) : attn_dkv_launch<T, DP, 2, 2>(a, z, s);
 }
 static size_t delta_bytes(const pf_attention_desc *d) { return align_up((size_t)d->B * d->heads_q * d->Lq * 2 * sizeof(float)); }
