@@ -689,7 +689,7 @@ static int attn_dkv_launch(AttnArgs &a, TableSum z, hipStream_t s)
 // Keys of a workgroup: 128, a wave's own 32 queries at a time, where that makes as many workgroups as fit the card at once (queries and
 // dO are read half as often); 64 shared by two waves each where it does not, and with a causal mask, whose first keys have
 // the most queries.  us, bf16: 64 x 128 tokens of 8 heads of 64, 512 tiles of 128, 19 and 24 with tiles of 64; 6 x 1024, 384 tiles,
-// 54 and 51; 4 x 1024 with heads of 128, 256 tiles (one to a compute unit), 61 and 68; 2 x 4096 causal, 512 tiles, 675 and 408.
+// 54 and 51; 4 x 1024 with heads of 128, 256 tiles (one to a compute unit), 61 and 68; 2 x 4096 causal, 256 tiles, 675 and 408.
 static bool dkv_wide(const AttnArgs &a, size_t row)
 {
     return (!a.causal || a.Lk <= 128) && (i64)a.B * a.Hkv * ((a.Lk + 127) / 128) >= (row <= 128 ? 512 : 256);
