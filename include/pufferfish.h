@@ -526,7 +526,8 @@ int pf_qk_norm_rotate_bwd(const pf_qk_norm_desc *d, const void *Q, const void *K
 /*   A query that sees nothing, and a query i >= q_len[b], has O = 0 and */
 /*   lse = -infinity and takes no part in any gradient; what K and V hold */
 /*   from kv_len[b] on, and Q and dO from q_len[b] on, does not matter   */
-/*   (not even NaN).                                                     */
+/*   (not even NaN).  A key that a causal mask hides from some queries   */
+/*   of a sequence and not from all has to be finite.                    */
 /*   q_start, q_len, kv_len: int32[B] on the device, each nullable       */
 /*   (0, Lq, Lk); lengths are taken as within 0 .. Lq and 0 .. Lk,       */
 /*   q_start as within -2^30 .. 2^30.                                    */
@@ -541,7 +542,8 @@ int pf_qk_norm_rotate_bwd(const pf_qk_norm_desc *d, const void *Q, const void *K
 /* buckets 0 or 2 .. 256, with bidirectional a multiple of 2 and >= 4;    */
 /* max_distance > e and <= 1024; Lq, Lk < 2^29; fewer than 2^31 blocks of  */
 /* 32 rows; less than 2^22 elements from one token to the next.           */
-/* Lq == 0 or Lk == 0 is legal.                                           */
+/* Lq == 0 or Lk == 0 is legal.  Outputs must not overlap inputs or each  */
+/* other (PF_ERR_UNSUPPORTED where they begin at one address).            */
 /* Sums are the same bits in every call of the same sizes.                */
 /* ------------------------------------------------------------------ */
 typedef struct {

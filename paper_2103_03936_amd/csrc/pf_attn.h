@@ -9,6 +9,8 @@
 // with the transposing reads).  For dK and dV the scores are formed with rows: queries, columns: keys, and the same holds.
 #pragma once
 
+#include <initializer_list>
+
 #include "pf_attn_bias.h"
 #include "pf_tile.h"
 
@@ -322,6 +324,18 @@ int attn_split_fwd(const pf_attention_desc *d, AttnArgs &a, void *workspace, hip
 int attn_split_count(const pf_attention_desc *d); // 0: the ordinary kernel
 size_t attn_split_bytes(const pf_attention_desc *d);
 int attn_check(const pf_attention_desc *d);
+// An output that begins where an input or another output does (partial overlaps are the caller's to avoid)
+inline bool attn_same(std::initializer_list<const void *> outputs, std::initializer_list<const void *> inputs)
+{
+    for (auto o = outputs.begin(); o != outputs.end(); ++o) {
+        if (!*o) continue;
+        for (auto x = outputs.begin(); x != o; ++x)
+            if (*x == *o) return true;
+        for (const void *x : inputs)
+            if (x == *o) return true;
+    }
+    return false;
+}
 void attn_fill(const pf_attention_desc *d, AttnArgs &a);
 
 } // namespace pf

@@ -747,6 +747,7 @@ int pf_attention_bwd(const pf_attention_desc *d, const void *Q, const void *K, c
     if (any_misaligned({workspace}, 256)) return PF_ERR_UNSUPPORTED;
     const size_t need = pf_attention_bwd_workspace_bytes(d);
     if (need && (!workspace || workspace_bytes < need)) return PF_ERR_WORKSPACE;
+    if (attn_same({dQ, dK, dV}, {Q, K, V, O, dO})) return PF_ERR_UNSUPPORTED;
     AttnArgs a = {};
     attn_fill(d, a);
     a.Q = Q, a.K = K, a.V = V, a.Oin = O, a.dO = dO, a.dQ = dQ, a.dK = dK, a.dV = dV;

@@ -325,6 +325,7 @@ int pf_attention_fwd(const pf_attention_desc *d, const void *Q, const void *K, c
         return PF_ERR_UNSUPPORTED;
     const size_t need = attn_split_bytes(d);
     if (need && (!workspace || workspace_bytes < need)) return PF_ERR_WORKSPACE;
+    if (attn_same({O}, {Q, K, V})) return PF_ERR_UNSUPPORTED;
     AttnArgs a = {};
     attn_fill(d, a);
     a.Q = Q, a.K = K, a.V = V, a.O = O;

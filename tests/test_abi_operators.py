@@ -80,6 +80,18 @@ def test_attention_refusals():
     assert b(_at(), dt=P(257)) == 3 and b(_at(), dO=P(264)) == 3 and b(_at(D=20)) == 3
 
 
+def test_attention_outputs_are_not_inputs():
+    q, k, v, o, lse, g, dq, dk, dv, ws = (P(256 * (i + 1)) for i in range(10))
+    d = _at()
+    for out in (q, k, v):
+        assert pf.lib.pf_attention_fwd(d, q, k, v, FAKE, None, None, None, out, None, None, Z(0), None) == 3
+    good = [dq, dk, dv]
+    for i in range(3):
+        for other in [q, k, v, o, g] + good[:i]:
+            outs = good[:i] + [other] + good[i + 1:]
+            assert pf.lib.pf_attention_bwd(d, q, k, v, FAKE, None, None, None, o, lse, g, *outs, None, 0, ws, BIG, None) == 3
+
+
 def _adamw(n=1, bits=32, b1=0.9, b2=0.99, eps=1e-8):
     return pf.pf_adamw_desc(n, bits, b1, b2, eps)
 
