@@ -85,11 +85,14 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b
     // tokens: dQ off by 6e-3, by 3e-3 with the exact one; the rounding of dS alone makes 2.4e-3 of any length)
     const int position0 = tile * QUERIES + n.start, fewest = a.causal && position0 + 1 < keys ? position0 + 1 : keys;
     const bool few = sizeof(T) == 2 && groups > 0 && fewest <= 128;
+    const bool plainly = few || (sizeof(T) == 4 && TAB);
     const auto fetch2 = [&](int j) { fetch(j, j & 1, (j & 1) - 1); }; // (two groups of keys, two of values)
-    if (few)
-        fetch2(0);
-    else if (groups > 0)
-        fetch(0, 0, 0);
+    if (groups > 0) {
+        if (plainly)
+            fetch2(0);
+        else
+            fetch(0, 0, 0);
+    }
     const i64 at = (((i64)b * a.Lq + i) * a.Hq + head) * a.D, stat = ((i64)b * a.Hq + head) * a.Lq + i;
     Frag<T> q[CH], g[CH];
     float delta = 0.f;
@@ -185,7 +188,7 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b
     const auto clear_blocks = [&] { // (what no value of a block is written to stays zero)
         for (int x = t; x < DIAG; x += 256) ((f32x4_t *)diag_all)[x] = f32x4_t{};
     };
-    if (few) { // twice over the keys: delta = sum P dP, then all that takes it
+    if (few) { // delta = sum P dP
         delta = 0.f;
 #pragma unroll 1
         for (int j = 0; j < groups; ++j) {
@@ -200,10 +203,17 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b
             __syncthreads();
         }
         delta = over_waves(delta + __shfl_xor(delta, 32));
-        if constexpr (TAB) clear_blocks();
         fetch2(0);
         fetched();
         __syncthreads();
+    }
+    // With the exact delta one pass makes dQ and the diagonals' sums.  (In float O is exact enough, and products of 64 cycles hide
+    // no vector work worth the order above: 4 x 333 tokens of 8 heads of 64 took 43 us in two passes, 28 so.)
+    if (plainly) {
+        if constexpr (TAB) {
+            clear_blocks();
+            __syncthreads();
+        }
 #pragma unroll 1
         for (int j = 0; j < groups; ++j) {
             const int k0 = STEP * j + own;
@@ -311,7 +321,7 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b
     };
     int start = -1; // (a number to the compiler: it would unroll the first turn for its own)
     asm volatile("" : "+s"(start));
-    for (int j = few ? groups : start; j < groups; j += 2) {
+    for (int j = plainly ? groups : start; j < groups; j += 2) {
         turn(j, sA, dpA, sB, dpB);
         if (j + 1 < groups) turn(j + 1, sB, dpB, sA, dpA);
     }
@@ -357,7 +367,7 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b
         int begin = 0, end = groups;
         const int lo = tile * QUERIES + n.start - far - (STEP - 1), hi = block_last + far;
         if (lo >= 0) begin = lo / STEP + 1;
-        if (few || hi <= 0)
+        if (plainly || hi <= 0)
             end = 0;
         else if ((hi + STEP - 1) / STEP < end)
             end = (hi + STEP - 1) / STEP;
