@@ -26,7 +26,7 @@ struct AttnArgs {
     float scale;
     i64 qs[3], ks[3], vs[3]; // strides: sequence, token, head
     // few queries: the split of the keys and where its parts go (partial O, then maxima and sums)
-    int splits, rows;
+    int splits, rows, tile_heads;
     float *part_o, *part_ml;
     AttnBuckets bk;
 };

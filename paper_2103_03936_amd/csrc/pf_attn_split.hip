@@ -1,11 +1,12 @@
-// Attention forward of few queries over many keys (decoding): the keys of a sequence are split between workgroups and
-// the parts joined.
+// Attention forward of few queries over many keys (decoding, a chunk of new tokens): the keys of a sequence are split between
+// workgroups and the parts joined.
 //
-// Bound by reading keys and values.  The query heads of one key head, and their few queries, are the columns of one
-// product (row r of the group: query head r / Lq, query r % Lq), so that keys and values are read once for all of them.
+// Bound by reading keys and values.  The query heads of one key head, and their queries, are the rows r of one product (query
+// head r / Lq, query r % Lq), 32 to a workgroup, so that keys and values are read once for all heads that share them.
 // A wave takes 32 keys at a time, in tiles of LDS that are its own, and the next 32 are on their way while these are used; no wave
 // waits for another before the end.  (K straight into the operand's registers meant loads of 32 bytes of 32 rows each, eight
-// times over: a decoding step of 32 sequences of up to 4096 keys took 85 us, not 78.)  The waves' and then the workgroups' results are joined by their maxima and sums in a fixed order.
+// times over: a decoding step of 32 sequences of up to 4096 keys took 85 us, not 78; today 65 to 75, 4.7 TB/s.)  The waves' and then
+// the workgroups' results are joined by their maxima and sums in a fixed order.
 #include "pf_attn.h"
 
 namespace pf {
@@ -20,15 +21,16 @@ struct SplitLds {
 
 // What a workgroup without keys writes: an empty part, or (the only part) rows of zeros
 template <typename T>
-__device__ __forceinline__ void leave_nothing(const AttnArgs &a, int bk, int split, int b, int kv, int t, int threads)
+__device__ __forceinline__ void leave_nothing(const AttnArgs &a, int bk, int tile, int split, int b, int kv, int t, int threads)
 {
     if (a.splits > 1) {
-        float *const ml = a.part_ml + ((i64)bk * a.splits + split) * 64;
+        float *const ml = a.part_ml + (((i64)bk * a.tiles + tile) * a.splits + split) * 64;
         if (t < 64) ml[t] = t & 1 ? 0.f : -INFINITY;
         return;
     }
-    for (int x = t; x < a.rows * a.D; x += threads) {
-        const int r = x / a.D, c = x % a.D, g = r / a.Lq, i = r - g * a.Lq;
+    for (int x = t; x < 32 * a.D; x += threads) {
+        const int r = tile * 32 + x / a.D, c = x % a.D, g = r / a.Lq, i = r - g * a.Lq;
+        if (r >= a.rows) break;
         ((T *)a.O)[(((i64)b * a.Lq + i) * a.Hq + kv * a.G + g) * a.D + c] = from_float<T>(0.f);
         if (c == 0 && a.lse) a.lse[((i64)b * a.Hq + kv * a.G + g) * a.Lq + i] = -INFINITY;
     }
@@ -41,18 +43,22 @@ __global__ __launch_bounds__(64 * SPLIT_WAVES, sizeof(T) * DP <= 256 ? 2 : 1) vo
     using Tl = Tile<T, DP, 32, 64>;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     float *const ml = (float *)(lds + SplitLds<T, DP>::AREA); // [2][NW][32]: the waves' maxima and sums
-    float *const tab = ml + 2 * NW * 32;                      // [buckets][G]: the bias (base 2)
-    uint8_t *const lut = (uint8_t *)(tab + a.buckets * a.G); // bucket of each distance from -far to far
+    float *const tab = ml + 2 * NW * 32;                      // [buckets][heads of the tile]: the bias (base 2)
+    uint8_t *const lut = (uint8_t *)(tab + a.buckets * a.tile_heads); // bucket of each distance from -far to far
     const int t = threadIdx.x, wave = wave_of(t), lane = t & 63, col = lane & 31, h = lane >> 5;
     T *const own_tiles = (T *)(lds + 4 * wave * Tl::BYTES); // two of keys and two of values, this wave's own
 
     const unsigned w = xcd_order(blockIdx.x, gridDim.x);
-    const int split = w % a.splits, bk = w / a.splits, b = bk / a.Hkv, kv = bk - b * a.Hkv;
+    const int split = w % a.splits, tile = w / a.splits % a.tiles, bk = w / a.splits / a.tiles, b = bk / a.Hkv, kv = bk - b * a.Hkv;
     const AttnLens n(a, b);
-    const int r = col, g = r / a.Lq, i = r - g * a.Lq, head = kv * a.G + g;
+    const int r = tile * 32 + col, g = r / a.Lq, i = r - g * a.Lq, head = kv * a.G + g;
     const bool row = r < a.rows, ok = row && i < n.nq;
-    const int pos = i + n.start, pmin = n.start, pmax = n.start + a.Lq - 1;
-    int keys = n.nk;
+    // the queries of the tile, from i0 to i1: all of them where it passes from one head to the next
+    const int r1 = (tile * 32 + 32 < a.rows ? tile * 32 + 32 : a.rows) - 1, first_head = kv * a.G + tile * 32 / a.Lq;
+    const bool one_head = tile * 32 / a.Lq == r1 / a.Lq;
+    const int i0 = one_head ? tile * 32 % a.Lq : 0, i1 = one_head ? r1 % a.Lq : a.Lq - 1;
+    const int pos = i + n.start, pmin = n.start + i0, pmax = n.start + i1;
+    int keys = i0 < n.nq ? n.nk : 0;
     if (a.causal && pmax + 1 < keys) keys = pmax + 1 < 0 ? 0 : pmax + 1;
     const int all = (keys + 31) / 32, per = (all + a.splits - 1) / a.splits;
     const int first = split * per, end = first + per < all ? first + per : all; // groups of 32 keys
@@ -60,7 +66,7 @@ __global__ __launch_bounds__(64 * SPLIT_WAVES, sizeof(T) * DP <= 256 ? 2 : 1) vo
     const int far = a.bk.far;
     float flat_before = 0.f, flat_after = 0.f;
     if (first >= end) { // (no keys: nothing but an empty part to leave)
-        leave_nothing<T>(a, bk, split, b, kv, t, 64 * NW);
+        leave_nothing<T>(a, bk, tile, split, b, kv, t, 64 * NW);
         return;
     }
     const T *const Kp = (const T *)a.K + b * a.ks[0] + kv * a.ks[2], *const Vp = (const T *)a.V + b * a.vs[0] + kv * a.vs[2];
@@ -85,14 +91,15 @@ __global__ __launch_bounds__(64 * SPLIT_WAVES, sizeof(T) * DP <= 256 ? 2 : 1) vo
     if (first + wave < end) fetch(first + wave, 0);
     if constexpr (BIAS) {
         for (int k = t; k <= 2 * far; k += 64 * NW) lut[k] = (uint8_t)bucket_of(a, k - far);
-        for (int k = t; k < a.buckets * a.G; k += 64 * NW)
-            tab[k] = bias_of(a, k / a.G, kv * a.G + k % a.G);
+        const int heads = a.tile_heads < (kv + 1) * a.G - first_head ? a.tile_heads : (kv + 1) * a.G - first_head;
+        for (int k = t; k < a.buckets * a.tile_heads; k += 64 * NW)
+            tab[k] = k % a.tile_heads < heads ? bias_of(a, k / a.tile_heads, first_head + k % a.tile_heads) : 0.f;
     }
-    const float *const mine = tab + (row ? g : 0);
+    const float *const mine = tab + (row ? head - first_head : 0);
     if constexpr (BIAS) {
         __syncthreads();
-        flat_before = mine[bucket_before(a) * a.G];
-        flat_after = mine[bucket_after(a) * a.G];
+        flat_before = mine[bucket_before(a) * a.tile_heads];
+        flat_after = mine[bucket_after(a) * a.tile_heads];
     }
     for (int k = first + wave, turn = 0; k < end; k += NW, turn ^= 1) {
         const int k0 = 32 * k;
@@ -114,7 +121,7 @@ __global__ __launch_bounds__(64 * SPLIT_WAVES, sizeof(T) * DP <= 256 ? 2 : 1) vo
             for (int e = 0; e < 16; ++e) u[e] = lut[clamped(rel + 8 * (e >> 2) + (e & 3), -far, far) + far];
             __builtin_amdgcn_sched_barrier(0); // (all reads of a kind first)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) y[e] = mine[u[e] * a.G];
+            for (int e = 0; e < 16; ++e) y[e] = mine[u[e] * a.tile_heads];
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int e = 0; e < 16; ++e) s[e] = s[e] * sl2 + y[e];
@@ -180,7 +187,7 @@ __global__ __launch_bounds__(64 * SPLIT_WAVES, sizeof(T) * DP <= 256 ? 2 : 1) vo
         __syncthreads();
     }
     // the rows, one after the other: adjacent lanes have adjacent columns of one row
-    const i64 piece = (i64)bk * a.splits + split;
+    const i64 piece = ((i64)bk * a.tiles + tile) * a.splits + split;
     if (wave == 0 && h == 0 && a.splits > 1) {
         a.part_ml[(piece * 32 + col) * 2] = top;
         a.part_ml[(piece * 32 + col) * 2 + 1] = total;
@@ -189,13 +196,13 @@ __global__ __launch_bounds__(64 * SPLIT_WAVES, sizeof(T) * DP <= 256 ? 2 : 1) vo
         a.lse[((i64)b * a.Hq + head) * a.Lq + i] = ok && total != 0.f ? (top + __builtin_amdgcn_logf(total)) * LN2 : -INFINITY;
     if (a.splits == 1 && wave == 0 && h == 0) ml[col] = ok && total != 0.f ? 1.f / total : 0.f;
     __syncthreads();
-    for (int x = t; x < a.rows * DP; x += 64 * NW) {
+    for (int x = t; x < (r1 - tile * 32 + 1) * DP; x += 64 * NW) {
         const int rr = x / DP, c = x % DP;
         if (c >= a.D) continue;
         if (a.splits > 1) {
             a.part_o[(piece * 32 + rr) * DP + c] = join[c * 33 + rr];
         } else {
-            const int gg = rr / a.Lq, ii = rr - gg * a.Lq;
+            const int gg = (tile * 32 + rr) / a.Lq, ii = tile * 32 + rr - gg * a.Lq;
             const float inv = ml[rr];
             ((T *)a.O)[(((i64)b * a.Lq + ii) * a.Hq + kv * a.G + gg) * a.D + c] = from_float<T>(inv != 0.f ? join[c * 33 + rr] * inv : 0.f);
         }
@@ -211,8 +218,8 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, int DP)
     if (all >= (i64)a.B * a.Hkv * a.rows) return;
     const int bk = (int)(all / a.rows), r = (int)(all - (i64)bk * a.rows), b = bk / a.Hkv, kv = bk - b * a.Hkv;
     const int g = r / a.Lq, i = r - g * a.Lq, head = kv * a.G + g;
-    const i64 piece = (i64)bk * a.splits;
-    const float *const ml = a.part_ml + (piece * 32 + r) * 2, *const po = a.part_o + (piece * 32 + r) * DP;
+    const i64 piece = ((i64)bk * a.tiles + r / 32) * a.splits;
+    const float *const ml = a.part_ml + (piece * 32 + r % 32) * 2, *const po = a.part_o + (piece * 32 + r % 32) * DP;
     // lane s: part s (and s + 64 ..)
     float top = -INFINITY, total = 0.f;
     for (int s = lane; s < a.splits; s += 64) top = fmaxf(top, ml[s * 64]);
@@ -248,11 +255,19 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, int DP)
 }
 
 // ------------------------------------------------------------------ host
+static i64 row_tiles(const pf_attention_desc *d) { return (d->Lq * (d->heads_q / d->heads_kv) + 31) / 32; }
 int attn_split_count(const pf_attention_desc *d)
 {
-    const i64 rows = d->Lq * (d->heads_q / d->heads_kv);
-    if (rows > 32 || d->Lk == 0) return 0;
-    const i64 base = d->B * d->heads_kv;
+    if (d->Lk == 0) return 0;
+    if (d->Lq * (d->heads_q / d->heads_kv) > 32) {
+        // More rows than one product takes: where the ordinary kernel has few tiles of 128 queries and many keys for each.  us, 128
+        // queries, bf16, heads of 128: 4 tiles of 8192 keys 98 ordinary and 22 split, 32 of 8192 100 and 63, 64 of 8192 103 and 102, 16 of
+        // 2048 31 and 23, 32 of 2048 32 and 36, 8 of 1024 20 and 17, 8 of 512 14 and 17; float, heads of 64: 8 of 600 32 and 22, 32 of
+        // 2048 86 and 56, 32 of 600 33 and 31.
+        const i64 tiles = d->B * d->heads_q * ((d->Lq + 127) / 128);
+        if (tiles > 64 || tiles * (d->dtype == PF_BF16 ? 128 : 32) > d->Lk) return 0;
+    }
+    const i64 base = d->B * d->heads_kv * row_tiles(d);
     // pieces of 256 keys or more; sequences differ in length, so that there are more pieces (1024) than places for them
     // (512: 32 sequences of up to 4096 keys took 78 us with 512 pieces, 76 with 1024, 82 with 2048)
     i64 n = (1024 + base - 1) / base, most = (d->Lk + 255) / 256;
@@ -264,15 +279,15 @@ size_t attn_split_bytes(const pf_attention_desc *d)
 {
     const int n = attn_split_count(d);
     if (n <= 1) return 0;
-    const i64 pieces = d->B * d->heads_kv * n;
+    const i64 pieces = d->B * d->heads_kv * row_tiles(d) * n;
     return align_up((size_t)pieces * 32 * 2 * sizeof(float)) + align_up((size_t)pieces * 32 * padded(d->head_dim) * sizeof(float));
 }
 
 template <typename T, int DP>
 static int attn_split_launch(const AttnArgs &a, hipStream_t s)
 {
-    const unsigned blocks = (unsigned)a.B * a.Hkv * a.splits;
-    const size_t lds = SplitLds<T, DP>::AREA + 2 * SPLIT_WAVES * 32 * sizeof(float) + (a.buckets ? a.buckets * a.G * sizeof(float) + 2 * a.bk.far + 1 : 0);
+    const unsigned blocks = (unsigned)a.B * a.Hkv * a.tiles * a.splits;
+    const size_t lds = SplitLds<T, DP>::AREA + 2 * SPLIT_WAVES * 32 * sizeof(float) + (a.buckets ? a.buckets * a.tile_heads * sizeof(float) + 2 * a.bk.far + 1 : 0);
     int st = PF_OK;
     if (a.buckets)
         PF_LAUNCH_LDS(st, "attn_split", (attn_split_kernel<T, DP, true>), dim3(blocks), dim3(64 * SPLIT_WAVES), lds, s, a);
@@ -289,9 +304,11 @@ int attn_split_fwd(const pf_attention_desc *d, AttnArgs &a, void *workspace, hip
 {
     a.splits = attn_split_count(d);
     a.rows = a.Lq * a.G;
+    a.tiles = (a.rows + 31) / 32;
+    a.tile_heads = a.G < 31 / a.Lq + 2 ? a.G : 31 / a.Lq + 2; // heads that 32 rows may touch
     const int DP = padded(a.D);
     if (a.splits > 1) {
-        const size_t pieces = (size_t)a.B * a.Hkv * a.splits;
+        const size_t pieces = (size_t)a.B * a.Hkv * a.tiles * a.splits;
         a.part_ml = (float *)workspace;
         a.part_o = (float *)((char *)workspace + align_up(pieces * 32 * 2 * sizeof(float)));
     }

@@ -311,3 +311,12 @@ def test_one_key(c, dtype):
         assert not x.any()
     dO = d["dO"].astype(np.float64)
     assert_within(dV, o.backward(dO)[2], attention_bounds(o, dO, dtype)[4], "dV")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("c", [(1, 100, 900, 4, 1, 64, True, 32, 128, "append"), (2, 45, 1300, 3, 1, 128, False, 16, 64, "pad"),
+                               (1, 130, 1500, 2, 2, 40, True, 0, 0, "append"), (1, 33, 500, 1, 1, 32, True, 32, 128, None),
+                               (2, 70, 700, 2, 2, 96, True, 8, 16, "before"), (1, 12, 2000, 6, 2, 64, False, 32, 128, "pad")], ids=str)
+def test_few_queries_many_keys(c, dtype):
+    """More rows than one product takes and keys split between workgroups: tiles that pass from one head to the next, and do not."""
+    test_against_definition(c, dtype)
