@@ -74,28 +74,6 @@ __device__ __forceinline__ Frag<float> row_frag_global(const float *row, int col
     return f;
 }
 
-// The same through a descriptor that ends with the last row; `at`: bytes to the lane's row
-__device__ __forceinline__ Frag<bf16_t> row_frag_buffer(const BufSrc &src, uint32_t at, int col, int D, int h, bf16_t *)
-{
-    union {
-        uint4 u;
-        bf16x8_t v;
-    } w;
-    w.u = src.load(col + 8 * h < D ? at + 2 * (col + 8 * h) : BUF_OUT);
-    Frag<bf16_t> f;
-    f.v = w.v;
-    return f;
-}
-__device__ __forceinline__ Frag<float> row_frag_buffer(const BufSrc &src, uint32_t at, int col, int D, int h, float *)
-{
-    const uint4 a = src.load(col + 4 * h < D ? at + 4 * (col + 4 * h) : BUF_OUT), b = src.load(col + 8 + 4 * h < D ? at + 4 * (col + 8 + 4 * h) : BUF_OUT);
-    Frag<float> f;
-    const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-    for (int e = 0; e < 8; ++e) f.v[e] = __uint_as_float(w[e]);
-    return f;
-}
-
 // Eight values of a result (its registers 8 c .. 8 c + 7) as the operand for rows 16 c .. 16 c + 15; bf16: rounded to
 // nearest even, the one rounding of P and dS, half a step of 2^-8 each
 __device__ __forceinline__ void pack(const f32x16_t &x, int c, Frag<bf16_t> &f)
