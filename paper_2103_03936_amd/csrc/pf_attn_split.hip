@@ -237,8 +237,10 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, int DP)
         }
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            const float g = s0 + k < a.splits ? exp2_fast(f[k] - base) : 0.f;
-            if (g != 0.f) { // (an empty part has no rows)
+            // A part without a key that the row sees has left no values, only the sum 0.  (Not told by its maximum: that of
+            // scores that are all NaN is -infinity, too, and their sum is NaN.)
+            if (s0 + k < a.splits && w[k] != 0.f) {
+                const float g = exp2_fast(f[k] - base);
                 total += w[k] * g;
                 o[0] += y[k] * g;
                 o[1] += z[k] * g;
