@@ -258,9 +258,29 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, int DP)
 
 // ------------------------------------------------------------------ host
 static i64 row_tiles(const pf_attention_desc *d) { return (d->Lq * (d->heads_q / d->heads_kv) + 31) / 32; }
+static int padded(int D) { return (D + 31) / 32 * 32; }
+// The most heads that 32 rows touch, of G heads with Lq rows each
+static int heads_of_tile(i64 Lq, int G) { return (int)(G < 31 / Lq + 2 ? G : 31 / Lq + 2); }
+// LDS of a workgroup: tiles, the waves' maxima and sums, the bias of the tile's heads by bucket and the bucket of each distance
+static size_t split_lds(size_t area, int buckets, int heads, int far)
+{
+    return area + 2 * SPLIT_WAVES * 32 * sizeof(float) + (buckets ? (size_t)buckets * heads * sizeof(float) + 2 * far + 1 : 0);
+}
+// Float rows of more than 64 values fill 128 KB with tiles: 256 buckets of 32 heads do not fit beside them.  The ordinary kernel has
+// one head's bias in LDS and takes any.
+static bool split_fits(const pf_attention_desc *d)
+{
+    const int DP = padded(d->head_dim), heads = heads_of_tile(d->Lq, d->heads_q / d->heads_kv);
+    const bool bf16 = d->dtype == PF_BF16;
+    const size_t area = DP == 32 ? (bf16 ? SplitLds<bf16_t, 32>::AREA : SplitLds<float, 32>::AREA)
+                      : DP == 64 ? (bf16 ? SplitLds<bf16_t, 64>::AREA : SplitLds<float, 64>::AREA)
+                      : DP == 96 ? (bf16 ? SplitLds<bf16_t, 96>::AREA : SplitLds<float, 96>::AREA)
+                                 : (bf16 ? SplitLds<bf16_t, 128>::AREA : SplitLds<float, 128>::AREA);
+    return split_lds(area, d->buckets, heads, d->max_distance) <= 160 * 1024; // (no border lies behind max_distance)
+}
 int attn_split_count(const pf_attention_desc *d)
 {
-    if (d->Lk == 0) return 0;
+    if (d->Lk == 0 || !split_fits(d)) return 0;
     if (d->Lq * (d->heads_q / d->heads_kv) > 32) {
         // More rows than one product takes: where the ordinary kernel has few tiles of 128 queries and many keys for each.  us, 128
         // queries, bf16, heads of 128: 4 tiles of 8192 keys 98 ordinary and 22 split, 32 of 8192 100 and 63, 64 of 8192 103 and 102, 16 of
@@ -276,7 +296,6 @@ int attn_split_count(const pf_attention_desc *d)
     n = n < most ? n : most;
     return (int)(n < 1 ? 1 : n > 256 ? 256 : n);
 }
-static int padded(int D) { return (D + 31) / 32 * 32; }
 size_t attn_split_bytes(const pf_attention_desc *d)
 {
     const int n = attn_split_count(d);
@@ -289,7 +308,7 @@ template <typename T, int DP>
 static int attn_split_launch(const AttnArgs &a, hipStream_t s)
 {
     const unsigned blocks = (unsigned)a.B * a.Hkv * a.tiles * a.splits;
-    const size_t lds = SplitLds<T, DP>::AREA + 2 * SPLIT_WAVES * 32 * sizeof(float) + (a.buckets ? a.buckets * a.tile_heads * sizeof(float) + 2 * a.bk.far + 1 : 0);
+    const size_t lds = split_lds(SplitLds<T, DP>::AREA, a.buckets, a.tile_heads, a.bk.far);
     int st = PF_OK;
     if (a.buckets)
         PF_LAUNCH_LDS(st, "attn_split", (attn_split_kernel<T, DP, true>), dim3(blocks), dim3(64 * SPLIT_WAVES), lds, s, a);
@@ -307,7 +326,7 @@ int attn_split_fwd(const pf_attention_desc *d, AttnArgs &a, void *workspace, hip
     a.splits = attn_split_count(d);
     a.rows = a.Lq * a.G;
     a.tiles = (a.rows + 31) / 32;
-    a.tile_heads = a.G < 31 / a.Lq + 2 ? a.G : 31 / a.Lq + 2; // heads that 32 rows may touch
+    a.tile_heads = heads_of_tile(a.Lq, a.G);
     const int DP = padded(a.D);
     if (a.splits > 1) {
         const size_t pieces = (size_t)a.B * a.Hkv * a.tiles * a.splits;
