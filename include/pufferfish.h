@@ -538,6 +538,9 @@ int pf_qk_norm_rotate_bwd(const pf_qk_norm_desc *d, const void *Q, const void *K
 /* logarithmically up to max_distance:                                   */
 /*   bucket(n) = min(nb - 1, e + floor((nb - e) log(n/e) / log(max_distance/e))) */
 /* for n >= e, with the borders where exact arithmetic has them.         */
+/* Entries of the table may have any size, the type's lowest value and    */
+/* -infinity among them: what all keys that a query sees have in common   */
+/* costs its scores no digits (finite ones beyond 2.3e38 count as that).  */
 /* Limits (PF_ERR_UNSUPPORTED): head_dim a multiple of 8, 8 .. 128;       */
 /* buckets 0 or 2 .. 256, with bidirectional a multiple of 2 and >= 4;    */
 /* max_distance > e and <= 1024; Lq, Lk < 2^29; fewer than 2^31 blocks of  */

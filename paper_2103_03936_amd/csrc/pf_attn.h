@@ -25,9 +25,9 @@ struct AttnArgs {
     int B, Lq, Lk, Hq, Hkv, G, D, causal, buckets, two_sided, tiles;
     float scale;
     i64 qs[3], ks[3], vs[3]; // strides: sequence, token, head
-    // few queries: the split of the keys and where its parts go (partial O, then maxima and sums)
+    // few queries: the split of the keys and where its parts go (partial O, maxima and sums), what the rows' biases are relative to
     int splits, rows, tile_heads;
-    float *part_o, *part_ml;
+    float *part_o, *part_ml, *part_shift;
     AttnBuckets bk;
 };
 
@@ -264,10 +264,42 @@ __device__ __forceinline__ float bias_of(const AttnArgs &a, int bucket, int head
     const float x = a.table[(i64)bucket * a.Hq + head], y = x * LOG2E;
     return __builtin_isinf(y) && !__builtin_isinf(x) ? __builtin_copysignf(3.4028234e38f, x) : y;
 }
-// bias[far + d], d = -far .. far: the head's bias at distance d (further ones have that of +-far), times log2(e)
-__device__ __forceinline__ void fill_bias(const AttnArgs &a, float *bias, int head, int t, int threads)
+// A bias (base 2) from here on takes so many digits that what is added to it loses more than float's sums do.  Softmax does not
+// change with what a whole row shares: where the largest bias that a row sees is such a one, all of the row's are taken relative to it.
+constexpr float ATTN_LARGE = 1024.f;
+__device__ __forceinline__ bool is_large(float x) { return fabsf(x) >= ATTN_LARGE && !__builtin_isinf(x); }
+// bias[far + d], d = -far .. far: the head's bias at distance d (further ones have that of +-far), times log2(e).  Whether the
+// thread met a large one.
+__device__ __forceinline__ bool fill_bias(const AttnArgs &a, float *bias, int head, int t, int threads)
 {
-    for (int i = t; i <= 2 * a.bk.far; i += threads) bias[i] = bias_of(a, bucket_of(a, i - a.bk.far), head);
+    bool large = false;
+    for (int i = t; i <= 2 * a.bk.far; i += threads) {
+        const float x = bias_of(a, bucket_of(a, i - a.bk.far), head);
+        bias[i] = x;
+        large |= is_large(x);
+    }
+    return large;
+}
+// Whether any thread of four waves has x: each wave leaves its answer before a barrier, all read them behind it
+__device__ __forceinline__ void leave(int *flags, bool x, int wave, int lane)
+{
+    const int any = __any(x);
+    if (lane == 0) flags[wave] = any;
+}
+__device__ __forceinline__ bool left(const int *flags, int waves)
+{
+    int any = 0;
+    for (int k = 0; k < waves; ++k) any |= flags[k];
+    return __builtin_amdgcn_readfirstlane(any) != 0;
+}
+// What the biases of a row that sees the distances lo .. hi are taken relative to; at(d) is the row's bias at distance d
+template <class F>
+__device__ __forceinline__ float row_shift(int lo, int hi, int far, F at)
+{
+    float top = -INFINITY;
+    if (lo <= hi)
+        for (int d = clamped(lo, -far, far); d <= clamped(hi, -far, far); ++d) top = fmaxf(top, at(d));
+    return is_large(top) ? top : 0.f;
 }
 
 // Scores of a block at an edge or near the diagonal: s scale + bias (base 2) - less; register e holds the distance

@@ -56,7 +56,8 @@ __device__ __forceinline__ void attn_fwd_tile(const AttnArgs &a, char *lds, int 
 #pragma unroll
         for (int c = 0; c < DP / 16; ++c) q[c] = row_frag_global(Qp, 16 * c, a.D, h, ok);
     }
-    if (BIAS && keys > 0) fill_bias(a, bias, head, t, 256); // (behind the loads that it need not wait for)
+    __shared__ int large[4];
+    if (BIAS && keys > 0) leave(large, fill_bias(a, bias, head, t, 256), wave, lane); // (behind the loads that it need not wait for)
     const float sl2 = a.scale * LOG2E;
     const int far = a.bk.far;
     f32x16_t o[DP / 32];
@@ -69,6 +70,8 @@ __device__ __forceinline__ void attn_fwd_tile(const AttnArgs &a, char *lds, int 
     constexpr int CH = DP / 16, SC = SUB * CH, DB = DP / 32, PV = 2 * SUB * DB, AHEAD = 3;
     fetched();
     __syncthreads();
+    float shift = 0.f; // what the row's biases, and its maximum, are relative to
+    if (BIAS && keys > 0 && left(large, 4)) shift = row_shift(-pos, most, far, [&](int x) { return bias[far + x]; });
     if (own < mine) {
 #pragma unroll
         for (int u = 0; u < SUB; ++u) {
@@ -88,7 +91,7 @@ __device__ __forceinline__ void attn_fwd_tile(const AttnArgs &a, char *lds, int 
         if (k0 < mine) {
             const bool edge = k0 + KT > n.nk || (a.causal && k0 + KT - 1 > pmin);
             const bool near = BIAS && k0 + KT - 1 - pmin > -far && k0 - pmax < far;
-            const float flat = BIAS ? bias[k0 >= pmin ? 2 * far : 0] : 0.f; // where no key is near
+            const float flat = BIAS ? bias[k0 >= pmin ? 2 * far : 0] - shift : 0.f; // where no key is near
             // Away from the edges and the near keys, nothing is done to a product but one fused multiply-add on its way into
             // the exponential; the maximum is that of the products themselves.
             const bool plain = !edge && !near && sl2 > 0.f;
@@ -99,7 +102,7 @@ __device__ __forceinline__ void attn_fwd_tile(const AttnArgs &a, char *lds, int 
                 const int rel = anew(k0 + 4 * h - pos); // distance of the first key that the lane holds
 #pragma unroll
                 for (int u = 0; u < SUB; ++u) {
-                    finish_scores<BIAS>(s[u], sl2, 0.f, bias, far, rel + 32 * u, 1, most);
+                    finish_scores<BIAS>(s[u], sl2, shift, bias, far, rel + 32 * u, 1, most);
 #pragma unroll
                     for (int e = 0; e < 16; ++e) top = fmaxf(top, s[u][e]);
                 }
@@ -198,7 +201,7 @@ __device__ __forceinline__ void attn_fwd_tile(const AttnArgs &a, char *lds, int 
             for (int x = 0; x < 4; ++x) v[x] = some ? o[d][e + x] * inv : 0.f;
             if (c < a.D) put4(Op + c, v[0], v[1], v[2], v[3]);
         }
-    if (a.lse && h == 0) a.lse[((i64)b * a.Hq + head) * a.Lq + i] = some ? (m + __builtin_amdgcn_logf(sum)) * LN2 : -INFINITY;
+    if (a.lse && h == 0) a.lse[((i64)b * a.Hq + head) * a.Lq + i] = some ? (m + __builtin_amdgcn_logf(sum)) * LN2 + shift * LN2 : -INFINITY;
 }
 
 // paired: a workgroup has a long tile of queries and a short one (causal; a.tiles of them to a head), so that all take the

@@ -89,17 +89,26 @@ __global__ __launch_bounds__(64 * SPLIT_WAVES, sizeof(T) * DP <= 256 ? 2 : 1) vo
         vl.fetch(own_tiles + (2 + turn) * Tl::SIZE, Vp + (i64)(32 * k) * a.vs[1], a.vs[1], keys - 32 * k, a.D, 0);
     };
     if (first + wave < end) fetch(first + wave, 0);
+    __shared__ int large[NW];
     if constexpr (BIAS) {
         for (int k = t; k <= 2 * far; k += 64 * NW) lut[k] = (uint8_t)bucket_of(a, k - far);
         const int heads = a.tile_heads < (kv + 1) * a.G - first_head ? a.tile_heads : (kv + 1) * a.G - first_head;
-        for (int k = t; k < a.buckets * a.tile_heads; k += 64 * NW)
-            tab[k] = k % a.tile_heads < heads ? bias_of(a, k / a.tile_heads, first_head + k % a.tile_heads) : 0.f;
+        bool any = false;
+        for (int k = t; k < a.buckets * a.tile_heads; k += 64 * NW) {
+            const float x = k % a.tile_heads < heads ? bias_of(a, k / a.tile_heads, first_head + k % a.tile_heads) : 0.f;
+            tab[k] = x;
+            any |= is_large(x);
+        }
+        leave(large, any, wave, lane);
     }
     const float *const mine = tab + (row ? head - first_head : 0);
+    float shift = 0.f; // what the row's biases, and its maximum, are relative to (in all parts the same: by all keys that it sees)
     if constexpr (BIAS) {
         __syncthreads();
-        flat_before = mine[bucket_before(a) * a.tile_heads];
-        flat_after = mine[bucket_after(a) * a.tile_heads];
+        if (left(large, NW))
+            shift = row_shift(-pos, a.causal && n.nk > pos ? 0 : n.nk - 1 - pos, far, [&](int x) { return mine[lut[far + x] * a.tile_heads]; });
+        flat_before = mine[bucket_before(a) * a.tile_heads] - shift;
+        flat_after = mine[bucket_after(a) * a.tile_heads] - shift;
     }
     for (int k = first + wave, turn = 0; k < end; k += NW, turn ^= 1) {
         const int k0 = 32 * k;
@@ -124,7 +133,7 @@ __global__ __launch_bounds__(64 * SPLIT_WAVES, sizeof(T) * DP <= 256 ? 2 : 1) vo
             for (int e = 0; e < 16; ++e) y[e] = mine[u[e] * a.tile_heads];
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) s[e] = s[e] * sl2 + y[e];
+            for (int e = 0; e < 16; ++e) s[e] = s[e] * sl2 + (y[e] - shift);
         } else {
 #pragma unroll
             for (int e = 0; e < 16; ++e) s[e] = s[e] * sl2 + (BIAS ? flat : 0.f);
@@ -191,9 +200,10 @@ __global__ __launch_bounds__(64 * SPLIT_WAVES, sizeof(T) * DP <= 256 ? 2 : 1) vo
     if (wave == 0 && h == 0 && a.splits > 1) {
         a.part_ml[(piece * 32 + col) * 2] = top;
         a.part_ml[(piece * 32 + col) * 2 + 1] = total;
+        if (split == 0) a.part_shift[((i64)bk * a.tiles + tile) * 32 + col] = shift; // (if any part has keys, this one has)
     }
     if (wave == 0 && h == 0 && a.splits == 1 && a.lse && row)
-        a.lse[((i64)b * a.Hq + head) * a.Lq + i] = ok && total != 0.f ? (top + __builtin_amdgcn_logf(total)) * LN2 : -INFINITY;
+        a.lse[((i64)b * a.Hq + head) * a.Lq + i] = ok && total != 0.f ? (top + __builtin_amdgcn_logf(total)) * LN2 + shift * LN2 : -INFINITY;
     if (a.splits == 1 && wave == 0 && h == 0) ml[col] = ok && total != 0.f ? 1.f / total : 0.f;
     __syncthreads();
     for (int x = t; x < (r1 - tile * 32 + 1) * DP; x += 64 * NW) {
@@ -253,7 +263,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, int DP)
 #pragma unroll
     for (int k = 0; k < 2; ++k)
         if (lane + 64 * k < a.D) O[lane + 64 * k] = from_float<T>(some ? o[k] / total : 0.f);
-    if (a.lse && lane == 0) a.lse[((i64)b * a.Hq + head) * a.Lq + i] = some ? (top + __builtin_amdgcn_logf(total)) * LN2 : -INFINITY;
+    if (a.lse && lane == 0) a.lse[((i64)b * a.Hq + head) * a.Lq + i] = some ? (top + __builtin_amdgcn_logf(total)) * LN2 + a.part_shift[piece / a.splits * 32 + r % 32] * LN2 : -INFINITY;
 }
 
 // ------------------------------------------------------------------ host
@@ -276,7 +286,8 @@ static bool split_fits(const pf_attention_desc *d)
                       : DP == 64 ? (bf16 ? SplitLds<bf16_t, 64>::AREA : SplitLds<float, 64>::AREA)
                       : DP == 96 ? (bf16 ? SplitLds<bf16_t, 96>::AREA : SplitLds<float, 96>::AREA)
                                  : (bf16 ? SplitLds<bf16_t, 128>::AREA : SplitLds<float, 128>::AREA);
-    return split_lds(area, d->buckets, heads, d->max_distance) <= 160 * 1024; // (no border lies behind max_distance)
+    // (no border lies behind max_distance; 16 bytes of the kernel's own)
+    return split_lds(area, d->buckets, heads, d->max_distance) + 16 <= 160 * 1024;
 }
 int attn_split_count(const pf_attention_desc *d)
 {
@@ -301,7 +312,8 @@ size_t attn_split_bytes(const pf_attention_desc *d)
     const int n = attn_split_count(d);
     if (n <= 1) return 0;
     const i64 pieces = d->B * d->heads_kv * row_tiles(d) * n;
-    return align_up((size_t)pieces * 32 * 2 * sizeof(float)) + align_up((size_t)pieces * 32 * padded(d->head_dim) * sizeof(float));
+    return align_up((size_t)pieces * 32 * 2 * sizeof(float)) + align_up((size_t)pieces * 32 * padded(d->head_dim) * sizeof(float)) +
+           align_up((size_t)pieces / n * 32 * sizeof(float));
 }
 
 template <typename T, int DP>
@@ -332,6 +344,7 @@ int attn_split_fwd(const pf_attention_desc *d, AttnArgs &a, void *workspace, hip
         const size_t pieces = (size_t)a.B * a.Hkv * a.tiles * a.splits;
         a.part_ml = (float *)workspace;
         a.part_o = (float *)((char *)workspace + align_up(pieces * 32 * 2 * sizeof(float)));
+        a.part_shift = (float *)((char *)a.part_o + align_up(pieces * 32 * DP * sizeof(float)));
     }
     if (d->dtype == PF_BF16)
         return DP == 32 ? attn_split_launch<bf16_t, 32>(a, s) : DP == 64 ? attn_split_launch<bf16_t, 64>(a, s)
