@@ -20,7 +20,8 @@ struct AttnArgs {
     const void *Q, *K, *V, *dO, *Oin;
     void *O, *dQ, *dK, *dV;
     const float *table, *lse_in;
-    float *lse, *delta, *tab; // delta[B, Hq, Lq][2]: lse (base 2; infinity where a query takes no part) and -delta; tab[Hq][B * tiles][buckets]: sums of dS per workgroup
+    float *lse, *stat, *tab; // stat[B, Hq][records]: what dK and dV need of each 32 queries (StatRecord); tab[Hq][B * tiles][buckets]: sums of dS per workgroup
+    int records;
     const int *q_start, *q_len, *kv_len;
     int B, Lq, Lk, Hq, Hkv, G, D, causal, buckets, two_sided, tiles;
     float scale;
@@ -29,6 +30,13 @@ struct AttnArgs {
     int splits, rows, tile_heads;
     float *part_o, *part_ml, *part_shift;
     AttnBuckets bk;
+};
+
+// Of 32 queries: P = exp2((S - shift) - rest), S with its bias (base 2); shift is infinity where a query takes no part
+struct StatRecord {
+    float before[32], after[32]; // the bias of a key far before, far after the query, less shift and rest
+    float neg_delta[32], shift[32], neg_rest[32];
+    float with_rest[32]; // [0]: whether a rest is not zero
 };
 
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
@@ -302,10 +310,10 @@ __device__ __forceinline__ float row_shift(int lo, int hi, int far, F at)
     return is_large(top) ? top : 0.f;
 }
 
-// Scores of a block at an edge or near the diagonal: s scale + bias (base 2) - less; register e holds the distance
-// rel + step (8 (e / 4) + e % 4), what is further than `most` is not seen
-template <bool BIAS>
-__device__ __forceinline__ void finish_scores(f32x16_t &s, float scale, float less, const float *bias, int far, int rel, int step, int most)
+// Scores of a block at an edge or near the diagonal: s scale + (bias (base 2) - less); register e holds the distance
+// rel + step (8 (e / 4) + e % 4), what is further than `most` is not seen.  less(e): of its row
+template <bool BIAS, class F>
+__device__ __forceinline__ void finish_scores_by(f32x16_t &s, float scale, F less, const float *bias, int far, int rel, int step, int most)
 {
     float y[16];
 #pragma unroll
@@ -313,7 +321,22 @@ __device__ __forceinline__ void finish_scores(f32x16_t &s, float scale, float le
     __builtin_amdgcn_sched_barrier(0); // (all reads first)
 #pragma unroll
     for (int e = 0; e < 16; ++e)
-        s[e] = fminf(s[e] * scale + (y[e] - less), rel + step * (8 * (e >> 2) + (e & 3)) > most ? -INFINITY : INFINITY);
+        s[e] = fminf(s[e] * scale + (y[e] - less(e)), rel + step * (8 * (e >> 2) + (e & 3)) > most ? -INFINITY : INFINITY);
+}
+// the lane has one query
+template <bool BIAS>
+__device__ __forceinline__ void finish_scores(f32x16_t &s, float scale, float less, const float *bias, int far, int rel, int step, int most)
+{
+    finish_scores_by<BIAS>(s, scale, [&](int) { return less; }, bias, far, rel, step, most);
+}
+// register e has the query 8 (e / 4) + e % 4 of those whose values lie at `less`, in LDS
+template <bool BIAS>
+__device__ __forceinline__ void finish_scores(f32x16_t &s, float scale, const float *less, const float *bias, int far, int rel, int step, int most)
+{
+    f32x4_t x[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = *(const f32x4_t *)(less + 8 * e);
+    finish_scores_by<BIAS>(s, scale, [&](int e) { return x[e / 4][e % 4]; }, bias, far, rel, step, most);
 }
 
 // XCDs take workgroups in turn: consecutive pieces of work (the tiles of a head, which share keys and values) go to one XCD

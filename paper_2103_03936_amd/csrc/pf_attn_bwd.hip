@@ -13,6 +13,11 @@
 // 2^-9 of delta then.  For queries that see many keys that is below what rounding dS itself costs dQ and dK; where some see few,
 // delta is formed from P and dP first.  For dtable, a float32 sum over all pairs in which the rows' errors would stay, it is never
 // good enough.  What delta is off by is the sum of the row's dS, so that it is known once the row is through.
+//
+// P = exp2((S - shift) - rest), shift = lse (base 2) and rest = 0.  An lse of 1024 or more has lost digits that P needs (at 1e9, a bias on
+// all keys that a query sees, it is known to +-64).  A tile with such a row goes through its keys before: shift is then the largest bias
+// that the row sees, or else its largest score, and rest comes from the row's own sum.  S is not formed at its full size then:
+// shift is taken off the bias before the product is added.
 #include "pf_attn.h"
 #include "pf_gemm.h"
 
@@ -36,7 +41,7 @@ struct DqLds {
 template <typename T, int DP, int KW, int QW>
 struct DkvLds {
     using Tl = Tile<T, DP, 32 * QW, 64 * KW * QW>;
-    static size_t bytes(int far, bool bias) { return 6 * Tl::BYTES + 3 * 2 * 32 * QW * 4 + (bias ? (2 * far + 1) * 4 : 0); }
+    static size_t bytes(int far, bool bias) { return 6 * Tl::BYTES + 3 * QW * sizeof(StatRecord) + (bias ? (2 * far + 1) * 4 : 0); }
 };
 
 // dQ, delta and the sums of dS by distance, for one tile of 128 queries of one head.  TAB: with the gradient of the table.
@@ -89,7 +94,7 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b
     // tokens: dQ off by 6e-3, by 3e-3 with the exact one; the rounding of dS alone makes 2.4e-3 of any length)
     const int position0 = tile * QUERIES + n.start, fewest = a.causal && position0 + 1 < keys ? position0 + 1 : keys;
     const bool few = sizeof(T) == 2 && groups > 0 && fewest <= 128;
-    const bool plainly = few || (sizeof(T) == 4 && TAB);
+    bool plainly = few || (sizeof(T) == 4 && TAB);
     const auto fetch2 = [&](int j) { fetch(j, j & 1, (j & 1) - 1); }; // (two groups of keys, two of values)
     if (groups > 0) {
         if (plainly)
@@ -125,6 +130,10 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b
         const float x = a.lse_in[stat];
         if (x != -INFINITY) lse2 = x * LOG2E;
     }
+    __shared__ int flags[4];
+    const bool large = fabsf(lse2) >= ATTN_LARGE && lse2 != INFINITY;
+    leave(flags, large, wave, lane);
+    float shift = lse2, rest = 0.f;
     const float sl2 = a.scale * LOG2E;
     f32x16_t dq[DB];
 #pragma unroll
@@ -132,7 +141,7 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b
     float before = 0.f, after = 0.f, before_p = 0.f, after_p = 0.f, off = 0.f; // far sums of dS and P; the sum of all dS
 
     const auto near_at = [&](int k0) { return BIAS && k0 + 31 - pmin > -far && k0 - pmax < far; };
-    const auto finish = [&](f32x16_t &s, int k0) { finish_scores<BIAS>(s, sl2, lse2, bias, far, anew(k0 + 4 * h - pos), 1, most); };
+    const auto finish = [&](f32x16_t &s, int k0) { finish_scores<BIAS>(s, sl2, shift, bias, far, anew(k0 + 4 * h - pos), 1, most); };
     if (BIAS && keys > 0) fill_bias(a, bias, head, t, 256); // (behind the loads that it need not wait for)
     if constexpr (TAB)
         for (int x = t; x < 4 * span; x += 256) sums_all[x] = 0.f;
@@ -152,16 +161,67 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b
         }
         finish(s, STEP * j + own);
     };
-    // The sum over the waves that share queries (between two barriers the tiles' room is free)
-    const auto over_waves = [&](float x) {
+    // The sum (or the largest) over the waves that share queries (between two barriers the tiles' room is free)
+    const auto over_waves = [&](float x, bool sum = true) {
         if constexpr (KW == 1) return x;
         float *const y = (float *)lds + DP * 64 + lane;
         y[wave * 64] = x;
         __syncthreads();
-        x = y[(wave & ~1) * 64] + y[(wave | 1) * 64];
+        const float u = y[(wave & ~1) * 64], v = y[(wave | 1) * 64];
         __syncthreads();
-        return x;
+        return sum ? u + v : fmaxf(u, v);
     };
+    // Over all keys, what f makes of a group's S and dP
+    const auto over_keys = [&](auto f) {
+#pragma unroll 1
+        for (int j = 0; j < groups; ++j) {
+            if (j + 1 < groups) fetch2(j + 1);
+            if (STEP * j + own < mine) {
+                f32x16_t s, dp;
+                form(j, 0.f, s, dp);
+                f(s, dp);
+            }
+            fetched();
+            __syncthreads();
+        }
+    };
+    const auto from_start = [&] {
+        fetch2(0);
+        fetched();
+        __syncthreads();
+    };
+    const bool large_tile = groups > 0 && left(flags, 4);
+    if (__builtin_expect(large_tile, 0)) {
+        const bool by_bias = BIAS && large && (shift = row_shift(-pos, most, far, [&](int x) { return bias[far + x]; })) != 0.f;
+        if (large && !by_bias) shift = 0.f;
+        float top = 0.f, sum = 0.f, sum_dp = 0.f;
+#pragma unroll 1
+        for (int pass = 0; pass < 3; ++pass) { // the largest score, the largest relative to shift, the sums
+            from_start();
+            float x = pass < 2 ? -INFINITY : 0.f;
+            over_keys([&](const f32x16_t &s, const f32x16_t &dp) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const float p = exp2_fast(s[e] - top);
+                    x = pass < 2 ? fmaxf(x, s[e]) : x + p;
+                    sum_dp += pass < 2 ? 0.f : p * dp[e];
+                }
+            });
+            const float y = __shfl_xor(x, 32);
+            x = over_waves(pass < 2 ? fmaxf(x, y) : x + y, pass == 2);
+            if (pass == 0 && large && !by_bias && x != -INFINITY) shift = x;
+            if (pass == 1 && large && x != -INFINITY) top = x;
+            sum = x;
+        }
+        sum_dp = over_waves(sum_dp + __shfl_xor(sum_dp, 32));
+        if (large && sum != 0.f) {
+            rest = top + __builtin_amdgcn_logf(sum);
+            sum_dp /= sum;
+        }
+        delta = sum_dp; // (other rows: shift is lse, P is normalised)
+        plainly = true;
+        from_start();
+    }
     // The sums of a near block's dS along its diagonals
     const auto diagonals = [&](int k0, const f32x16_t &ds) {
 #pragma unroll
@@ -192,24 +252,14 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b
     const auto clear_blocks = [&] { // (what no value of a block is written to stays zero)
         for (int x = t; x < DIAG; x += 256) ((f32x4_t *)diag_all)[x] = f32x4_t{};
     };
-    if (few) { // delta = sum P dP
+    if (few && !large_tile) { // delta = sum P dP
         delta = 0.f;
-#pragma unroll 1
-        for (int j = 0; j < groups; ++j) {
-            if (j + 1 < groups) fetch2(j + 1);
-            if (STEP * j + own < mine) {
-                f32x16_t s, dp;
-                form(j, 0.f, s, dp);
+        over_keys([&](const f32x16_t &s, const f32x16_t &dp) {
 #pragma unroll
-                for (int e = 0; e < 16; ++e) delta += exp2_fast(s[e]) * dp[e];
-            }
-            fetched();
-            __syncthreads();
-        }
+            for (int e = 0; e < 16; ++e) delta += exp2_fast(s[e]) * dp[e];
+        });
         delta = over_waves(delta + __shfl_xor(delta, 32));
-        fetch2(0);
-        fetched();
-        __syncthreads();
+        from_start();
     }
     // With the exact delta one pass makes dQ and the diagonals' sums.  (In float O is exact enough, and products of 64 cycles hide
     // no vector work worth the order above: 4 x 333 tokens of 8 heads of 64 took 43 us in two passes, 28 so.)
@@ -226,7 +276,7 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b
                 f32x16_t s, dp;
                 form(j, -delta, s, dp);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) s[e] = exp2_fast(s[e]) * dp[e];
+                for (int e = 0; e < 16; ++e) s[e] = exp2_fast(s[e] - rest) * dp[e];
                 if constexpr (TAB) {
                     if (near_at(k0)) {
                         diagonals(k0, s);
@@ -265,7 +315,7 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b
             const bool near = near_at(k0), plain = !near && k0 + 32 <= n.nk && !(a.causal && k0 + 31 > pmin);
             const float flat = BIAS ? bias[k0 >= pmin ? 2 * far : 0] : 0.f;
             if (now && !plain) finish(s, k0);
-            const float mul = plain ? sl2 : 1.f, add = plain ? flat - lse2 : 0.f;
+            const float mul = plain ? sl2 : 1.f, add = plain ? flat - shift : 0.f;
             const float start = anew(-delta); // (dP is formed on -delta: dS = P (dP - delta))
 #pragma unroll
             for (int e = 0; e < 16; ++e) next[e] = 0.f, dnext[e] = start;
@@ -365,7 +415,18 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b
         before -= off * before_p;
         after -= off * after_p;
     }
-    if (i < a.Lq && h == 0 && kw == 0) *(float2 *)(a.delta + 2 * stat) = make_float2(lse2, ok ? -(delta + kept) : 0.f);
+    if (kw == 0) { // the wave's record, of queries behind the last, too
+        StatRecord *const out = (StatRecord *)a.stat + ((i64)b * a.Hq + head) * a.records + i0 / 32;
+        const bool table = BIAS && groups > 0, with_rest = __any(rest != 0.f);
+        if (h == 0) {
+            out->before[col] = ((table ? bias[0] : 0.f) - shift) - rest;
+            out->after[col] = ((table ? bias[2 * far] : 0.f) - shift) - rest;
+            out->neg_delta[col] = ok ? -(delta + kept) : 0.f;
+            out->shift[col] = shift;
+            out->neg_rest[col] = -rest;
+            if (col == 0) out->with_rest[0] = with_rest ? 1.f : 0.f;
+        }
+    }
     if constexpr (TAB) {
         // the near blocks once more: STEP begin + STEP - 1 > first position - far, STEP (end - 1) < last position + far
         int begin = 0, end = groups;
@@ -473,8 +534,8 @@ __global__ __launch_bounds__((64 * KW * QW), (DP * sizeof(T) <= 128 ? 2 : 1)) vo
     constexpr int CH = DP / 16, DB = DP / 32, AHEAD = DP * sizeof(T) <= 128 ? 3 : sizeof(T) == 2 ? 6 : 3; // (one wave to a unit needs more on the way)
     extern __shared__ __attribute__((aligned(16))) char lds[];
     T *const qb = (T *)lds, *const gb = qb + 3 * Tl::SIZE;
-    float *const stats = (float *)(lds + 6 * Tl::BYTES); // [3][2][ROWS]: lse (base 2) and -delta of each query
-    float *const bias = stats + 3 * 2 * ROWS;
+    StatRecord *const stats = (StatRecord *)(lds + 6 * Tl::BYTES); // [3][QW]
+    float *const bias = (float *)(stats + 3 * QW);
 
     if (blockIdx.x >= z.after) return attn_table(a, z, (int)(blockIdx.x - z.after) * KW * QW + (threadIdx.x >> 6), threadIdx.x & 63);
     const unsigned w = xcd_order(blockIdx.x, z.after);
@@ -514,35 +575,25 @@ __global__ __launch_bounds__((64 * KW * QW), (DP * sizeof(T) <= 128 ? 2 : 1)) vo
     for (int g0 = 0; g0 < a.G && begin < end; ++g0) {
         const int head = kv * a.G + g0;
         const T *const Qp = (const T *)a.Q + b * a.qs[0] + head * a.qs[2], *const Gp = (const T *)a.dO + ((i64)b * a.Lq * a.Hq + head) * a.D;
-        const i64 stat = ((i64)b * a.Hq + head) * a.Lq;
+        const StatRecord *const records = (const StatRecord *)a.stat + ((i64)b * a.Hq + head) * a.records;
         const auto fetch = [&](int x, int slot) {
             ql.fetch(qb + slot * Tl::SIZE, Qp + (i64)(ROWS * x) * a.qs[1], a.qs[1], n.nq - ROWS * x, a.D, wave);
             gl.fetch(gb + slot * Tl::SIZE, Gp + (i64)(ROWS * x) * grow, grow, n.nq - ROWS * x, a.D, wave);
-        };
-        // thread t: lse (t even) or delta of query t / 2 of the group
-        const auto stat_of = [&](int x) {
-            const int left = a.Lq - ROWS * x;
-            const BufSrc src(a.delta + 2 * (stat + ROWS * x), 8 * (left < ROWS ? left : ROWS));
-            return src.load4(t < 2 * ROWS ? 4 * t : BUF_OUT);
-        };
-        const auto put_stat = [&](int x, int slot, float y) { // (behind the last query: lse = infinity, P = 0)
-            if (t < 2 * ROWS) stats[(2 * slot + (t & 1)) * ROWS + t / 2] = !(t & 1) && ROWS * x + t / 2 >= a.Lq ? INFINITY : y;
+            // the group's records, 16 bytes a lane
+            typedef __attribute__((address_space(3))) void *lds_ptr;
+            const BufSrc src(records + QW * x, QW * sizeof(StatRecord));
+            if (16 * t < QW * (int)sizeof(StatRecord))
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(src.r, (lds_ptr)((char *)(stats + QW * slot) + 1024 * wave), 16, 16 * t, 0, 0, 0);
         };
         int slot = (begin + 2) % 3;
         fetch(begin, begin % 3);
-        const float early = stat_of(begin);
         if constexpr (BIAS) fill_bias(a, bias, head, t, THREADS);
-        put_stat(begin, begin % 3, early);
         fetched();
         __syncthreads();
         f32x16_t sA = {}, sB = {}, dpA = {}, dpB = {};
         const auto turn = [&](int x0, f32x16_t &s, f32x16_t &dp, f32x16_t &next, f32x16_t &dnext) {
             const int s1 = slot == 2 ? 0 : slot + 1, s2 = slot == 0 ? 2 : slot - 1;
-            float coming = 0.f;
-            if (x0 + 2 < end) {
-                fetch(x0 + 2, s2);
-                coming = stat_of(x0 + 2);
-            }
+            if (x0 + 2 < end) fetch(x0 + 2, s2);
             const int i0 = ROWS * x0 + r0; // the wave's first query
             const bool now = x0 >= begin && i0 < n.nq && i0 + 31 >= mine, then = x0 + 1 < end && i0 + ROWS < n.nq && i0 + ROWS + 31 >= mine;
             if (now || then) {
@@ -552,14 +603,15 @@ __global__ __launch_bounds__((64 * KW * QW), (DP * sizeof(T) <= 128 ? 2 : 1)) vo
                     const int y = x - 2 * CH;
                     return x < 2 * CH ? Tl::by_rows(lds, x & 1 ? grow_at : qrow, 0, x / 2) : Tl::by_cols(lds, y & 1 ? qcol : gcol, 16 * (y / (2 * DB)), y / 2 % DB);
                 };
-                const float *const st = stats + 2 * slot * ROWS + r0 + 4 * h, *const st1 = stats + (2 * s1 + 1) * ROWS + r0 + 4 * h;
+                const StatRecord &own = stats[QW * slot + wave / KW];
+                const float *const st1 = stats[QW * s1 + wave / KW].neg_delta + 4 * h;
                 const int p0 = i0 + n.start; // the position of the first row
                 const bool edge = j0 + 32 > n.nk || (a.causal && j0 + 31 > p0);
                 const bool near = BIAS && j0 + 31 - p0 > -far && j0 - (p0 + 31) < far;
-                const float flat = BIAS ? bias[j0 >= p0 ? 2 * far : 0] : 0.f;
-                const bool plain = !edge && !near;
-                if (now && !plain) finish_scores<BIAS>(s, sl2, 0.f, bias, far, anew(j - p0 - 4 * h), -1, most);
-                const float mul = plain ? sl2 : 1.f, add = plain ? flat : 0.f;
+                const bool plain = !edge && !near && __builtin_amdgcn_readfirstlane(own.with_rest[0]) == 0;
+                if (now && !plain) finish_scores<BIAS>(s, sl2, own.shift + 4 * h, bias, far, anew(j - p0 - 4 * h), -1, most);
+                // what is added to the products: with a far key its bias, too
+                const float mul = plain ? sl2 : 1.f, *const st = (plain ? j0 >= p0 ? own.after : own.before : own.neg_rest) + 4 * h;
 #pragma unroll
                 for (int e = 0; e < 16; e += 4) { // (dP is formed on -delta: dS = P (dP - delta))
                     const f32x4_t y = *(const f32x4_t *)(st1 + 2 * e);
@@ -581,7 +633,7 @@ __global__ __launch_bounds__((64 * KW * QW), (DP * sizeof(T) <= 128 ? 2 : 1)) vo
                         mma(next, ring[x % (AHEAD + 1)], k[x / 2]);
 #pragma unroll
                     for (int e = x * 16 / (2 * CH); e < (x + 1) * 16 / (2 * CH); ++e) {
-                        p[e] = exp2_fast(s[e] * mul + (add - l4[e % 4]));
+                        p[e] = exp2_fast(s[e] * mul + l4[e % 4]);
                         s[e] = p[e] * dp[e];
                         if (e % 8 == 7) {
                             pack(p, e / 8, fp[e / 8]);
@@ -605,7 +657,6 @@ __global__ __launch_bounds__((64 * KW * QW), (DP * sizeof(T) <= 128 ? 2 : 1)) vo
                     }
                 }
             }
-            if (x0 + 2 < end) put_stat(x0 + 2, s2, coming);
             slot = s1;
             fetched();
             __syncthreads();
@@ -726,7 +777,19 @@ static int attn_bwd_launch(AttnArgs &a, float *dtable, int accumulate, hipStream
     if constexpr (DP * sizeof(T) > 256) return (i64)a.B * a.Hkv * ((a.Lk + 63) / 64) > 256 ? attn_dkv_launch<T, DP, 4, 1>(a, z, s) : attn_dkv_launch<T, DP, 2, 1>(a, z, s);
     return dkv_wide(a, DP * sizeof(T)) ? attn_dkv_launch<T, DP, 4, 1>(a, z, s) : attn_dkv_launch<T, DP, 2, 2>(a, z, s);
 }
-static size_t delta_bytes(const pf_attention_desc *d) { return align_up((size_t)d->B * d->heads_q * d->Lq * 2 * sizeof(float)); }
+// The workspace: records of each head's queries, whole tiles of them; the table's sums
+struct BwdSpace {
+    int records;
+    size_t stat, tab;
+    BwdSpace(const pf_attention_desc *d)
+    {
+        const size_t row = padded(d->head_dim) * (d->dtype == PF_BF16 ? 2 : 4), heads = (size_t)d->B * d->heads_q;
+        const i64 tiles = dq_tiles(d->B, d->heads_q, d->Lq, row);
+        records = (int)(tiles * (128 / dq_sharing(d->B, d->heads_q, d->Lq, row)) / 32);
+        stat = align_up(heads * records * sizeof(StatRecord));
+        tab = align_up(heads * tiles * d->buckets * sizeof(float));
+    }
+};
 
 } // namespace pf
 
@@ -737,8 +800,8 @@ using namespace pf;
 size_t pf_attention_bwd_workspace_bytes(const pf_attention_desc *d)
 {
     if (attn_check(d) != PF_OK || d->B == 0 || d->Lq == 0) return 0;
-    const i64 tiles = dq_tiles(d->B, d->heads_q, d->Lq, padded(d->head_dim) * (d->dtype == PF_BF16 ? 2 : 4));
-    return delta_bytes(d) + align_up((size_t)d->heads_q * d->B * tiles * d->buckets * sizeof(float));
+    const BwdSpace w(d);
+    return w.stat + w.tab;
 }
 
 int pf_attention_bwd(const pf_attention_desc *d, const void *Q, const void *K, const void *V, const void *table, const void *q_start,
@@ -770,8 +833,10 @@ int pf_attention_bwd(const pf_attention_desc *d, const void *Q, const void *K, c
     a.q_start = (const int *)q_start;
     a.q_len = (const int *)q_len;
     a.kv_len = (const int *)kv_len;
-    a.delta = (float *)workspace;
-    a.tab = (float *)((char *)workspace + delta_bytes(d));
+    const BwdSpace w(d);
+    a.records = w.records;
+    a.stat = (float *)workspace;
+    a.tab = (float *)((char *)workspace + w.stat);
     const int DP = (a.D + 31) / 32 * 32;
     float *const dt = d->buckets ? (float *)dtable : nullptr;
     if (d->dtype == PF_BF16)

@@ -71,7 +71,7 @@ __device__ __forceinline__ void attn_fwd_tile(const AttnArgs &a, char *lds, int 
     fetched();
     __syncthreads();
     float shift = 0.f; // what the row's biases, and its maximum, are relative to
-    if (BIAS && keys > 0 && left(large, 4)) shift = row_shift(-pos, most, far, [&](int x) { return bias[far + x]; });
+    if (BIAS && keys > 0 && __builtin_expect(left(large, 4), 0)) shift = row_shift(-pos, most, far, [&](int x) { return bias[far + x]; });
     if (own < mine) {
 #pragma unroll
         for (int u = 0; u < SUB; ++u) {
