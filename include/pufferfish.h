@@ -525,9 +525,10 @@ int pf_qk_norm_rotate_bwd(const pf_qk_norm_desc *d, const void *Q, const void *K
 /*   lse[B, heads_q, Lq] (float, nullable) = log sum exp S.              */
 /*   A query that sees nothing, and a query i >= q_len[b], has O = 0 and */
 /*   lse = -infinity and takes no part in any gradient; what K and V hold */
-/*   from kv_len[b] on, and Q and dO from q_len[b] on, does not matter   */
-/*   (not even NaN).  A key that a causal mask hides from some queries   */
-/*   of a sequence and not from all has to be finite.                    */
+/*   from kv_len[b] on, and Q and dO from q_len[b] on or of queries that */
+/*   stand before the first key (causal), does not matter (not even NaN). */
+/*   A key that a causal mask hides from some queries of a sequence and  */
+/*   not from all has to be finite.                                      */
 /*   q_start, q_len, kv_len: int32[B] on the device, each nullable       */
 /*   (0, Lq, Lk); lengths are taken as within 0 .. Lq and 0 .. Lk,       */
 /*   q_start as within -2^30 .. 2^30.                                    */

@@ -171,16 +171,18 @@ struct Tile {
         }
     }
     // ROWS rows from `first` on (the same for all threads), zeros from row `rows` on: the descriptor ends with the last row.
-    // wave: the thread's wave among those of THREADS.
-    __device__ __forceinline__ void fetch(T *lds, const T *first, i64 stride, int rows, int D, int wave) const
+    // wave: the thread's wave among those of THREADS.  The first `skip` rows are zeros: the descriptor begins behind them.
+    __device__ __forceinline__ void fetch(T *lds, const T *first, i64 stride, int rows, int D, int wave, int skip = 0) const
     {
         typedef __attribute__((address_space(3))) void *lds_ptr;
         const int n = rows < ROWS ? rows : ROWS;
-        const BufSrc src(first, n > 0 ? ((n - 1) * (int)stride + D) * (int)sizeof(T) : 0);
+        const BufSrc src(first + skip * stride, n > skip ? ((n - 1 - skip) * (int)stride + D) * (int)sizeof(T) : 0);
+        const uint32_t gone = skip * (uint32_t)stride * (uint32_t)sizeof(T); // (what is out of range stays so: both are below 2^30)
+        const auto offset = [&](uint32_t x) { return x < gone ? BUF_OUT : x - gone; };
 #pragma unroll
         for (int i = 0; i < N; ++i)
             if (PIECES % THREADS == 0 || i * THREADS + wave * 64 < PIECES)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(src.r, (lds_ptr)((char *)lds + (i * THREADS + wave * 64) * 16), 16, (int)at[i], 0, 0, 0);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(src.r, (lds_ptr)((char *)lds + (i * THREADS + wave * 64) * 16), 16, (int)offset(at[i]), 0, 0, 0);
     }
     // Where a lane reads, in bytes from the tile's start.  turn() permutes bits, so that a step along a row is an exclusive or of
     // the place (tiles lie at multiples of their rows' lengths): one number for a lane and constants, not an address for every read.

@@ -130,6 +130,12 @@ __device__ __forceinline__ void attn_dq_tile(const AttnArgs &a, char *lds, int b
         const float x = a.lse_in[stat];
         if (x != -INFINITY) lse2 = x * LOG2E;
     }
+    // A query that sees nothing takes no part, whatever its dO holds
+    if (lse2 == INFINITY) {
+        delta = kept = 0.f;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) g[c] = {};
+    }
     __shared__ int flags[4];
     const bool large = fabsf(lse2) >= ATTN_LARGE && lse2 != INFINITY;
     leave(flags, large, wave, lane);
@@ -564,9 +570,10 @@ __global__ __launch_bounds__((64 * KW * QW), (DP * sizeof(T) <= 128 ? 2 : 1)) vo
     const Tl ql(a.qs[1], a.D, t), gl(grow, a.D, t);
     const int rows = Tl::row_place(lane) + r0 * Tl::RB, cols = Tl::col_place(lane) + r0 * Tl::RB; // (turn() repeats after 16 rows)
     // the groups of queries that see a key of the workgroup; the first query that sees one of the wave
-    int begin = 0, mine = 0;
+    int begin = 0, mine = 0, hidden = 0; // the first `hidden` queries see nothing: they are not read (0 times NaN is not 0)
     const int end = (n.nq + ROWS - 1) / ROWS;
     if (a.causal) {
+        hidden = clamped(-n.start, 0, n.nq);
         begin = clamped(tile * KEYS - n.start, 0, a.Lq) / ROWS;
         mine = clamped(j0 - n.start, 0, a.Lq);
     }
@@ -576,9 +583,9 @@ __global__ __launch_bounds__((64 * KW * QW), (DP * sizeof(T) <= 128 ? 2 : 1)) vo
         const int head = kv * a.G + g0;
         const T *const Qp = (const T *)a.Q + b * a.qs[0] + head * a.qs[2], *const Gp = (const T *)a.dO + ((i64)b * a.Lq * a.Hq + head) * a.D;
         const StatRecord *const records = (const StatRecord *)a.stat + ((i64)b * a.Hq + head) * a.records;
-        const auto fetch = [&](int x, int slot) {
-            ql.fetch(qb + slot * Tl::SIZE, Qp + (i64)(ROWS * x) * a.qs[1], a.qs[1], n.nq - ROWS * x, a.D, wave);
-            gl.fetch(gb + slot * Tl::SIZE, Gp + (i64)(ROWS * x) * grow, grow, n.nq - ROWS * x, a.D, wave);
+        const auto fetch = [&](int x, int slot, int skip) {
+            ql.fetch(qb + slot * Tl::SIZE, Qp + (i64)(ROWS * x) * a.qs[1], a.qs[1], n.nq - ROWS * x, a.D, wave, skip);
+            gl.fetch(gb + slot * Tl::SIZE, Gp + (i64)(ROWS * x) * grow, grow, n.nq - ROWS * x, a.D, wave, skip);
             // the group's records, 16 bytes a lane
             typedef __attribute__((address_space(3))) void *lds_ptr;
             const BufSrc src(records + QW * x, QW * sizeof(StatRecord));
@@ -586,14 +593,14 @@ __global__ __launch_bounds__((64 * KW * QW), (DP * sizeof(T) <= 128 ? 2 : 1)) vo
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(src.r, (lds_ptr)((char *)(stats + QW * slot) + 1024 * wave), 16, 16 * t, 0, 0, 0);
         };
         int slot = (begin + 2) % 3;
-        fetch(begin, begin % 3);
+        fetch(begin, begin % 3, hidden > ROWS * begin ? hidden - ROWS * begin : 0);
         if constexpr (BIAS) fill_bias(a, bias, head, t, THREADS);
         fetched();
         __syncthreads();
         f32x16_t sA = {}, sB = {}, dpA = {}, dpB = {};
         const auto turn = [&](int x0, f32x16_t &s, f32x16_t &dp, f32x16_t &next, f32x16_t &dnext) {
             const int s1 = slot == 2 ? 0 : slot + 1, s2 = slot == 0 ? 2 : slot - 1;
-            if (x0 + 2 < end) fetch(x0 + 2, s2);
+            if (x0 + 2 < end) fetch(x0 + 2, s2, 0);
             const int i0 = ROWS * x0 + r0; // the wave's first query
             const bool now = x0 >= begin && i0 < n.nq && i0 + 31 >= mine, then = x0 + 1 < end && i0 + ROWS < n.nq && i0 + ROWS + 31 >= mine;
             if (now || then) {
