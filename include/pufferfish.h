@@ -503,7 +503,8 @@ int pf_qk_norm_rotate_fwd(const pf_qk_norm_desc *d, const void *Q, const void *K
 
 /* From dQo = dL/dQo, dKo = dL/dKo and the forward call's inputs: dQ, dK, and
  * dgamma_q, dgamma_k (float[head_dim], each nullable; overwritten or
- * accumulated; untouched with PF_NORM_NONE).  The same call gives the same
+ * accumulated; untouched with PF_NORM_NONE; at one address for both, for a
+ * gamma that queries and keys share: their sum).  The same call gives the same
  * bits each time.  With PF_NORM_NONE Q and K are not read (nullable). */
 size_t pf_qk_norm_rotate_bwd_workspace_bytes(const pf_qk_norm_desc *d);
 int pf_qk_norm_rotate_bwd(const pf_qk_norm_desc *d, const void *Q, const void *K,

@@ -411,7 +411,7 @@ def pf_qk_norm_rotate_fwd(Q, K, gamma_q=None, gamma_k=None, positions=None, norm
 def pf_qk_norm_rotate_bwd(Q, K, dQo, dKo, gamma_q=None, gamma_k=None, positions=None, norm="rms", eps=1e-6, rot_dim=None,
                           theta=10000.0, style="halves", grads=None, out=None):
     """From the gradients of pf_qk_norm_rotate_fwd's outputs: (dQ, dK, dgamma_q, dgamma_k), the latter float32 [D] (None
-    without that gamma), accumulated into `grads` = (dgamma_q, dgamma_k) when given.  out = (dQ, dK): where to write them."""
+    without that gamma), accumulated into `grads` = (dgamma_q, dgamma_k) when given (one tensor for both: their sum).  out = (dQ, dK): where to write them."""
     return _native.qk_bwd(Q, K, dQo, dKo, gamma_q, gamma_k, positions, _NORM[norm], eps, rot_dim, theta, _ROT[style], grads,
                           out)
 

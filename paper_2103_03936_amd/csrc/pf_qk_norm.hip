@@ -264,22 +264,27 @@ __global__ __launch_bounds__(256, 4) void qk_norm_kernel(QkArgs a, int log)
 }
 
 // The workgroups' sums to dgamma: one workgroup per value, in double and always in one order.  Bound by latency: a lane's loads
-// are on their way together (one wave that loaded one by one took 6.7 us for 1024 workgroups, this 3.9)
+// are on their way together (one wave that loaded one by one took 6.7 us for 1024 workgroups, this 3.9).  Where queries and keys
+// share their gamma (dq == dk) a value is the sum of both, in one workgroup.
 __global__ __launch_bounds__(256) void qk_gamma_kernel(const float *partial, int blocks, int D, float *dq, float *dk, int accumulate)
 {
-    __shared__ double part[4];
-    const int i = blockIdx.x, t = threadIdx.x;
-    float x[4];
+    __shared__ double part[2][4];
+    const int t = threadIdx.x, values = dq == dk ? 2 : 1, j = blockIdx.x < D ? blockIdx.x : blockIdx.x - D;
+    for (int v = 0; v < values; ++v) {
+        const int i = blockIdx.x + v * D;
+        float x[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) x[k] = t + 256 * k < blocks ? partial[(i64)(t + 256 * k) * 2 * D + i] : 0.f;
-    double s = ((double)x[0] + (double)x[1]) + ((double)x[2] + (double)x[3]);
-    for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o);
-    if ((t & 63) == 0) part[t >> 6] = s;
+        for (int k = 0; k < 4; ++k) x[k] = t + 256 * k < blocks ? partial[(i64)(t + 256 * k) * 2 * D + i] : 0.f;
+        double s = ((double)x[0] + (double)x[1]) + ((double)x[2] + (double)x[3]);
+        for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o);
+        if ((t & 63) == 0) part[v][t >> 6] = s;
+    }
     __syncthreads();
-    s = (part[0] + part[1]) + (part[2] + part[3]);
-    float *out = i < D ? dq : dk;
-    const int j = i < D ? i : i - D;
-    if (t == 0 && out) out[j] = accumulate ? out[j] + (float)s : (float)s;
+    float *const out = blockIdx.x < D ? dq : dk;
+    if (t || !out) return;
+    double s = (part[0][0] + part[0][1]) + (part[0][2] + part[0][3]);
+    if (values == 2) s += (part[1][0] + part[1][1]) + (part[1][2] + part[1][3]);
+    out[j] = accumulate ? out[j] + (float)s : (float)s;
 }
 
 // ------------------------------------------------------------------ host
@@ -435,9 +440,10 @@ int pf_qk_norm_rotate_bwd(const pf_qk_norm_desc *d, const void *Q, const void *K
     a.partial = sums ? (float *)workspace : nullptr;
     const int blocks = qk_blocks(d, true);
     st = qk_launch<true>(a, d->dtype, d->rotation == PF_ROT_PAIRS, blocks, (hipStream_t)stream);
+    float *const dgq = (float *)dgamma_q, *const dgk = d->heads_k ? (float *)dgamma_k : nullptr;
     if (sums)
-        PF_LAUNCH(st, "qk_gamma", qk_gamma_kernel, dim3(2 * d->head_dim), dim3(256), (hipStream_t)stream, a.partial, blocks, d->head_dim,
-                  (float *)dgamma_q, d->heads_k ? (float *)dgamma_k : nullptr, accumulate);
+        PF_LAUNCH(st, "qk_gamma", qk_gamma_kernel, dim3((dgq == dgk ? 1 : 2) * d->head_dim), dim3(256), (hipStream_t)stream, a.partial, blocks,
+                  d->head_dim, dgq, dgk, accumulate);
     return st;
 }
 
