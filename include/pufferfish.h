@@ -476,7 +476,9 @@ int pf_lowrank_lstm_stack_bwd(const pf_lstm_stack_desc *d, const void *x,
 /* heads_k == 0: no keys, K and all that belongs to it are not touched.  */
 /* head_dim: a multiple of 8, 8 .. 256; rot_dim: a multiple of 4,        */
 /* 0 .. head_dim; B L heads < 2^30 (PF_ERR_UNSUPPORTED otherwise).       */
-/* Outputs may be the inputs themselves (same strides).                  */
+/* An output may be the input it belongs to (Qo: Q, dQ: Q or dQo, ..), at */
+/* the same strides; other overlaps of outputs with inputs or each other  */
+/* are refused (PF_ERR_UNSUPPORTED).                                      */
 /* ------------------------------------------------------------------ */
 typedef enum { PF_NORM_NONE = 0, PF_NORM_RMS = 1 } pf_norm;
 typedef enum { PF_ROT_HALVES = 0, PF_ROT_PAIRS = 1 } pf_rotation;
@@ -547,8 +549,8 @@ int pf_qk_norm_rotate_bwd(const pf_qk_norm_desc *d, const void *Q, const void *K
 /* buckets 0 or 2 .. 256, with bidirectional a multiple of 2 and >= 4;    */
 /* max_distance > e and <= 1024; Lq, Lk < 2^29; fewer than 2^31 blocks of  */
 /* 32 rows; less than 2^22 elements from one token to the next.           */
-/* Lq == 0 or Lk == 0 is legal.  Outputs must not overlap inputs or each  */
-/* other (PF_ERR_UNSUPPORTED where they begin at one address).            */
+/* Lq == 0 or Lk == 0 is legal.  Outputs that overlap Q, K, V, O, dO, lse, */
+/* the table or each other are refused (PF_ERR_UNSUPPORTED).              */
 /* Sums are the same bits in every call of the same sizes.                */
 /* ------------------------------------------------------------------ */
 typedef struct {

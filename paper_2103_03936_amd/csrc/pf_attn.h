@@ -9,9 +9,8 @@
 // with the transposing reads).  For dK and dV the scores are formed with rows: queries, columns: keys, and the same holds.
 #pragma once
 
-#include <initializer_list>
-
 #include "pf_attn_bias.h"
+#include "pf_overlap.h"
 #include "pf_tile.h"
 
 namespace pf {
@@ -359,18 +358,18 @@ int attn_split_fwd(const pf_attention_desc *d, AttnArgs &a, void *workspace, hip
 int attn_split_count(const pf_attention_desc *d); // 0: the ordinary kernel
 size_t attn_split_bytes(const pf_attention_desc *d);
 int attn_check(const pf_attention_desc *d);
-// An output that begins where an input or another output does (partial overlaps are the caller's to avoid)
-inline bool attn_same(std::initializer_list<const void *> outputs, std::initializer_list<const void *> inputs)
-{
-    for (auto o = outputs.begin(); o != outputs.end(); ++o) {
-        if (!*o) continue;
-        for (auto x = outputs.begin(); x != o; ++x)
-            if (*x == *o) return true;
-        for (const void *x : inputs)
-            if (x == *o) return true;
-    }
-    return false;
-}
 void attn_fill(const pf_attention_desc *d, AttnArgs &a);
+// What the tensors of a call take in memory
+struct AttnAreas {
+    const pf_attention_desc *d;
+    const AttnArgs &a;
+    int64_t elem() const { return d->dtype == PF_BF16 ? 2 : 4; }
+    Area queries(const void *p) const { return Area(p, d->B, a.Lq, a.Hq, a.qs, a.D, elem()); }
+    Area keys(const void *p, const i64 (&s)[3]) const { return Area(p, d->B, a.Lk, a.Hkv, s, a.D, elem()); }
+    Area dense_queries(const void *p) const { return Area(p, d->B * d->Lq * a.Hq * a.D * elem()); }
+    Area dense_keys(const void *p) const { return Area(p, d->B * d->Lk * a.Hkv * a.D * elem()); }
+    Area rows(const void *p) const { return Area(p, d->B * d->Lq * a.Hq * 4); }
+    Area table(const void *p) const { return Area(a.buckets ? p : nullptr, (int64_t)a.buckets * a.Hq * 4); }
+};
 
 } // namespace pf

@@ -831,9 +831,12 @@ int pf_attention_bwd(const pf_attention_desc *d, const void *Q, const void *K, c
     if (any_misaligned({workspace}, 256)) return PF_ERR_UNSUPPORTED;
     const size_t need = pf_attention_bwd_workspace_bytes(d);
     if (need && (!workspace || workspace_bytes < need)) return PF_ERR_WORKSPACE;
-    if (attn_same({dQ, dK, dV}, {Q, K, V, O, dO})) return PF_ERR_UNSUPPORTED;
     AttnArgs a = {};
     attn_fill(d, a);
+    const AttnAreas of{d, a};
+    if (outputs_meet({of.dense_queries(dQ), of.dense_keys(dK), of.dense_keys(dV), of.table(dtable)},
+                     {of.queries(Q), of.keys(K, a.ks), of.keys(V, a.vs), of.dense_queries(O), of.dense_queries(dO), of.rows(lse), of.table(table)}))
+        return PF_ERR_UNSUPPORTED;
     a.Q = Q, a.K = K, a.V = V, a.Oin = O, a.dO = dO, a.dQ = dQ, a.dK = dK, a.dV = dV;
     a.table = (const float *)table;
     a.lse_in = (const float *)lse;

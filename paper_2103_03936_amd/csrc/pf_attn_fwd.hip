@@ -331,9 +331,10 @@ int pf_attention_fwd(const pf_attention_desc *d, const void *Q, const void *K, c
         return PF_ERR_UNSUPPORTED;
     const size_t need = attn_split_bytes(d);
     if (need && (!workspace || workspace_bytes < need)) return PF_ERR_WORKSPACE;
-    if (attn_same({O}, {Q, K, V})) return PF_ERR_UNSUPPORTED;
     AttnArgs a = {};
     attn_fill(d, a);
+    const AttnAreas of{d, a};
+    if (outputs_meet({of.dense_queries(O), of.rows(lse)}, {of.queries(Q), of.keys(K, a.ks), of.keys(V, a.vs), of.table(table)})) return PF_ERR_UNSUPPORTED;
     a.Q = Q, a.K = K, a.V = V, a.O = O;
     a.table = (const float *)table;
     a.lse = (float *)lse;

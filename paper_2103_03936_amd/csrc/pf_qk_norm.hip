@@ -10,6 +10,7 @@
 #include <string.h>
 
 #include "pf_gemm.h"
+#include "pf_overlap.h"
 
 namespace pf {
 
@@ -376,6 +377,14 @@ static int qk_launch(const QkArgs &a, int dtype, bool pairs, int blocks, hipStre
     return qk_launch_w<float, 2, BWD>(a, pairs, blocks, s);
 }
 
+// The queries' or keys' outputs of one direction: an output may be one of its own inputs, element for element
+static bool meets_other(const Area &out, std::initializer_list<Area> own, std::initializer_list<Area> others)
+{
+    for (const Area &x : own)
+        if (!x.same(out) && meet(x, out)) return true;
+    return outputs_meet({out}, others);
+}
+
 } // namespace pf
 
 extern "C" {
@@ -398,6 +407,11 @@ int pf_qk_norm_rotate_fwd(const pf_qk_norm_desc *d, const void *Q, const void *K
     a.gamma[1] = (const float *)gamma_k;
     a.positions = (const int *)(positions ? positions : Qo);
     a.given = positions != nullptr;
+    const auto area = [&](const void *p, int k, const i64 (&s)[3]) {
+        return Area(p, d->B, d->L, a.heads[k], s, a.D, d->dtype == PF_BF16 ? 2 : 4);
+    };
+    const Area q = area(Q, 0, a.in[0]), k = area(K, 1, a.in[1]), qo = area(Qo, 0, a.out[0]), ko = area(Ko, 1, a.out[1]);
+    if (meets_other(qo, {q}, {k, ko}) || meets_other(ko, {k}, {q})) return PF_ERR_UNSUPPORTED;
     return qk_launch<false>(a, d->dtype, d->rotation == PF_ROT_PAIRS, qk_blocks(d, false), (hipStream_t)stream);
 }
 
@@ -437,6 +451,14 @@ int pf_qk_norm_rotate_bwd(const pf_qk_norm_desc *d, const void *Q, const void *K
         a.Q = dQo, a.K = dKo;
         memcpy(a.in, a.out, sizeof a.in);
     }
+    const auto area = [&](const void *p, int k, const i64 (&s)[3]) {
+        return Area(p, d->B, d->L, a.heads[k], s, a.D, d->dtype == PF_BF16 ? 2 : 4);
+    };
+    const Area q = area(a.Q, 0, a.in[0]), k = area(a.K, 1, a.in[1]), dqo = area(dQo, 0, a.out[0]), dko = area(dKo, 1, a.out[1]),
+               dq = area(dQ, 0, a.din[0]), dk = area(dK, 1, a.din[1]), gq(sums ? dgamma_q : nullptr, d->head_dim * 4),
+               gk(sums && d->heads_k ? dgamma_k : nullptr, d->head_dim * 4);
+    if (meets_other(dq, {q, dqo}, {k, dko, dk}) || meets_other(dk, {k, dko}, {q, dqo})) return PF_ERR_UNSUPPORTED;
+    if (meets_other(gq, {gk}, {q, k, dqo, dko, dq, dk}) || meets_other(gk, {gq}, {q, k, dqo, dko, dq, dk})) return PF_ERR_UNSUPPORTED;
     a.partial = sums ? (float *)workspace : nullptr;
     const int blocks = qk_blocks(d, true);
     st = qk_launch<true>(a, d->dtype, d->rotation == PF_ROT_PAIRS, blocks, (hipStream_t)stream);
