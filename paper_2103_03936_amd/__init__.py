@@ -500,8 +500,15 @@ class AdamW:
     zeros.  `steps` (int64, one element, device) counts the steps done, `lr` (float32 [1], device) is read by each step:
     `opt.lr.fill_(x)` changes it, also between replays of a captured step.
 
-    The addresses are noted once: the tensors are updated in place and must not be replaced.  Steps of one AdamW follow
-    one another: do not let two streams run them at once."""
+    The addresses are noted once: the tensors are updated in place, and assigning to what the optimizer was made with
+    (`opt.lr = x`, `opt.betas = ..`) raises AttributeError.  Steps of one AdamW follow one another: do not let two streams
+    run them at once."""
+
+    def __setattr__(self, name, value):
+        if "_args" in self.__dict__ and name in self.__dict__:
+            raise AttributeError(f"{name} is noted when the optimizer is made; " + (f"write into it: {name}.fill_(x)" if name in ("lr", "steps")
+                                 else "make a new one, with state= and steps= of this one"))
+        object.__setattr__(self, name, value)
 
     def __init__(self, params, grads, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, copies=None, state_bits=32,
                  state=None, steps=None):
