@@ -547,8 +547,9 @@ int pf_qk_norm_rotate_bwd(const pf_qk_norm_desc *d, const void *Q, const void *K
 /* costs its scores no digits (finite ones beyond 2.3e38 count as that).  */
 /* Limits (PF_ERR_UNSUPPORTED): head_dim a multiple of 8, 8 .. 128;       */
 /* buckets 0 or 2 .. 256, with bidirectional a multiple of 2 and >= 4;    */
-/* max_distance > e and <= 1024; Lq, Lk < 2^29; fewer than 2^31 blocks of  */
-/* 32 rows; less than 2^22 elements from one token to the next.           */
+/* max_distance > e and <= 1024; Lq, Lk < 2^29; launches of fewer than    */
+/* 2^32 threads (about 2^24 tiles of 128 queries of a head, or of 64 keys  */
+/* of a key head); less than 2^22 elements from one token to the next.    */
 /* Lq == 0 or Lk == 0 is legal.  Outputs that overlap Q, K, V, O, dO, lse, */
 /* the table or each other are refused (PF_ERR_UNSUPPORTED).              */
 /* Sums are the same bits in every call of the same sizes.                */

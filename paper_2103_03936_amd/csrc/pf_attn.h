@@ -358,6 +358,8 @@ int attn_split_fwd(const pf_attention_desc *d, AttnArgs &a, void *workspace, hip
 int attn_split_count(const pf_attention_desc *d); // 0: the ordinary kernel
 size_t attn_split_bytes(const pf_attention_desc *d);
 int attn_check(const pf_attention_desc *d);
+// A launch of 2^32 threads or more does not exist
+inline bool too_many(i64 blocks, int threads) { return blocks * threads >= (i64)1 << 32; }
 void attn_fill(const pf_attention_desc *d, AttnArgs &a);
 // What the tensors of a call take in memory
 struct AttnAreas {

@@ -717,6 +717,7 @@ static int attn_dq_launch(AttnArgs &a, bool tab, hipStream_t s)
     a.tiles = (a.Lq + 128 / KW - 1) / (128 / KW);
     const int paired = a.causal && (i64)a.B * a.Hq * a.tiles > 512; // (two workgroups to a compute unit are resident)
     const dim3 grid((unsigned)a.B * a.Hq * (paired ? (a.tiles + 1) / 2 : a.tiles));
+    if (too_many(grid.x, 256)) return PF_ERR_UNSUPPORTED;
     const size_t lds = DqLds<T, DP, KW>::bytes(a.bk.far, a.buckets, tab);
     if (a.Lq == 0) return st;
     if (tab)
@@ -762,13 +763,17 @@ static int attn_dkv_launch(AttnArgs &a, TableSum z, hipStream_t s)
 // dO are read half as often); 64 shared by two waves each where it does not, and with a causal mask, whose first keys have
 // the most queries.  us, bf16: 64 x 128 tokens of 8 heads of 64, 512 tiles of 128, 19 and 24 with tiles of 64; 6 x 1024, 384 tiles,
 // 54 and 51; 4 x 1024 with heads of 128, 256 tiles (one to a compute unit), 61 and 68; 2 x 4096 causal, 256 tiles, 675 and 408.
-static bool dkv_wide(const AttnArgs &a, size_t row)
+// (Six tiles of rows of more than 256 bytes leave no room for two waves' queries, nor for a second workgroup: four waves where
+// there are more tiles of 64 keys than compute units.  16 x 512 tokens of 8 heads of 128: 320 us, with two waves 591)
+static int dkv_keys(const pf_attention_desc *d, size_t row)
 {
-    return (!a.causal || a.Lk <= 128) && (i64)a.B * a.Hkv * ((a.Lk + 127) / 128) >= (row <= 128 ? 512 : 256);
+    const i64 heads = d->B * d->heads_kv;
+    if (row > 256) return heads * ((d->Lk + 63) / 64) > 256 ? 128 : 64;
+    return (!d->causal || d->Lk <= 128) && heads * ((d->Lk + 127) / 128) >= (row <= 128 ? 512 : 256) ? 128 : 64;
 }
 
 template <typename T, int DP>
-static int attn_bwd_launch(AttnArgs &a, float *dtable, int accumulate, hipStream_t s)
+static int attn_bwd_launch(AttnArgs &a, int keys, float *dtable, int accumulate, hipStream_t s)
 {
     const bool bias = a.buckets > 0, tab = bias && dtable;
     int st;
@@ -779,10 +784,7 @@ static int attn_bwd_launch(AttnArgs &a, float *dtable, int accumulate, hipStream
     const int parts = a.B * a.tiles;
     if (st != PF_OK) return st;
     const TableSum z = {tab ? dtable : nullptr, parts, accumulate, 0};
-    // (Six tiles of more than 256 bytes a row leave no room for two waves' queries, nor for a second workgroup: four waves where
-    // there are more tiles of 64 keys than compute units.  16 x 512 tokens of 8 heads of 128: 320 us, with two waves 591)
-    if constexpr (DP * sizeof(T) > 256) return (i64)a.B * a.Hkv * ((a.Lk + 63) / 64) > 256 ? attn_dkv_launch<T, DP, 4, 1>(a, z, s) : attn_dkv_launch<T, DP, 2, 1>(a, z, s);
-    return dkv_wide(a, DP * sizeof(T)) ? attn_dkv_launch<T, DP, 4, 1>(a, z, s) : attn_dkv_launch<T, DP, 2, 2>(a, z, s);
+    return keys == 128 ? attn_dkv_launch<T, DP, 4, 1>(a, z, s) : attn_dkv_launch<T, DP, 2, (DP * sizeof(T) > 256 ? 1 : 2)>(a, z, s);
 }
 // The workspace: records of each head's queries, whole tiles of them; the table's sums
 struct BwdSpace {
@@ -831,6 +833,9 @@ int pf_attention_bwd(const pf_attention_desc *d, const void *Q, const void *K, c
     if (any_misaligned({workspace}, 256)) return PF_ERR_UNSUPPORTED;
     const size_t need = pf_attention_bwd_workspace_bytes(d);
     if (need && (!workspace || workspace_bytes < need)) return PF_ERR_WORKSPACE;
+    // (the second launch, and the workgroups in it that sum up the table; the first one refuses by itself)
+    const int keys = dkv_keys(d, padded(d->head_dim) * (d->dtype == PF_BF16 ? 2 : 4));
+    if (too_many(d->B * d->heads_kv * ((d->Lk + keys - 1) / keys) + (i64)d->buckets * d->heads_q, 256)) return PF_ERR_UNSUPPORTED;
     AttnArgs a = {};
     attn_fill(d, a);
     const AttnAreas of{d, a};
@@ -850,10 +855,10 @@ int pf_attention_bwd(const pf_attention_desc *d, const void *Q, const void *K, c
     const int DP = (a.D + 31) / 32 * 32;
     float *const dt = d->buckets ? (float *)dtable : nullptr;
     if (d->dtype == PF_BF16)
-        return DP == 32 ? attn_bwd_launch<bf16_t, 32>(a, dt, accumulate, s) : DP == 64 ? attn_bwd_launch<bf16_t, 64>(a, dt, accumulate, s)
-             : DP == 96 ? attn_bwd_launch<bf16_t, 96>(a, dt, accumulate, s) : attn_bwd_launch<bf16_t, 128>(a, dt, accumulate, s);
-    return DP == 32 ? attn_bwd_launch<float, 32>(a, dt, accumulate, s) : DP == 64 ? attn_bwd_launch<float, 64>(a, dt, accumulate, s)
-         : DP == 96 ? attn_bwd_launch<float, 96>(a, dt, accumulate, s) : attn_bwd_launch<float, 128>(a, dt, accumulate, s);
+        return DP == 32 ? attn_bwd_launch<bf16_t, 32>(a, keys, dt, accumulate, s) : DP == 64 ? attn_bwd_launch<bf16_t, 64>(a, keys, dt, accumulate, s)
+             : DP == 96 ? attn_bwd_launch<bf16_t, 96>(a, keys, dt, accumulate, s) : attn_bwd_launch<bf16_t, 128>(a, keys, dt, accumulate, s);
+    return DP == 32 ? attn_bwd_launch<float, 32>(a, keys, dt, accumulate, s) : DP == 64 ? attn_bwd_launch<float, 64>(a, keys, dt, accumulate, s)
+         : DP == 96 ? attn_bwd_launch<float, 96>(a, keys, dt, accumulate, s) : attn_bwd_launch<float, 128>(a, keys, dt, accumulate, s);
 }
 
 } // extern "C"

@@ -289,6 +289,7 @@ static int attn_fwd_launch(AttnArgs &a, hipStream_t s)
     // two workgroups to a compute unit are resident: causal tiles are paired where there are more
     const bool paired = a.causal && (i64)a.B * a.Hq * a.tiles > 512;
     const unsigned blocks = (unsigned)a.B * a.Hq * (paired ? (a.tiles + 1) / 2 : a.tiles);
+    if (too_many(blocks, 256)) return PF_ERR_UNSUPPORTED;
     const size_t lds = 4 * Tl::BYTES + (a.buckets ? (2 * a.bk.far + 1) * sizeof(float) : 0);
     int st = PF_OK;
     if (a.buckets)

@@ -320,6 +320,7 @@ template <typename T, int DP>
 static int attn_split_launch(const AttnArgs &a, hipStream_t s)
 {
     const unsigned blocks = (unsigned)a.B * a.Hkv * a.tiles * a.splits;
+    if (too_many(blocks, 64 * SPLIT_WAVES)) return PF_ERR_UNSUPPORTED;
     const size_t lds = split_lds(SplitLds<T, DP>::AREA, a.buckets, a.tile_heads, a.bk.far);
     int st = PF_OK;
     if (a.buckets)
