@@ -144,8 +144,10 @@ __device__ inline bf16x4_t read_turned(const LdsBf16x4 *__restrict__ p) { return
 // rows) and by columns (the transposing reads: 32 lanes that a cycle serves have four adjacent pieces of four rows; float:
 // 32 adjacent values of two rows, four apart), and turn() lets each way meet each of the 64 banks once (float of 32
 // columns: twice).
+constexpr int ATTN_MAX_STRIDE = 1 << 22; // elements from one token to the next
 template <typename T, int DP, int ROWS, int THREADS>
 struct Tile {
+    static_assert((int64_t)ROWS * ATTN_MAX_STRIDE * sizeof(T) <= 1 << 30, "offsets of 31 bits, what is skipped included"); // 128 rows of bf16, 64 of float
     static constexpr int VEC = 16 / sizeof(T), PITCH = DP == 96 ? 128 : DP, CHUNKS = PITCH / VEC, PIECES = ROWS * CHUNKS, N = (PIECES + THREADS - 1) / THREADS;
     static constexpr int BYTES = PIECES * 16, SIZE = ROWS * PITCH;
     static_assert(PIECES % 64 == 0, "whole waves of pieces");

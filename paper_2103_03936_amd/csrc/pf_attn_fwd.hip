@@ -253,8 +253,8 @@ int attn_check(const pf_attention_desc *d)
     }
     const int unit = 16 / (d->dtype == PF_BF16 ? 2 : 4);
     if (!strides_ok(d->q_stride, unit) || !strides_ok(d->k_stride, unit) || !strides_ok(d->v_stride, unit)) return PF_ERR_UNSUPPORTED;
-    // a tile of 64 tokens is read through one descriptor, with offsets of 31 bits
-    const i64 q = (i64)d->heads_q * d->head_dim, k = (i64)d->heads_kv * d->head_dim, most = (1 << 22) - d->head_dim;
+    // a tile of tokens is read through one descriptor, with offsets of 31 bits
+    const i64 q = (i64)d->heads_q * d->head_dim, k = (i64)d->heads_kv * d->head_dim, most = ATTN_MAX_STRIDE - d->head_dim;
     if (q > most || k > most || d->q_stride[1] > most || d->k_stride[1] > most || d->v_stride[1] > most) return PF_ERR_UNSUPPORTED;
     return PF_OK;
 }
