@@ -6,8 +6,8 @@
 // and dP each (seven products where one kernel with atomic sums of dQ would have five).
 //
 // 2 x 4096 tokens of 16 heads of 128, causal: dQ with the table 268 us (matrix unit busy 38 %; vector work beside the products),
-// dK and dV 408 (28 %; accumulators and operands fill the registers, so that a unit has one wave and little overlaps).  64 x 128 padded
-// tokens of 8 heads of 64: 23 and 17.5, launch and latency of one to four tiles.
+// dK and dV 398 (29 %; accumulators and operands fill the registers, so that a unit has one wave and little overlaps).  64 x 128 padded
+// tokens of 8 heads of 64: 23 and 17, launch and latency of one to four tiles.
 //
 // delta = sum P dP of a row is sum O dO, too, but O is rounded to bf16 there and P was before O was formed: dS is off by about
 // 2^-9 of delta then.  For queries that see many keys that is below what rounding dS itself costs dQ and dK; where some see few,

@@ -5,7 +5,7 @@
 // share their queries, each with half of the keys of a tile.  One pass over the keys with the running maximum and
 // sum of each query; the score matrix, the bias and P exist in registers only.
 //
-// Bound by the vector work of a tile beside its products: 2 x 4096 tokens of 16 heads of 128, causal, take 158 us, with the matrix unit
+// Bound by the vector work of a tile beside its products: 2 x 4096 tokens of 16 heads of 128, causal, take 155 us, with the matrix unit
 // busy 45 % of the time.  64 x 128 padded tokens of 8 heads of 64 take 12: launch, first loads and one or two tiles.
 #include "pf_attn.h"
 
@@ -300,7 +300,9 @@ static int attn_fwd_launch(AttnArgs &a, hipStream_t s)
 }
 // Two waves share queries where that makes no more workgroups than fit the card at once, two to a compute unit if the tiles of
 // both fit its LDS (us, bf16, 8 heads: 2 x 1024 tokens of 64 columns, 128 tiles, 25 alone and 18 shared; 4 x 1024, 256 tiles,
-// 26 and 23; 6 x 1024 34 and 33; 512 queries of 32 heads of 128 over 4096 keys, 128 tiles, 80 and 54; twice those 84 and 104)
+// 26 and 23; 6 x 1024 34 and 33; 512 queries of 32 heads of 128 over 4096 keys, 128 tiles, 80 and 54; twice those 84 and 104; float,
+// B x 512 tokens of 8 heads of 64: 128 tiles 49 and 29, 256 50 and 47, 512 83 and 90; of 128: 128 tiles 87 and 52, 256 89 and 101.  Of
+// 320 tiles, which fill the card once and a quarter, shared ones are the faster in float, 82 and 70: not taken)
 template <typename T, int DP>
 static int attn_fwd_launch(AttnArgs &a, hipStream_t s)
 {

@@ -5,7 +5,8 @@
 // head r / Lq, query r % Lq), 32 to a workgroup, so that keys and values are read once for all heads that share them.
 // A wave takes 32 keys at a time, in tiles of LDS that are its own, and the next 32 are on their way while these are used; no wave
 // waits for another before the end.  (K straight into the operand's registers meant loads of 32 bytes of 32 rows each, eight
-// times over: a decoding step of 32 sequences of up to 4096 keys took 85 us, not 78; today 65 to 75, 4.7 TB/s.)  The waves' and then
+// times over: a decoding step of 32 sequences of up to 4096 keys took 85 us, not 78; today 62 to 75, 4.7 TB/s; in float,
+// where two waves to a compute unit are all that LDS holds, 289, and 131 with heads of 64.)  The waves' and then
 // the workgroups' results are joined by their maxima and sums in a fixed order.
 #include "pf_attn.h"
 
@@ -105,7 +106,7 @@ __global__ __launch_bounds__(64 * SPLIT_WAVES, sizeof(T) * DP <= 256 ? 2 : 1) vo
     float shift = 0.f; // what the row's biases, and its maximum, are relative to (in all parts the same: by all keys that it sees)
     if constexpr (BIAS) {
         __syncthreads();
-        if (left(large, NW))
+        if (__builtin_expect(left(large, NW), 0))
             shift = row_shift(-pos, a.causal && n.nk > pos ? 0 : n.nk - 1 - pos, far, [&](int x) { return mine[lut[far + x] * a.tile_heads]; });
         flat_before = mine[bucket_before(a) * a.tile_heads] - shift;
         flat_after = mine[bucket_after(a) * a.tile_heads] - shift;
@@ -295,8 +296,9 @@ int attn_split_count(const pf_attention_desc *d)
     if (d->Lq * (d->heads_q / d->heads_kv) > 32) {
         // More rows than one product takes: where the ordinary kernel has few tiles of 128 queries and many keys for each.  us, 128
         // queries, bf16, heads of 128: 4 tiles of 8192 keys 98 ordinary and 22 split, 32 of 8192 100 and 63, 64 of 8192 103 and 102, 16 of
-        // 2048 31 and 23, 32 of 2048 32 and 36, 8 of 1024 20 and 17, 8 of 512 14 and 17; float, heads of 64: 8 of 600 32 and 22, 32 of
-        // 2048 86 and 56, 32 of 600 33 and 31.
+        // 2048 31 and 23, 32 of 2048 32 and 36, 8 of 1024 20 and 17, 8 of 512 14 and 17; float, heads of 64: 8 of 600 33 and 23, 16 of
+        // 600 33 and 24, 32 of 600 33 and 31, 32 of 2048 86 and 57, 64 of 2048 87 and 93, 32 of 8192 321 and 161; of 128: 16 of 600 59 and 37, 32 of 600
+        // 59 and 65, 32 of 2048 163 and 124, 64 of 2048 164 and 204, 32 of 8192 618 and 356.
         const i64 tiles = d->B * d->heads_q * ((d->Lq + 127) / 128);
         if (tiles > 64 || tiles * (d->dtype == PF_BF16 ? 128 : 32) > d->Lk) return 0;
     }
