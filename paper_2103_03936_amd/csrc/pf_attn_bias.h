@@ -4,8 +4,6 @@
 #include <math.h>
 #include <stdint.h>
 
-#include <vector>
-
 namespace pf {
 
 constexpr int ATTN_MAX_BORDERS = 128, ATTN_MAX_DISTANCE = 1024, ATTN_MAX_BUCKETS = 256;
@@ -17,27 +15,34 @@ struct AttnBuckets {
     uint16_t border[ATTN_MAX_BORDERS];
 };
 
-// Whether a^m b^k >= c^k d^m, in whole numbers
-inline bool power_product_ge(uint32_t a, int m, uint32_t b, int k, uint32_t c, uint32_t d)
-{
-    const auto product = [&](uint32_t x, int nx, uint32_t y, int ny) {
-        std::vector<uint32_t> r(1, 1u);
+// x^nx y^ny in 32-bit digits, the lowest first: at most 256 factors of at most 1024 = 2^10, 2560 bits.  (No memory is asked for: the
+// callers are entry points that C code calls, where nothing may be thrown.)
+struct PowerProduct {
+    uint32_t w[80];
+    int n = 1;
+    PowerProduct(uint32_t x, int nx, uint32_t y, int ny)
+    {
+        w[0] = 1;
         for (int i = 0; i < nx + ny; ++i) {
             const uint64_t f = i < nx ? x : y;
             uint64_t carry = 0;
-            for (uint32_t &w : r) {
-                carry += f * w;
-                w = (uint32_t)carry;
+            for (int j = 0; j < n; ++j) {
+                carry += f * w[j];
+                w[j] = (uint32_t)carry;
                 carry >>= 32;
             }
-            if (carry) r.push_back((uint32_t)carry);
+            if (carry) w[n++] = (uint32_t)carry;
         }
-        return r;
-    };
-    const std::vector<uint32_t> l = product(a, m, b, k), r = product(c, k, d, m);
-    if (l.size() != r.size()) return l.size() > r.size();
-    for (size_t i = l.size(); i-- > 0;)
-        if (l[i] != r[i]) return l[i] > r[i];
+    }
+};
+static_assert(ATTN_MAX_DISTANCE <= 1 << 10 && ATTN_MAX_BUCKETS / 2 <= 128, "digits of a PowerProduct");
+// Whether a^m b^k >= c^k d^m, in whole numbers; k < m
+inline bool power_product_ge(uint32_t a, int m, uint32_t b, int k, uint32_t c, uint32_t d)
+{
+    const PowerProduct l(a, m, b, k), r(c, k, d, m);
+    if (l.n != r.n) return l.n > r.n;
+    for (int i = l.n; i-- > 0;)
+        if (l.w[i] != r.w[i]) return l.w[i] > r.w[i];
     return true;
 }
 
