@@ -610,8 +610,9 @@ int pf_attention_bwd(const pf_attention_desc *d, const void *Q, const void *K,
 /*                                                                       */
 /* The addresses live in a plan: ask its size, let pf_adamw_plan_fill     */
 /* write it to HOST memory, copy it to the device once (256-byte aligned),*/
-/* and hand it to every step.  A plan holds a counter of the launch that  */
-/* runs: steps of one plan must not overlap.                              */
+/* and hand it to every step, with the size that was asked and the same   */
+/* descriptor (a plan for states of other bits is refused).  A plan holds */
+/* a counter of the launch that runs: steps of one plan must not overlap. */
 /* ------------------------------------------------------------------ */
 typedef struct {
     void *param;

@@ -273,9 +273,10 @@ static i64 adamw_chunks(const pf_adamw_desc *d, const pf_adamw_tensor *q)
     for (i64 i = 0; i < d->tensors; ++i) n += (q[i].count + ADAMW_CHUNK - 1) / ADAMW_CHUNK;
     return n;
 }
-static size_t adamw_bytes(i64 tensors, i64 chunks)
+// (records and pieces are multiples of 8 bytes: 4 bytes more tell a plan for 8-bit states, which a step must not take for the other)
+static size_t adamw_bytes(i64 tensors, i64 chunks, int bits)
 {
-    return sizeof(AdamwHead) + sizeof(AdamwTensor) * (size_t)tensors + sizeof(AdamwChunk) * (size_t)chunks;
+    return sizeof(AdamwHead) + sizeof(AdamwTensor) * (size_t)tensors + sizeof(AdamwChunk) * (size_t)chunks + (bits == 8 ? 4 : 0);
 }
 
 } // namespace pf
@@ -287,14 +288,14 @@ using namespace pf;
 size_t pf_adamw_plan_bytes(const pf_adamw_desc *d, const pf_adamw_tensor *tensors)
 {
     if (adamw_check(d, tensors) != PF_OK) return 0;
-    return adamw_bytes(d->tensors, adamw_chunks(d, tensors));
+    return adamw_bytes(d->tensors, adamw_chunks(d, tensors), d->state_bits);
 }
 
 int pf_adamw_plan_fill(const pf_adamw_desc *d, const pf_adamw_tensor *tensors, void *plan_host, size_t plan_bytes)
 {
     const int status = adamw_check(d, tensors);
     if (status != PF_OK) return status;
-    if (!plan_host || plan_bytes < adamw_bytes(d->tensors, adamw_chunks(d, tensors))) return PF_ERR_WORKSPACE;
+    if (!plan_host || plan_bytes < adamw_bytes(d->tensors, adamw_chunks(d, tensors), d->state_bits)) return PF_ERR_WORKSPACE;
     char *p = (char *)plan_host;
     memset(p, 0, sizeof(AdamwHead));
     p += sizeof(AdamwHead);
@@ -320,15 +321,15 @@ int pf_adamw_step(const pf_adamw_desc *d, void *plan, size_t plan_bytes, const v
     if (d->state_bits != 32 && d->state_bits != 8) return PF_ERR_UNSUPPORTED;
     if (!(d->beta1 >= 0 && d->beta1 < 1 && d->beta2 >= 0 && d->beta2 < 1 && d->eps >= 0)) return PF_ERR_UNSUPPORTED;
     if (any_misaligned({lr, grad_scale}, 4) || any_misaligned({steps}, 8) || any_misaligned({plan}, 256)) return PF_ERR_UNSUPPORTED;
-    const size_t fixed = adamw_bytes(d->tensors, 0);
-    // the table's size says how many pieces it lists: it is the size that pf_adamw_plan_bytes gave
+    const size_t fixed = adamw_bytes(d->tensors, 0, d->state_bits);
+    // the table's size says how many pieces it lists, and for which states: it is the size that pf_adamw_plan_bytes gave
     if (!plan || plan_bytes < fixed || (plan_bytes - fixed) % sizeof(AdamwChunk) != 0) return PF_ERR_WORKSPACE;
     const size_t chunks = (plan_bytes - fixed) / sizeof(AdamwChunk);
     if (chunks >= (size_t)1 << 31) return PF_ERR_WORKSPACE;
     AdamwArgs a;
     a.head = (AdamwHead *)plan;
     a.tensors = (const AdamwTensor *)((char *)plan + sizeof(AdamwHead));
-    a.chunks = (const AdamwChunk *)((char *)plan + fixed);
+    a.chunks = (const AdamwChunk *)((char *)plan + adamw_bytes(d->tensors, 0, 32));
     a.lr = (const float *)lr;
     a.scale = (const float *)grad_scale;
     a.steps = (i64 *)steps;
