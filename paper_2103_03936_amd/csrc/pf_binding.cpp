@@ -166,6 +166,14 @@ long integer(PyObject *o)
     return v;
 }
 
+// (a number that an int does not hold is refused, not taken modulo 2^32)
+int integer32(PyObject *o)
+{
+    const long v = integer(o);
+    if (v != (int)v) throw Fail{PyExc_OverflowError, std::to_string(v) + " does not fit 32 bits"};
+    return (int)v;
+}
+
 template <PyObject *(*F)(PyObject *const *), int N>
 PyObject *entry(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
@@ -728,7 +736,7 @@ struct QkCall {
         d.dtype = dtype_code(Q);
         d.norm = (int)integer(a[1]);
         d.eps = (float)number(a[2]);
-        d.rot_dim = a[3] == Py_None ? d.head_dim : (int)integer(a[3]);
+        d.rot_dim = a[3] == Py_None ? d.head_dim : integer32(a[3]);
         d.theta = number(a[4]);
         d.rotation = (int)integer(a[5]);
         positions = dense(a[0], {sq[0], sq[1]}, at::kInt, dev, "positions");
@@ -853,7 +861,7 @@ struct AttnCall {
             if (tab[0] == 0) throw Fail{PyExc_ValueError, "table has no bucket"};
             table = dense(a[3], at::IntArrayRef(tab, 2), F32, dev, "table");
             d.buckets = (int)std::min<int64_t>(tab[0], INT32_MAX);
-            d.max_distance = (int)integer(a[6]);
+            d.max_distance = integer32(a[6]);
             d.bidirectional = truth(a[7]);
         }
         start = dense(a[8], {sq[0]}, at::kInt, dev, "q_start");
